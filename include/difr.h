@@ -48,7 +48,7 @@
  *   - Return value: a difr_status (0 = DIFR_OK).  Nothing aborts or throws.  On an
  *     error return no kernel has been launched and no output has been touched.
  *   - Problems that are only visible on the device are reported per row in `flags`.
- *   - N == 0 (or S == 0 for difr_seq_reduce) is a successful no-op.
+ *   - N == 0 (or S == 0 for difr_seq_reduce) is a successful no-op; a loss over nothing is written as 0.
  */
 #ifndef DIFR_H
 #define DIFR_H
@@ -72,8 +72,8 @@ typedef enum {
     DIFR_ERR_LAUNCH = 6,      /* the HIP runtime refused the launch                  */
     DIFR_ERR_UNSUPPORTED = 7, /* the current device is not gfx950                    */
     DIFR_ERR_ARGUMENT = 8,    /* sigma <= 0, eps < 0, NaN where a number is needed, or */
-                              /* a top_k / top_p / s / M combination the call does not  */
-                              /* take (stated at each call)                             */
+                              /* a top_k / top_p / s / M combination or a coefficient   */
+                              /* the call does not take (stated at each call)           */
     DIFR_ERR_CAPACITY = 9     /* the batch needs more scratch memory than the library's */
                               /* built-in buffer holds (difr_lmhead_score_static)       */
 } difr_status;
@@ -93,6 +93,8 @@ typedef enum { DIFR_BF16 = 0, DIFR_F32 = 1 } difr_dtype;
                                    /* bit set like -inf (masked, need not be flagged)  */
 #define DIFR_FLAG_SLOW_PATH 8u     /* informational: the row left the streaming fast   */
                                    /* path (re-read of the row)                        */
+#define DIFR_FLAG_CLIPPED 16u      /* difr_policy_loss: the ratio's clip is what counts, */
+                                   /* and nothing flows back through the ratio         */
 
 /*
  * One batch of token rows: "claimed token t*, verifier logits, seed, temperature"
@@ -461,6 +463,124 @@ int difr_classify(const float *scores, const int32_t *ranks, int64_t N, float ta
 int difr_seq_reduce(const float *scores, const uint8_t *row_flags, const int64_t *seq_offsets, int64_t N,
                     int64_t S, float threshold, float *seq_mean, float *seq_max, int32_t *seq_mismatch,
                     uint8_t *seq_flag, void *hip_stream);
+
+/*
+ * Log-probabilities of logged tokens, and what is trained on them.  The rows are those the scores above are taken on, without the
+ * sampler's seeds: the old and reference log-probabilities of a rollout whose tokens the verifier audits, a loss of the caller's own
+ * on them, and the two losses below.
+ *
+ *   p = softmax(x / T) over the row;  logp = ln p_t;  H = -sum_v p_v ln p_v
+ *
+ * A logit of -inf or of the type's lowest value is a masked entry: no probability, no gradient (a row that holds nothing but the
+ * lowest value is uniform).  A row that holds no finite logit, a NaN or +inf, or has a temperature that is not positive and finite,
+ * gets NaN and DIFR_FLAG_NONFINITE; a token outside [0, V) gets a NaN log-probability and DIFR_FLAG_INVALID_CLAIM.  Other rows are
+ * not touched by either.
+ *
+ * Gradients are written in the logits' type, rounded once; `grad` is [N, V] with row pitch ld_grad >= V and may be the logits
+ * themselves (same address and pitch): the row is read before it is overwritten.  Any other overlap gives wrong results.
+ * Sums of a row are formed in fp32 per thread and in fp64 from there on, in a fixed order; everything per row is fp64.
+ */
+typedef struct {
+    const void *logits;        /* as in difr_rows: [N, ld], base aligned to the element size */
+    int32_t dtype;
+    int64_t N, V, ld;
+    float temperature;
+    const float *temperatures; /* optional [N] */
+    const int32_t *tokens;     /* [N] the logged tokens */
+} difr_token_rows;
+
+/*
+ * logp     [N] fp32
+ * stats    [N, 2] fp32 or NULL: (r, sum_v exp((x_v - r) / T)) with r a logit of the row, what difr_token_logprob_backward needs
+ * entropy  [N] fp32 or NULL
+ * flags    [N]
+ * One pass over the logits.
+ */
+int difr_token_logprob(const difr_token_rows *in, float *logp, float *stats, float *entropy, uint8_t *flags, void *hip_stream);
+
+/*
+ * The gradient in the logits of a loss whose gradients in logp and entropy are grad_logp [N] and grad_entropy [N] (or NULL: none):
+ *   grad[n][v] = (1/T) ( grad_logp (1[v = t] - p_v) - grad_entropy p_v (ln p_v + H) )
+ * stats and entropy are the forward call's outputs for the same rows (entropy may be NULL without grad_entropy).  A row whose two
+ * gradients are both 0 gets zeros whatever it holds, and is not read; one with a token outside [0, V) and grad_logp != 0 gets NaN.
+ */
+int difr_token_logprob_backward(const difr_token_rows *in, const float *stats, const float *entropy, const float *grad_logp,
+                                const float *grad_entropy, void *grad, int64_t ld_grad, void *hip_stream);
+
+/*
+ * Clipped policy loss with a KL term.  With r = exp(logp - old), A the advantage, w the weight of a token:
+ *   token_loss = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef kl - entropy_coef H
+ *   kl         = exp(ref - logp) - (ref - logp) - 1       (never negative; its mean is the KL divergence from the reference)
+ *   loss       = sum_n w_n token_loss_n
+ * weights  [N] or NULL (1 / N each): 1 / (number of tokens that count) for a mean over tokens, 1 / (S length of the sequence) for a
+ *          mean over sequences, times whatever the loss is scaled by.  A token of weight 0 is left out: its row is not read, its
+ *          outputs are 0 and so is its gradient, whatever it holds.
+ * old_logp [N] or NULL: old = logp (the ratio is 1, and A flows back as it is).
+ * ref_logp [N] or NULL: no KL term; then kl and kl_coef have to be NULL and 0.
+ * clip_low in [0, 1], clip_high >= 0 (infinity: no clip on that side), coefficients finite (else DIFR_ERR_ARGUMENT).
+ * Outputs: loss [1]; token_loss, logp [N]; entropy, kl [N] or NULL; flags [N], with DIFR_FLAG_CLIPPED where the clip counts; grad
+ * [N, V] or NULL: the gradient of loss.  N == 0 writes loss = 0.
+ */
+typedef struct {
+    const float *advantages;   /* [N] */
+    const float *weights;
+    const float *old_logp, *ref_logp;
+    double clip_low, clip_high, kl_coef, entropy_coef;
+} difr_policy;
+
+int difr_policy_loss(const difr_token_rows *in, const difr_policy *p, float *loss, float *token_loss, float *logp, float *entropy,
+                     float *kl, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream);
+
+/*
+ * Preference loss over pairs of replies.  Rows of sequence s are [seq_offsets[s], seq_offsets[s + 1]) as in difr_seq_reduce;
+ * sequences 2 p and 2 p + 1 are the chosen and the rejected reply of pair p.  With L_s the sum of the sequence's logp, or their mean
+ * (average != 0), R_s = ref_seq_logp[s]:
+ *   h    = beta ((L_c - R_c) - (L_r - R_r)) - margin
+ *   pair_loss = -(1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h);   loss = sum_p pair_weights[p] pair_loss[p]
+ * mask [N] or NULL: a token whose byte is 0 (a prompt's, padding) does not count: its row is not read, its logp and gradient are 0.
+ * An empty sequence, or one that is masked whole, has L = 0.  Rows outside all sequences get their logp and a gradient of 0.
+ * ref_seq_logp [S] or NULL: 0.  pair_weights [S / 2] or NULL: 2 / S each.  S even (DIFR_ERR_SHAPE); beta, margin finite,
+ * label_smoothing in [0, 1] (DIFR_ERR_ARGUMENT).
+ * Outputs: loss [1]; pair_loss [S / 2]; seq_logp [S] (L_s); logp [N]; flags [N]; and for the gradient, all three or none: grad [N, V],
+ * stats [N, 2] as of difr_token_logprob, grad_logp [N] the gradient of loss in each logp.  S == 0 writes loss = 0.
+ */
+typedef struct {
+    const int64_t *seq_offsets; /* [S + 1] */
+    int64_t S;
+    const uint8_t *mask;
+    const float *ref_seq_logp;
+    const float *pair_weights;
+    double beta, label_smoothing, margin;
+    int32_t average;
+} difr_preference;
+
+int difr_preference_loss(const difr_token_rows *in, const difr_preference *p, float *loss, float *pair_loss, float *seq_logp,
+                         float *logp, float *stats, float *grad_logp, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream);
+
+/*
+ * Microscaled 4-bit floating point, for LM heads that are served in it: a verifier that is to reproduce such a server's logits has to
+ * form the product of the same 4-bit values.
+ *   An element is E2M1 (sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6); 32 elements of a row, from a multiple of 32 on, share the scale
+ *   2^(byte - 127).  A block's exponent is floor(log2 of its largest magnitude) - 2, -127 at least; elements are x divided by the scale,
+ *   rounded to nearest, ties to the even code, and 6 from 5 on.  A block with a NaN or an infinity has the scale byte 255 and stands
+ *   for 32 NaN.
+ *   codes  [rows, K / 2]: element 2 i in the lower half of byte i;  scales [rows, K / 32];  both without gaps, codes and scales
+ *   aligned to 16 and 4 bytes; K is d rounded up to a multiple of 128, elements from d on are 0.
+ */
+/* K of rows of d elements (host only). */
+int64_t difr_mx4_padded(int64_t d);
+/* x [N, ld] bf16 or fp32, base aligned to the element size -> codes, scales.  d >= 1. */
+int difr_mx4_quantize(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, uint8_t *codes, uint8_t *scales, void *hip_stream);
+/* The values that the first d elements of every row stand for, [N, ld] bf16 or fp32 (both hold them exactly). */
+int difr_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N, int64_t d, void *x, int32_t dtype, int64_t ld,
+                        void *hip_stream);
+/*
+ * out[n][v] = sum_k a[n][k] b[v][k], fp32 accumulation on the matrix cores, rounded once to bf16 or fp32: the logits of N hidden states
+ * under an LM head of V rows.  a: N rows, b: V rows of K = padded elements each (K % 128 == 0, else DIFR_ERR_SHAPE).  out [N, ld], ld >=
+ * V, base aligned to its element size.  N, V < 2^31, K < 2^24.
+ */
+int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
+                     int64_t V, int64_t K, void *out, int32_t dtype, int64_t ld, void *hip_stream);
 
 /*
  * Test and audit helper: difr_gumbel_score with the exact pre-filter switched off, so that

@@ -11,6 +11,7 @@ library is missing, ``load_library()`` - and with it every call - fails loudly.
 from .binding import (  # noqa: F401
     admissible_count,
     DifrError,
+    FLAG_CLIPPED,
     FLAG_INVALID_CLAIM,
     FLAG_MATCH,
     FLAG_NONFINITE,
@@ -28,11 +29,19 @@ from .binding import (  # noqa: F401
     lmhead_score_static,
     lmhead_workspace_bytes,
     load_library,
+    mx4_dequantize,
+    mx4_padded,
+    mx4_product,
+    mx4_quantize,
     philox4x32_10,
+    policy_loss,
+    preference_loss,
     score_both,
     score_both_admissible,
     score_both_filtered,
     score_both_peaked,
     seq_reduce,
+    token_logprob,
+    token_logprob_backward,
     version,
 )

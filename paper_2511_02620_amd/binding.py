@@ -22,6 +22,7 @@ FLAG_MATCH = 1
 FLAG_INVALID_CLAIM = 2
 FLAG_NONFINITE = 4
 FLAG_SLOW_PATH = 8
+FLAG_CLIPPED = 16
 
 DTYPE_BF16 = 0
 DTYPE_F32 = 1
@@ -84,7 +85,25 @@ class _LikelihoodParams(C.Structure):
                 ("M", C.c_int32), ("z", C.c_void_p)]
 
 
-EXPORTS = ("difr_gumbel_score", "difr_debug_gumbel_score_unfiltered", "difr_ipt_score", "difr_score_both", "difr_score_both_peaked", "difr_score_both_admissible", "difr_admissible_count", "difr_gumbel_likelihood", "difr_ipt_score_filtered", "difr_score_both_filtered", "difr_lmhead_score", "difr_lmhead_score_static", "difr_lmhead_workspace_bytes", "difr_split_workspace_bytes", "difr_score_split", "difr_classify", "difr_seq_reduce", "difr_debug_noise", "difr_debug_gumbel_map",
+class _TokenRows(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int32), ("N", C.c_int64), ("V", C.c_int64), ("ld", C.c_int64),
+                ("temperature", C.c_float), ("temperatures", C.c_void_p), ("tokens", C.c_void_p)]
+
+
+class _Policy(C.Structure):
+    _fields_ = [("advantages", C.c_void_p), ("weights", C.c_void_p), ("old_logp", C.c_void_p), ("ref_logp", C.c_void_p),
+                ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double), ("entropy_coef", C.c_double)]
+
+
+class _Preference(C.Structure):
+    _fields_ = [("seq_offsets", C.c_void_p), ("S", C.c_int64), ("mask", C.c_void_p), ("ref_seq_logp", C.c_void_p),
+                ("pair_weights", C.c_void_p), ("beta", C.c_double), ("label_smoothing", C.c_double), ("margin", C.c_double),
+                ("average", C.c_int32)]
+
+
+EXPORTS = ("difr_gumbel_score", "difr_debug_gumbel_score_unfiltered", "difr_ipt_score", "difr_score_both", "difr_score_both_peaked", "difr_score_both_admissible", "difr_admissible_count", "difr_gumbel_likelihood", "difr_ipt_score_filtered", "difr_score_both_filtered", "difr_lmhead_score", "difr_lmhead_score_static", "difr_lmhead_workspace_bytes", "difr_split_workspace_bytes", "difr_score_split", "difr_classify", "difr_seq_reduce",
+           "difr_token_logprob", "difr_token_logprob_backward", "difr_policy_loss", "difr_preference_loss", "difr_mx4_padded",
+           "difr_mx4_quantize", "difr_mx4_dequantize", "difr_mx4_product", "difr_debug_noise", "difr_debug_gumbel_map",
            "difr_philox4x32_10", "difr_status_string", "difr_version")
 
 
@@ -138,6 +157,18 @@ def load_library():
     lib.difr_ipt_score.restype = C.c_int
     lib.difr_seq_reduce.argtypes = [vp, vp, vp, C.c_int64, C.c_int64, C.c_float, vp, vp, vp, vp, vp]
     lib.difr_seq_reduce.restype = C.c_int
+    lib.difr_token_logprob.argtypes = [C.POINTER(_TokenRows)] + [vp] * 5
+    lib.difr_token_logprob_backward.argtypes = [C.POINTER(_TokenRows)] + [vp] * 5 + [C.c_int64, vp]
+    lib.difr_policy_loss.argtypes = [C.POINTER(_TokenRows), C.POINTER(_Policy)] + [vp] * 7 + [C.c_int64, vp]
+    lib.difr_preference_loss.argtypes = [C.POINTER(_TokenRows), C.POINTER(_Preference)] + [vp] * 8 + [C.c_int64, vp]
+    lib.difr_mx4_padded.argtypes = [C.c_int64]
+    lib.difr_mx4_padded.restype = C.c_int64
+    lib.difr_mx4_quantize.argtypes = [vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, vp, vp, vp]
+    lib.difr_mx4_dequantize.argtypes = [vp, vp, C.c_int64, C.c_int64, vp, C.c_int32, C.c_int64, vp]
+    lib.difr_mx4_product.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_int64, C.c_int64, vp, C.c_int32, C.c_int64, vp]
+    for name in ("token_logprob", "token_logprob_backward", "policy_loss", "preference_loss", "mx4_quantize", "mx4_dequantize",
+                 "mx4_product"):
+        getattr(lib, "difr_" + name).restype = C.c_int
     lib.difr_debug_noise.argtypes = [C.POINTER(_Rows), C.c_int64, C.c_int32, vp, vp]
     lib.difr_debug_noise.restype = C.c_int
     lib.difr_debug_gumbel_map.argtypes = [vp, C.c_int64, vp, vp]
@@ -526,6 +557,168 @@ def classify(scores, ranks, tau, rank_cutoff, V, log2_admissible=None):
             _check(log2_admissible, torch.float32, N, "log2_admissible", dev)
         _refused("difr_classify", out, checks)
     return out
+
+
+def _token_rows(logits, V, tokens, temperatures):
+    """Checks of the calls on logged tokens; (device, rows, vocabulary)."""
+    if not logits.is_cuda:
+        raise ValueError("logits must be a GPU tensor")
+    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
+        raise ValueError("logits must be 2-D with unit column stride")
+    if logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be bfloat16 or float32")
+    N, dev = logits.shape[0], logits.device
+    _check(tokens, torch.int32, N, "tokens", dev)
+    if tokens is None:
+        raise ValueError("tokens must be a contiguous 1-D int32 tensor of %d elements" % N)
+    _check(temperatures, torch.float32, N, "temperatures", dev)
+    return dev, N, logits.shape[1] if V is None else int(V)
+
+
+def _check_grad(out, logits, V):
+    if out is None:
+        return
+    N = logits.shape[0]
+    if out.device != logits.device or out.dtype != logits.dtype or tuple(out.shape) != (N, V) or (V > 1 and out.stride(1) != 1) or (
+            N > 1 and out.stride(0) < V):
+        raise ValueError("out must be a [%d, %d] %s tensor with unit column stride on %s" % (N, V, logits.dtype, logits.device))
+    raise ValueError("out must be the logits themselves or not overlap them")
+
+
+def token_logprob(logits, temperature, tokens, temperatures=None, V=None, want_entropy=False):
+    """difr_token_logprob: log-probabilities of the logged tokens (int32 [N]) under softmax(logits / temperature).
+    logits [N, >=V] bf16/fp32 on the GPU.  Returns a dict of device tensors: logp [N], stats [N, 2] (for
+    :func:`token_logprob_backward`), entropy [N] if wanted, flags [N]."""
+    out = (_native or _load_native()).token_logprob(logits, V if V is None else int(V), float(temperature), tokens, temperatures,
+                                                    want_entropy)
+    if out.__class__ is not dict:
+        _refused("difr_token_logprob", out, lambda: _token_rows(logits, V, tokens, temperatures))
+    return out
+
+
+def token_logprob_backward(logits, temperature, tokens, stats, grad_logp, entropy=None, grad_entropy=None, temperatures=None, V=None,
+                           out=None):
+    """difr_token_logprob_backward: the gradient [N, V] in the logits, in their type, of a loss whose gradients in the
+    log-probabilities and entropies are grad_logp and grad_entropy (fp32 [N]).  stats, entropy: of :func:`token_logprob` on the same
+    rows.  out: where to put it; the logits themselves are overwritten, any other overlap is refused."""
+    got = (_native or _load_native()).token_logprob_backward(logits, V if V is None else int(V), float(temperature), tokens,
+                                                             temperatures, stats, grad_logp, entropy, grad_entropy, out)
+    if got is None:
+        dev, N, cols = _token_rows(logits, V, tokens, temperatures)
+        if stats.device != dev or stats.dtype != torch.float32 or tuple(stats.shape) != (N, 2) or not stats.is_contiguous():
+            raise ValueError("stats must be a contiguous [%d, 2] float32 tensor on %s" % (N, dev))
+        for t, name in ((grad_logp, "grad_logp"), (entropy, "entropy"), (grad_entropy, "grad_entropy")):
+            _check(t, torch.float32, N, name, dev)
+        if grad_entropy is not None and entropy is None:
+            raise ValueError("grad_entropy needs entropy, the output of token_logprob")
+        _check_grad(out, logits, cols)
+    if got.__class__ is int or got is None:
+        _refused("difr_token_logprob_backward", got, lambda: None)
+    return got
+
+
+def policy_loss(logits, temperature, tokens, advantages, weights=None, old_logp=None, ref_logp=None, clip_low=0.2, clip_high=0.2,
+                kl_coef=0.0, entropy_coef=0.0, temperatures=None, V=None, want_entropy=False, want_grad=True, out=None):
+    """difr_policy_loss: the clipped policy loss of the logged tokens with a KL term against ref_logp, and its gradient in the
+    logits.  advantages, weights, old_logp, ref_logp fp32 [N]; weights None: 1 / N each, a token of weight 0 is left out (its row is
+    not read).  Returns a dict of device tensors: loss [1], token_loss, logp, entropy (if wanted), kl (with ref_logp), flags [N], and
+    grad [N, V] with want_grad, in `out` if that is given (the logits themselves are overwritten, any other overlap is refused)."""
+    got = (_native or _load_native()).policy_loss(logits, V if V is None else int(V), float(temperature), tokens, temperatures,
+                                                  advantages, weights, old_logp, ref_logp, float(clip_low), float(clip_high),
+                                                  float(kl_coef), float(entropy_coef), want_entropy, want_grad, out)
+    if got.__class__ is not dict:
+        def checks():
+            dev, N, cols = _token_rows(logits, V, tokens, temperatures)
+            for t, name in ((advantages, "advantages"), (weights, "weights"), (old_logp, "old_logp"), (ref_logp, "ref_logp")):
+                _check(t, torch.float32, N, name, dev)
+            if advantages is None:
+                raise ValueError("advantages must be a contiguous 1-D float32 tensor of %d elements" % N)
+            _check_grad(out, logits, cols)
+        _refused("difr_policy_loss", got, checks)
+    return got
+
+
+def preference_loss(logits, temperature, tokens, seq_offsets, beta, mask=None, ref_seq_logp=None, pair_weights=None,
+                    label_smoothing=0.0, margin=0.0, average=False, temperatures=None, V=None, want_grad=True, out=None):
+    """difr_preference_loss: sequences 2 p and 2 p + 1 of seq_offsets (int64 [S + 1]) are the chosen and the rejected reply of pair
+    p.  mask uint8 [N] (0: does not count), ref_seq_logp fp32 [S], pair_weights fp32 [S / 2].  Returns a dict of device tensors:
+    loss [1], pair_loss [S / 2], seq_logp [S], logp, flags [N], and with want_grad stats, grad_logp [N] and grad [N, V], in `out` if that
+    is given (the logits themselves are overwritten, any other overlap is refused)."""
+    got = (_native or _load_native()).preference_loss(logits, V if V is None else int(V), float(temperature), tokens, temperatures,
+                                                      seq_offsets, float(beta), mask, ref_seq_logp, pair_weights,
+                                                      float(label_smoothing), float(margin), average, want_grad, out)
+    if got.__class__ is not dict:
+        def checks():
+            dev, N, cols = _token_rows(logits, V, tokens, temperatures)
+            if (seq_offsets.device != dev or seq_offsets.dtype != torch.int64 or seq_offsets.dim() != 1 or not seq_offsets.is_contiguous()
+                    or seq_offsets.shape[0] % 2 != 1):
+                raise ValueError("seq_offsets must be a contiguous 1-D int64 GPU tensor of S+1 elements, S even")
+            S = seq_offsets.shape[0] - 1
+            _check(mask, torch.uint8, N, "mask", dev)
+            _check(ref_seq_logp, torch.float32, S, "ref_seq_logp", dev)
+            _check(pair_weights, torch.float32, S // 2, "pair_weights", dev)
+            _check_grad(out, logits, cols)
+        _refused("difr_preference_loss", got, checks)
+    return got
+
+
+def mx4_padded(d) -> int:
+    """difr_mx4_padded: elements of a row of codes for rows of d elements (whole slabs of 128)."""
+    return int(load_library().difr_mx4_padded(int(d)))
+
+
+def mx4_quantize(x):
+    """difr_mx4_quantize: the rows of x [N, d] (bf16/fp32 on the GPU, unit column stride) in microscaled 4-bit floating point.
+    Returns a dict of uint8 tensors: codes [N, K / 2], two elements a byte, and scales [N, K / 32], K = mx4_padded(d)."""
+    got = (_native or _load_native()).mx4_quantize(x)
+    if got.__class__ is not dict:
+        def checks():
+            if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+                raise ValueError("x must be a 2-D bfloat16 or float32 GPU tensor with unit column stride")
+        _refused("difr_mx4_quantize", got, checks)
+    return got
+
+
+def _check_coded(codes, scales, name):
+    if not codes.is_cuda or codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_contiguous() or codes.shape[1] % 64:
+        raise ValueError("%scodes must be a contiguous [rows, K / 2] uint8 GPU tensor, K a multiple of 128" % name)
+    if (scales.device != codes.device or scales.dtype != torch.uint8 or not scales.is_contiguous()
+            or tuple(scales.shape) != (codes.shape[0], codes.shape[1] // 16)):
+        raise ValueError("%sscales must be a contiguous [%d, %d] uint8 tensor on the device of the codes" % (
+            name, codes.shape[0], codes.shape[1] // 16))
+
+
+def _check_float_type(dtype):
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be torch.bfloat16 or torch.float32")
+    return dtype == torch.float32
+
+
+def mx4_dequantize(codes, scales, columns, dtype=torch.bfloat16):
+    """difr_mx4_dequantize: the values [rows, columns] that codes and scales stand for (bf16 and fp32 both hold them exactly)."""
+    got = (_native or _load_native()).mx4_dequantize(codes, scales, int(columns), _check_float_type(dtype))
+    if got is None or got.__class__ is int:
+        def checks():
+            _check_coded(codes, scales, "")
+            raise ValueError("columns must be a number of elements whose rows have codes for %d" % (2 * codes.shape[1]))
+        _refused("difr_mx4_dequantize", got, checks)
+    return got
+
+
+def mx4_product(a_codes, a_scales, b_codes, b_scales, dtype=torch.bfloat16, out=None):
+    """difr_mx4_product: [N, V] products of the N rows of a (hidden states) and the V rows of b (an LM head), both as
+    :func:`mx4_quantize` returns them.  out: a [N, V] tensor of that dtype (unit column stride) to write into."""
+    got = (_native or _load_native()).mx4_product(a_codes, a_scales, b_codes, b_scales, _check_float_type(dtype), out)
+    if got is None or got.__class__ is int:
+        def checks():
+            _check_coded(a_codes, a_scales, "a_")
+            _check_coded(b_codes, b_scales, "b_")
+            if b_codes.device != a_codes.device or b_codes.shape[1] != a_codes.shape[1] or not a_codes.shape[1]:
+                raise ValueError("b must have rows as long as those of a, on the same device")
+            raise ValueError("out must be a [%d, %d] %s tensor with unit column stride on the device of the codes" % (
+                a_codes.shape[0], b_codes.shape[0], dtype))
+        _refused("difr_mx4_product", got, checks)
+    return got
 
 
 def debug_noise(logits, temperature, seeds, seq_ids, positions, row, stream, V=None):

@@ -11,6 +11,7 @@
 #include "gumbel_stream.hpp"
 #include "ipt_stream.hpp"
 #include "lmhead.hpp"
+#include "token_loss.hpp"
 
 // Built-in workspace of difr_lmhead_score_static: every GPU the library runs on holds its own copy, at its own
 // address, until the process ends.  In host code the name `scratch` is only a handle for hipGetSymbolAddress;
@@ -119,6 +120,29 @@ int validate_lmhead(const difr_lmhead *in, difr::LmHeadBatch *b)
     b->claimed_gumbel = in->claimed_gumbel;
     b->claimed_ipt = in->claimed_ipt;
     return DIFR_OK;
+}
+
+int validate_token_rows(const difr_token_rows *in, difr::TokenRows *b)
+{
+    if (!in) return DIFR_ERR_NULL;
+    if (in->N < 0 || in->V < 0 || in->ld < 0) return DIFR_ERR_SHAPE;
+    if (in->N >= (int64_t)1 << 31 || in->V >= (int64_t)1 << 31) return DIFR_ERR_SHAPE;
+    if (in->dtype != DIFR_BF16 && in->dtype != DIFR_F32) return DIFR_ERR_DTYPE;
+    if (in->N > 0) {
+        if (in->V == 0 || in->ld < in->V) return DIFR_ERR_SHAPE;
+        if (!in->logits || !in->tokens) return DIFR_ERR_NULL;
+        if (!in->temperatures && !(in->temperature > 0.0f && isfinite(in->temperature))) return DIFR_ERR_TEMPERATURE;
+    }
+    if ((uintptr_t)in->logits % (in->dtype == DIFR_BF16 ? 2u : 4u)) return DIFR_ERR_ALIGN;
+    *b = difr::TokenRows{in->logits, in->dtype, in->N, in->V, in->ld, in->temperature, in->temperatures, in->tokens};
+    return DIFR_OK;
+}
+
+// the gradient of N > 0 rows
+int validate_grad(const difr::TokenRows &b, const void *grad, int64_t ld_grad)
+{
+    if (ld_grad < b.V) return DIFR_ERR_SHAPE;
+    return (uintptr_t)grad % (b.dtype == DIFR_BF16 ? 2u : 4u) ? DIFR_ERR_ALIGN : DIFR_OK;
 }
 
 }  // namespace
@@ -451,6 +475,123 @@ int difr_classify(const float *scores, const int32_t *ranks, int64_t N, float ta
                : DIFR_OK;
 }
 
+int difr_token_logprob(const difr_token_rows *in, float *logp, float *stats, float *entropy, uint8_t *flags, void *hip_stream)
+{
+    difr::TokenRows b;
+    int rc = validate_token_rows(in, &b);
+    if (rc != DIFR_OK) return rc;
+    if (b.N == 0) return DIFR_OK;
+    if (!logp || !flags) return DIFR_ERR_NULL;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_token_logprob(b, nullptr, difr::LogProbOutputs{logp, stats, entropy, flags}, (hipStream_t)hip_stream)
+               ? DIFR_ERR_LAUNCH
+               : DIFR_OK;
+}
+
+int difr_token_logprob_backward(const difr_token_rows *in, const float *stats, const float *entropy, const float *grad_logp,
+                                const float *grad_entropy, void *grad, int64_t ld_grad, void *hip_stream)
+{
+    difr::TokenRows b;
+    int rc = validate_token_rows(in, &b);
+    if (rc != DIFR_OK) return rc;
+    if (b.N == 0) return DIFR_OK;
+    if (!stats || !grad_logp || !grad || (grad_entropy && !entropy)) return DIFR_ERR_NULL;
+    if ((rc = validate_grad(b, grad, ld_grad)) != DIFR_OK) return rc;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_token_logprob_backward(b, stats, entropy, grad_logp, grad_entropy, grad, ld_grad, (hipStream_t)hip_stream)
+               ? DIFR_ERR_LAUNCH
+               : DIFR_OK;
+}
+
+int difr_policy_loss(const difr_token_rows *in, const difr_policy *p, float *loss, float *token_loss, float *logp, float *entropy,
+                     float *kl, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream)
+{
+    difr::TokenRows b;
+    int rc = validate_token_rows(in, &b);
+    if (rc != DIFR_OK) return rc;
+    if (!p || !loss) return DIFR_ERR_NULL;
+    if (!(p->clip_low >= 0.0 && p->clip_low <= 1.0) || !(p->clip_high >= 0.0) || !isfinite(p->kl_coef) || !isfinite(p->entropy_coef) ||
+        (!p->ref_logp && (p->kl_coef != 0.0 || kl)))
+        return DIFR_ERR_ARGUMENT;
+    if (b.N > 0) {
+        if (!p->advantages || !token_loss || !logp || !flags) return DIFR_ERR_NULL;
+        if (grad && (rc = validate_grad(b, grad, ld_grad)) != DIFR_OK) return rc;
+    }
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    const difr::PolicyParams q{p->advantages, p->weights, p->old_logp, p->ref_logp, p->clip_low, p->clip_high, p->kl_coef, p->entropy_coef};
+    const difr::PolicyOutputs o{loss, token_loss, {logp, nullptr, entropy, flags}, kl, grad, ld_grad};
+    return difr::launch_policy_loss(b, q, o, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+}
+
+int difr_preference_loss(const difr_token_rows *in, const difr_preference *p, float *loss, float *pair_loss, float *seq_logp,
+                         float *logp, float *stats, float *grad_logp, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream)
+{
+    difr::TokenRows b;
+    int rc = validate_token_rows(in, &b);
+    if (rc != DIFR_OK) return rc;
+    if (!p || !loss) return DIFR_ERR_NULL;
+    if (p->S < 0 || p->S % 2 || p->S >= (int64_t)1 << 31) return DIFR_ERR_SHAPE;
+    if (!isfinite(p->beta) || !isfinite(p->margin) || !(p->label_smoothing >= 0.0 && p->label_smoothing <= 1.0)) return DIFR_ERR_ARGUMENT;
+    if (p->S > 0 && (!p->seq_offsets || !pair_loss || !seq_logp)) return DIFR_ERR_NULL;
+    if (b.N > 0) {
+        if (!logp || !flags) return DIFR_ERR_NULL;
+        if (grad && (!stats || !grad_logp)) return DIFR_ERR_NULL;
+        if (grad && (rc = validate_grad(b, grad, ld_grad)) != DIFR_OK) return rc;
+    }
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    const difr::PreferenceParams q{p->seq_offsets, p->S, p->mask, p->ref_seq_logp, p->pair_weights, p->beta, p->label_smoothing, p->margin,
+                                   p->average != 0};
+    const difr::PreferenceOutputs o{loss, pair_loss, seq_logp, {logp, stats, nullptr, flags}, grad ? grad_logp : nullptr, grad, ld_grad};
+    return difr::launch_preference_loss(b, q, o, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+}
+
+int64_t difr_mx4_padded(int64_t d) { return d <= 0 ? 0 : (d + difr::kMxSlab - 1) / difr::kMxSlab * difr::kMxSlab; }
+
+static int validate_mx4(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, const void *codes, const void *scales)
+{
+    if (N < 0 || d < 1 || ld < d || N >= (int64_t)1 << 31 || d >= (int64_t)1 << 24) return DIFR_ERR_SHAPE;
+    if (dtype != DIFR_BF16 && dtype != DIFR_F32) return DIFR_ERR_DTYPE;
+    if (N == 0) return DIFR_OK;
+    if (!x || !codes || !scales) return DIFR_ERR_NULL;
+    if ((uintptr_t)x % (dtype == DIFR_BF16 ? 2u : 4u) || (uintptr_t)codes % 16u || (uintptr_t)scales % 4u) return DIFR_ERR_ALIGN;
+    return DIFR_OK;
+}
+
+int difr_mx4_quantize(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, uint8_t *codes, uint8_t *scales, void *hip_stream)
+{
+    int rc = validate_mx4(x, dtype, N, d, ld, codes, scales);
+    if (rc != DIFR_OK || N == 0) return rc;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_mx4_quantize(x, dtype, N, d, ld, codes, scales, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+}
+
+int difr_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N, int64_t d, void *x, int32_t dtype, int64_t ld,
+                        void *hip_stream)
+{
+    int rc = validate_mx4(x, dtype, N, d, ld, codes, scales);
+    if (rc != DIFR_OK || N == 0) return rc;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_mx4_dequantize(codes, scales, N, d, x, dtype, ld, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+}
+
+int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
+                     int64_t V, int64_t K, void *out, int32_t dtype, int64_t ld, void *hip_stream)
+{
+    if (N < 0 || V < 0 || ld < V || N >= (int64_t)1 << 31 || V >= (int64_t)1 << 31) return DIFR_ERR_SHAPE;
+    if (K < difr::kMxSlab || K % difr::kMxSlab || K >= (int64_t)1 << 24) return DIFR_ERR_SHAPE;
+    if (dtype != DIFR_BF16 && dtype != DIFR_F32) return DIFR_ERR_DTYPE;
+    if (N == 0 || V == 0) return DIFR_OK;
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return DIFR_ERR_NULL;
+    if (((uintptr_t)a_codes | (uintptr_t)b_codes) % 16u || ((uintptr_t)a_scales | (uintptr_t)b_scales) % 4u ||
+        (uintptr_t)out % (dtype == DIFR_BF16 ? 2u : 4u))
+        return DIFR_ERR_ALIGN;
+    int rc = check_device();
+    if (rc != DIFR_OK) return rc;
+    return difr::launch_mx4_product(a_codes, a_scales, N, b_codes, b_scales, V, K, out, dtype, ld, (hipStream_t)hip_stream)
+               ? DIFR_ERR_LAUNCH
+               : DIFR_OK;
+}
+
 int difr_debug_noise(const difr_rows *in, int64_t row, int32_t stream, uint32_t *bits, void *hip_stream)
 {
     difr::RowBatch b;
@@ -507,7 +648,7 @@ const char *difr_status_string(int status)
         case DIFR_ERR_ALIGN: return "logits pointer not aligned to its element size";
         case DIFR_ERR_LAUNCH: return "HIP kernel launch failed";
         case DIFR_ERR_UNSUPPORTED: return "current device is not gfx950";
-        case DIFR_ERR_ARGUMENT: return "bad scalar argument (sigma, eps, threshold, delta, or a top_k / top_p / s / M combination the call does not take)";
+        case DIFR_ERR_ARGUMENT: return "bad scalar argument (sigma, eps, threshold, delta, a coefficient of a loss, or a top_k / top_p / s / M combination the call does not take)";
         case DIFR_ERR_CAPACITY: return "batch needs more scratch memory than the library's built-in buffer holds";
         default: return "unknown status";
     }

@@ -41,7 +41,15 @@ namespace {
     X(difr_lmhead_workspace_bytes)                                                                                      \
     X(difr_lmhead_score)                                                                                                \
     X(difr_seq_reduce)                                                                                                  \
-    X(difr_classify)
+    X(difr_classify)                                                                                                    \
+    X(difr_token_logprob)                                                                                               \
+    X(difr_token_logprob_backward)                                                                                      \
+    X(difr_policy_loss)                                                                                                 \
+    X(difr_preference_loss)                                                                                             \
+    X(difr_mx4_padded)                                                                                                  \
+    X(difr_mx4_quantize)                                                                                                \
+    X(difr_mx4_dequantize)                                                                                              \
+    X(difr_mx4_product)
 
 struct Entries {
 #define X(name) decltype(&::name) name = nullptr;
@@ -53,7 +61,8 @@ struct Entries {
 #define DIFR_KEYS(X)                                                                                                    \
     X(margin) X(argmax) X(max_score) X(claimed_score) X(flags) X(logit_rank) X(dist) X(cdf_lo) X(cdf_hi) X(u)           \
     X(ipt_token) X(log_mass) X(count) X(log2_count) X(kept) X(pi) X(log_pi) X(tau) X(active) X(seq_mean) X(seq_max)     \
-    X(seq_mismatch) X(seq_flag) X(cls) X(bits)
+    X(seq_mismatch) X(seq_flag) X(cls) X(bits) X(logp) X(stats) X(entropy) X(loss) X(token_loss) X(kl) X(grad)           \
+    X(grad_logp) X(pair_loss) X(seq_logp) X(codes) X(scales)
 namespace key {
 #define X(name) PyObject *name = nullptr;
 DIFR_KEYS(X)
@@ -515,6 +524,254 @@ PyObject *classify(PyObject *const *a)
     return one(enter(dev, [&](void *s) { return lib.difr_classify(scores, ranks, N, tau, cutoff, V, log2_adm, cls, bits, s); }), o);
 }
 
+// ---- log-probabilities and losses ----
+
+// The first five arguments of these calls: logits, V, temperature, tokens, temperatures.
+struct TokenRows {
+    difr_token_rows in;
+    int64_t N;
+    c10::Device dev;
+    at::ScalarType type;
+
+    explicit TokenRows(PyObject *const *a) : dev(c10::kCUDA)
+    {
+        const at::Tensor &x = tensor(a[0]);
+        if (!x.is_cuda() || x.dim() != 2 || (x.stride(1) != 1 && x.size(1) > 1)) throw Refused();
+        type = x.scalar_type();
+        if (type != at::kBFloat16 && type != at::kFloat) throw Refused();
+        in.dtype = type == at::kFloat ? DIFR_F32 : DIFR_BF16;
+        dev = x.device();
+        N = x.size(0);
+        in.logits = x.data_ptr();
+        in.N = N;
+        in.V = a[1] == Py_None ? x.size(1) : whole(a[1]);
+        in.ld = N > 1 ? x.stride(0) : std::max(x.size(1), N ? x.stride(0) : (int64_t)0);
+        in.temperature = (float)number(a[2]);
+        in.tokens = (const int32_t *)vec(a[3], at::kInt, N, dev);
+        in.temperatures = (const float *)vec_or_null(a[4], at::kFloat, N, dev);
+    }
+    size_t element() const { return in.dtype == DIFR_F32 ? 4 : 2; }
+};
+constexpr int kTokenRowArgs = 5;
+
+// Where a gradient [N, V] goes: a tensor of the caller's (the logits themselves, or one that does not overlap them), or a new one.
+struct Grad {
+    void *data = nullptr;
+    int64_t ld = 0;
+    at::Tensor t;
+    Grad(const TokenRows &r, PyObject *out, Outputs &o)
+    {
+        if (out == Py_None) {
+            t = o.make(r.type, {r.N, std::max(r.in.V, (int64_t)0)});
+            data = t.data_ptr();
+            ld = std::max(r.in.V, (int64_t)1);
+            return;
+        }
+        t = tensor(out);
+        if (t.device() != r.dev || t.scalar_type() != r.type || t.dim() != 2 || t.size(0) != r.N || t.size(1) != r.in.V ||
+            (t.stride(1) != 1 && t.size(1) > 1))
+            throw Refused();
+        data = t.data_ptr();
+        ld = r.N > 1 ? t.stride(0) : r.in.ld;  // (the pitch of a single row is never used)
+        if (r.N > 1 && ld < r.in.V) throw Refused();
+        const char *g = (const char *)data, *x = (const char *)r.in.logits;
+        const size_t e = r.element();
+        const size_t gn = r.N ? ((r.N - 1) * ld + r.in.V) * e : 0, xn = r.N ? ((r.N - 1) * r.in.ld + r.in.V) * e : 0;
+        if (g < x + xn && x < g + gn && !(g == x && ld == r.in.ld)) throw Refused();
+    }
+    PyObject *wrap()
+    {
+        PyObject *w = THPVariable_Wrap(std::move(t));
+        if (!w) throw python_error();
+        return w;
+    }
+    void into(Outputs &o)
+    {
+        THPObjectPtr w(wrap());
+        if (PyDict_SetItem(o.dict, key::grad, w) < 0) throw python_error();
+    }
+};
+
+// token rows, want_entropy
+PyObject *token_logprob(PyObject *const *a)
+{
+    TokenRows r(a);
+    Outputs o(r.dev);
+    float *logp = o.f32(key::logp, r.N);
+    float *stats = (float *)o.add(key::stats, at::kFloat, {r.N, 2});
+    float *entropy = truth(a[kTokenRowArgs]) ? o.f32(key::entropy, r.N) : nullptr;
+    uint8_t *flags = o.u8(key::flags, r.N);
+    return one(enter(r.dev, [&](void *s) { return lib.difr_token_logprob(&r.in, logp, stats, entropy, flags, s); }), o);
+}
+
+// token rows, stats, grad_logp, entropy, grad_entropy, out
+PyObject *token_logprob_backward(PyObject *const *a)
+{
+    TokenRows r(a);
+    a += kTokenRowArgs;
+    const at::Tensor &st = tensor(a[0]);
+    if (st.device() != r.dev || st.scalar_type() != at::kFloat || st.dim() != 2 || st.size(0) != r.N || st.size(1) != 2 || !st.is_contiguous())
+        throw Refused();
+    const float *stats = (const float *)st.data_ptr(), *ga = (const float *)vec(a[1], at::kFloat, r.N, r.dev);
+    const float *entropy = (const float *)vec_or_null(a[2], at::kFloat, r.N, r.dev);
+    const float *ge = (const float *)vec_or_null(a[3], at::kFloat, r.N, r.dev);
+    if (ge && !entropy) throw Refused();
+    Outputs o(r.dev);
+    Grad g(r, a[4], o);
+    const int rc = enter(r.dev, [&](void *s) { return lib.difr_token_logprob_backward(&r.in, stats, entropy, ga, ge, g.data, g.ld, s); });
+    return rc ? PyLong_FromLong(rc) : g.wrap();
+}
+
+// token rows, advantages, weights, old_logp, ref_logp, clip_low, clip_high, kl_coef, entropy_coef, want_entropy, want_grad, out
+PyObject *policy_loss(PyObject *const *a)
+{
+    TokenRows r(a);
+    a += kTokenRowArgs;
+    difr_policy p;
+    p.advantages = (const float *)vec(a[0], at::kFloat, r.N, r.dev);
+    p.weights = (const float *)vec_or_null(a[1], at::kFloat, r.N, r.dev);
+    p.old_logp = (const float *)vec_or_null(a[2], at::kFloat, r.N, r.dev);
+    p.ref_logp = (const float *)vec_or_null(a[3], at::kFloat, r.N, r.dev);
+    p.clip_low = number(a[4]), p.clip_high = number(a[5]), p.kl_coef = number(a[6]), p.entropy_coef = number(a[7]);
+    Outputs o(r.dev);
+    float *loss = o.f32(key::loss, 1), *token_loss = o.f32(key::token_loss, r.N), *logp = o.f32(key::logp, r.N);
+    float *entropy = truth(a[8]) ? o.f32(key::entropy, r.N) : nullptr;
+    float *kl = p.ref_logp ? o.f32(key::kl, r.N) : nullptr;
+    uint8_t *flags = o.u8(key::flags, r.N);
+    void *grad = nullptr;
+    int64_t ld = 0;
+    if (truth(a[9])) {
+        Grad g(r, a[10], o);
+        grad = g.data, ld = g.ld;
+        g.into(o);
+    }
+    if (!r.N) grad = nullptr;
+    return one(enter(r.dev, [&](void *s) {
+                   return lib.difr_policy_loss(&r.in, &p, loss, token_loss, logp, entropy, kl, flags, grad, ld, s);
+               }), o);
+}
+
+// token rows, seq_offsets, beta, mask, ref_seq_logp, pair_weights, label_smoothing, margin, average, want_grad, out
+PyObject *preference_loss(PyObject *const *a)
+{
+    TokenRows r(a);
+    a += kTokenRowArgs;
+    difr_preference p;
+    p.seq_offsets = (const int64_t *)vec(a[0], at::kLong, -1, r.dev);
+    p.S = tensor(a[0]).size(0) - 1;
+    if (p.S < 0 || p.S % 2) throw Refused();
+    p.beta = number(a[1]);
+    p.mask = (const uint8_t *)vec_or_null(a[2], at::kByte, r.N, r.dev);
+    p.ref_seq_logp = (const float *)vec_or_null(a[3], at::kFloat, p.S, r.dev);
+    p.pair_weights = (const float *)vec_or_null(a[4], at::kFloat, p.S / 2, r.dev);
+    p.label_smoothing = number(a[5]), p.margin = number(a[6]), p.average = truth(a[7]);
+    Outputs o(r.dev);
+    float *loss = o.f32(key::loss, 1), *pair_loss = o.f32(key::pair_loss, p.S / 2), *seq_logp = o.f32(key::seq_logp, p.S);
+    float *logp = o.f32(key::logp, r.N), *stats = nullptr, *grad_logp = nullptr;
+    uint8_t *flags = o.u8(key::flags, r.N);
+    void *grad = nullptr;
+    int64_t ld = 0;
+    if (truth(a[8])) {
+        stats = (float *)o.add(key::stats, at::kFloat, {r.N, 2});
+        grad_logp = o.f32(key::grad_logp, r.N);
+        Grad g(r, a[9], o);
+        grad = g.data, ld = g.ld;
+        g.into(o);
+    }
+    if (!r.N) grad = nullptr;
+    return one(enter(r.dev, [&](void *s) {
+                   return lib.difr_preference_loss(&r.in, &p, loss, pair_loss, seq_logp, logp, stats, grad_logp, flags, grad, ld, s);
+               }), o);
+}
+
+// ---- 4-bit floating point ----
+
+int32_t float_type(at::ScalarType t)
+{
+    if (t == at::kBFloat16) return DIFR_BF16;
+    if (t == at::kFloat) return DIFR_F32;
+    throw Refused();
+}
+
+// [rows, K / 2] codes and [rows, K / 32] scales
+struct Coded {
+    const uint8_t *codes, *scales;
+    int64_t rows, K;
+    c10::Device dev;
+    Coded(PyObject *c, PyObject *s) : dev(c10::kCUDA)
+    {
+        const at::Tensor &x = tensor(c), &y = tensor(s);
+        if (!x.is_cuda() || x.scalar_type() != at::kByte || x.dim() != 2 || !x.is_contiguous()) throw Refused();
+        dev = x.device();
+        rows = x.size(0), K = 2 * x.size(1);
+        if (y.device() != dev || y.scalar_type() != at::kByte || y.dim() != 2 || !y.is_contiguous() || y.size(0) != rows || K % 128 ||
+            y.size(1) != K / 32)
+            throw Refused();
+        codes = (const uint8_t *)x.data_ptr(), scales = (const uint8_t *)y.data_ptr();
+    }
+};
+
+// x
+PyObject *mx4_quantize(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[0]);
+    if (!x.is_cuda() || x.dim() != 2 || (x.stride(1) != 1 && x.size(1) > 1)) throw Refused();
+    const int32_t dtype = float_type(x.scalar_type());
+    const int64_t N = x.size(0), d = x.size(1), K = lib.difr_mx4_padded(d);
+    const int64_t ld = N > 1 ? x.stride(0) : d;
+    Outputs o(x.device());
+    uint8_t *codes = (uint8_t *)o.add(key::codes, at::kByte, {N, K / 2}), *scales = (uint8_t *)o.add(key::scales, at::kByte, {N, K / 32});
+    return one(enter(x.device(), [&](void *s) { return lib.difr_mx4_quantize(x.data_ptr(), dtype, N, d, ld, codes, scales, s); }), o);
+}
+
+PyObject *wrapped(int rc, at::Tensor &t)
+{
+    if (rc) return PyLong_FromLong(rc);
+    PyObject *w = THPVariable_Wrap(std::move(t));
+    if (!w) throw python_error();
+    return w;
+}
+
+// codes, scales, columns, fp32
+PyObject *mx4_dequantize(PyObject *const *a)
+{
+    const Coded c(a[0], a[1]);
+    const int64_t d = whole(a[2]);
+    if (d < 1 || lib.difr_mx4_padded(d) != c.K) throw Refused();
+    const bool f32 = truth(a[3]);
+    Outputs o(c.dev);
+    at::Tensor t = o.make(f32 ? at::kFloat : at::kBFloat16, {c.rows, d});
+    const int rc = enter(c.dev, [&](void *s) {
+        return lib.difr_mx4_dequantize(c.codes, c.scales, c.rows, d, t.data_ptr(), f32 ? DIFR_F32 : DIFR_BF16, d, s);
+    });
+    return wrapped(rc, t);
+}
+
+// a_codes, a_scales, b_codes, b_scales, fp32, out
+PyObject *mx4_product(PyObject *const *a)
+{
+    const Coded x(a[0], a[1]), y(a[2], a[3]);
+    if (y.dev != x.dev || y.K != x.K || !x.K) throw Refused();
+    bool f32 = truth(a[4]);
+    Outputs o(x.dev);
+    at::Tensor t;
+    int64_t ld = y.rows;
+    if (a[5] == Py_None) {
+        t = o.make(f32 ? at::kFloat : at::kBFloat16, {x.rows, y.rows});
+    } else {
+        t = tensor(a[5]);
+        if (t.device() != x.dev || t.scalar_type() != (f32 ? at::kFloat : at::kBFloat16) || t.dim() != 2 || t.size(0) != x.rows ||
+            t.size(1) != y.rows || (t.stride(1) != 1 && y.rows > 1) || (x.rows > 1 && t.stride(0) < y.rows))
+            throw Refused();
+        if (x.rows > 1) ld = t.stride(0);
+    }
+    const int rc = enter(x.dev, [&](void *s) {
+        return lib.difr_mx4_product(x.codes, x.scales, x.rows, y.codes, y.scales, y.rows, x.K, t.data_ptr(), f32 ? DIFR_F32 : DIFR_BF16,
+                                    ld, s);
+    });
+    return wrapped(rc, t);
+}
+
 // ---- module ----
 
 template <PyObject *(*F)(PyObject *const *), int N>
@@ -570,6 +827,13 @@ PyMethodDef methods[] = {
     method<lmhead_score, 15>("lmhead_score"),
     method<seq_reduce, 4>("seq_reduce"),
     method<classify, 6>("classify"),
+    method<token_logprob, kTokenRowArgs + 1>("token_logprob"),
+    method<token_logprob_backward, kTokenRowArgs + 5>("token_logprob_backward"),
+    method<policy_loss, kTokenRowArgs + 11>("policy_loss"),
+    method<preference_loss, kTokenRowArgs + 10>("preference_loss"),
+    method<mx4_quantize, 1>("mx4_quantize"),
+    method<mx4_dequantize, 4>("mx4_dequantize"),
+    method<mx4_product, 6>("mx4_product"),
     {nullptr, nullptr, 0, nullptr},
 };
 

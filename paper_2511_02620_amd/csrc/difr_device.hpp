@@ -21,6 +21,7 @@ constexpr uint32_t kFlagMatch = 1u;
 constexpr uint32_t kFlagInvalidClaim = 2u;
 constexpr uint32_t kFlagNonfinite = 4u;
 constexpr uint32_t kFlagSlowPath = 8u;
+constexpr uint32_t kFlagClipped = 16u;
 
 constexpr float kLn2 = 0.693147180559945309417f;
 constexpr float kLog2e = 1.44269504088896340736f;

@@ -1,0 +1,202 @@
+// Softmax statistics of one row of logits by one workgroup, and the gradient of a row, for the kernels of the log-probabilities and
+// the losses (token_loss.hip).
+//
+//   t_j = (x_j - ref) c,  c = log2(e) / T;   e_j = 2^t_j;   S = sum e_j;   A = sum e_j t_j
+//   ln p_j = ln 2 t_j - ln S;   H = -sum p_j ln p_j = ln S - ln 2 A / S
+//
+// The reference is a logit of the row and no exact maximum: the largest of the row's first entries, raised only where a later one
+// exceeds it by 60 binary orders, which fp32 has room for.  So a wave keeps one scalar instead of a running maximum per thread, and
+// the sums of the waves are on the same reference (which costs no rounding) unless one of them had to raise it.
+// t is formed as a difference first: a masked logit of -inf or of the type's lowest value has e = 0, and a row that holds nothing but
+// the lowest value is uniform.
+#pragma once
+
+#include "difr_device.hpp"
+
+namespace difr {
+
+// Entries of a vector that are not there, and t of entries without mass where e t is formed (0 times -inf is no number).
+constexpr float kNoLogit = -__builtin_inff();
+constexpr float kLeastExponent = -200.0f;
+constexpr float kRaise = 60.0f;
+
+template <int DT>
+__device__ __forceinline__ u32x4 no_logits()
+{
+    return DT == 0 ? u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u} : u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u};
+}
+
+// Vector `i` (E entries) of a row of V; past its end, no logits.
+template <int DT>
+__device__ __forceinline__ u32x4 row_vector(const typename Elem<DT>::type *row, int64_t i, int64_t V)
+{
+    const int64_t base = i * Elem<DT>::kPerVec;
+    return base < V ? load_vector<DT>(row, base, V) : no_logits<DT>();
+}
+
+template <int DT>
+__device__ __forceinline__ float vector_max(const float x[Elem<DT>::kPerVec])
+{
+    float m = fmaxf(x[0], x[1]);
+#pragma unroll
+    for (int j = 2; j < Elem<DT>::kPerVec; ++j) m = fmaxf(m, x[j]);
+    return m;
+}
+
+// One wave's share of a row's sums.
+template <int DT, bool ENT>
+struct SoftmaxSums {
+    float c;          // log2(e) / T
+    float ref, base;  // the reference, -inf as long as there is none; what is subtracted: the same, or 0
+    float most;       // logits beyond this raise the reference
+    float S, A;       // this lane's
+
+    __device__ __forceinline__ void begin(float first, float c_)
+    {
+        c = c_;
+        S = A = 0.0f;
+        set(first);
+    }
+    __device__ __forceinline__ void set(float r)
+    {
+        ref = r;
+        base = r == kNoLogit ? 0.0f : r;
+        most = r == kNoLogit ? r : r + kRaise / c;
+    }
+    __device__ __forceinline__ void add(const float x[Elem<DT>::kPerVec])
+    {
+        const float m = vector_max<DT>(x);
+        if (__builtin_amdgcn_ballot_w64(m > most) != 0ull) raise(m);
+#pragma unroll
+        for (int j = 0; j < Elem<DT>::kPerVec; ++j) {
+            const float t = (x[j] - base) * c;
+            const float e = fast_exp2(t);
+            S += e;
+            if (ENT) A = __fmaf_rn(e, fmaxf(t, kLeastExponent), A);
+        }
+    }
+    __device__ __forceinline__ void raise(float m)
+    {
+        asm volatile("" ::: "memory");  // keep this a real, rarely taken branch
+        const float top = wave_max(m);
+        const float d = ref == kNoLogit ? 0.0f : fmaxf((ref - top) * c, -1000.0f);
+        const float f = fast_exp2(d);
+        A = f * (A + d * S);
+        S *= f;
+        set(top);
+    }
+};
+
+// What a row's statistics come to, in 64 bits.
+struct RowSums {
+    float ref;    // -inf: a row without a finite logit
+    double S, A;
+};
+
+// The waves' sums in a fixed order; every thread gets them.  lds: 3 floats for each wave.
+template <int THREADS, int DT, bool ENT>
+__device__ __forceinline__ RowSums merge_sums(const SoftmaxSums<DT, ENT> &w, float *lds)
+{
+    constexpr int W = THREADS / 64;
+    const float S = wave_sum(w.S), A = ENT ? wave_sum(w.A) : 0.0f;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+        lds[3 * wave] = w.ref;
+        lds[3 * wave + 1] = S;
+        lds[3 * wave + 2] = A;
+    }
+    __syncthreads();
+    float ref = lds[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) ref = fmaxf(ref, lds[3 * i]);
+    RowSums r{ref, 0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const float from = lds[3 * i];
+        double s = lds[3 * i + 1], a = lds[3 * i + 2];
+        if (from != ref) {  // uniform; a wave without a reference has seen nothing
+            const double d = from == kNoLogit ? 0.0 : fmax(((double)from - (double)ref) * (double)w.c, -1000.0);
+            const double f = exp2(d);
+            a = f * (a + d * s);
+            s *= f;
+        }
+        r.S += s;
+        r.A += a;
+    }
+    return r;
+}
+
+// ln p of a logit, and the entropy, in 64 bits
+__device__ __forceinline__ double row_log_prob(float x, float ref, double S, double T) { return ((double)x - (double)ref) / T - log(S); }
+
+// Upstream gradients a (of ln p_t) and b (of the entropy) to the gradient in the logits:
+//   g_j = (1/T) [ a (1[j = t] - p_j) - b p_j (ln p_j + H) ] = e_j (k0 + k1 t_j)  for j != t
+struct RowGrad {
+    float base, c, k0, k1;
+    double at_token;  // g_t
+    __device__ __forceinline__ void set(float ref, float c_, double S, double T, double a, double b, double H, double logp)
+    {
+        base = ref == kNoLogit ? 0.0f : ref;
+        c = c_;
+        const double z = 1.0 / (S * T);
+        k0 = (float)(z * (-a - (b != 0.0 ? b * (H - log(S)) : 0.0)));
+        k1 = (float)(z * -b * 0.69314718055994530942);
+        at_token = (-a * expm1(logp) - (b != 0.0 && logp > -700.0 ? b * exp(logp) * (logp + H) : 0.0)) / T;
+    }
+    template <bool ENT>
+    __device__ __forceinline__ float operator()(float x) const
+    {
+        const float t = (x - base) * c;
+        const float e = fast_exp2(t);
+        return ENT ? e * __fmaf_rn(fmaxf(t, kLeastExponent), k1, k0) : e * k0;
+    }
+};
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4 pack_vector(const float g[Elem<DT>::kPerVec])
+{
+    if constexpr (DT == 0)
+        return u32x4{pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7])};
+    else
+        return u32x4{__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3])};
+}
+
+template <int DT>
+__device__ __forceinline__ void store_element(typename Elem<DT>::type *p, float v)
+{
+    if constexpr (DT == 0)
+        *p = (uint16_t)pack_bf16(v, v);
+    else
+        *p = v;
+}
+
+// Vector `i` of a row of V: whole, or the entries that there are.
+template <int DT>
+__device__ __forceinline__ void store_vector(typename Elem<DT>::type *row, int64_t i, int64_t V, u32x4 q)
+{
+    constexpr int E = Elem<DT>::kPerVec;
+    const int64_t base = i * E;
+    if (base + E <= V) {
+        *reinterpret_cast<u32x4_any *>(row + base) = q;
+        return;
+    }
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (base + j < V) {
+            if constexpr (DT == 0)
+                row[base + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            else
+                row[base + j] = __uint_as_float(w[j]);
+        }
+}
+
+}  // namespace difr

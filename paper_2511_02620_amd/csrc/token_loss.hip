@@ -1,0 +1,407 @@
+// Log-probabilities of logged tokens under stored logits, their gradient, and two losses on them: the clipped policy loss with a KL
+// term and the preference loss over pairs of replies.  Formulas at the entry points in difr.h and in softmax_row.hpp.
+#include <math.h>
+
+#include "difr_host.hpp"
+#include "softmax_row.hpp"
+#include "token_loss.hpp"
+
+namespace difr {
+
+constexpr double kLn2d = 0.69314718055994530942;
+
+// Per-row scalars.
+struct TokenRow {
+    float T, c;
+    int32_t t;
+    bool temp_ok, token_ok;
+};
+__device__ __forceinline__ TokenRow load_token_row(const TokenRows &b, int64_t row)
+{
+    TokenRow r;
+    r.T = b.temperatures ? b.temperatures[row] : b.temperature;
+    r.temp_ok = r.T > 0.0f && r.T < __builtin_inff();
+    r.t = b.tokens[row];
+    r.token_ok = r.t >= 0 && (int64_t)r.t < b.V;
+    r.c = r.temp_ok ? kLog2e / r.T : __builtin_nanf("");
+    return r;
+}
+
+// A row's log-probability, entropy and flags from its sums.
+struct RowResult {
+    double logp, H;
+    uint32_t flags;
+};
+__device__ __forceinline__ RowResult row_result(const TokenRow &r, const RowSums &s, float x_t)
+{
+    const double nan = __builtin_nan("");
+    RowResult o;
+    const bool ok = r.temp_ok && s.S > 0.0 && s.S < (double)__builtin_inff();
+    o.flags = (ok ? 0u : kFlagNonfinite) | (r.token_ok ? 0u : kFlagInvalidClaim);
+    o.logp = ok && r.token_ok ? row_log_prob(x_t, s.ref, s.S, (double)r.T) : nan;
+    o.H = ok ? log(s.S) - kLn2d * s.A / s.S : nan;
+    return o;
+}
+
+// The row in vectors of 16 bytes, U of a thread's in flight; f(values, index of the vector) is called by whole waves.
+template <int DT, int THREADS, int U, class F>
+__device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, int64_t V, F &&f)
+{
+    constexpr int E = Elem<DT>::kPerVec;
+    const int tid = threadIdx.x;
+    const int64_t nvec = V / E, total = (V + E - 1) / E;
+    int64_t i = 0;
+    for (; i + (int64_t)U * THREADS <= nvec; i += (int64_t)U * THREADS) {
+        u32x4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u] = *reinterpret_cast<const u32x4_any *>(row + (i + u * THREADS + tid) * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[E];
+            unpack_vector<DT>(q[u], x);
+            f(x, i + u * THREADS + tid);
+        }
+    }
+    for (; i < total; i += THREADS) {
+        float x[E];
+        unpack_vector<DT>(row_vector<DT>(row, i + tid, V), x);
+        f(x, i + tid);
+    }
+}
+
+// The row's sums, by all threads of the workgroup.
+template <int DT, int THREADS, bool ENT>
+__device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, float c, float *lds)
+{
+    constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64;
+    float x[E];
+    unpack_vector<DT>(row_vector<DT>(row, threadIdx.x, V), x);
+    const float m = wave_max(vector_max<DT>(x));
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+    __syncthreads();
+    float first = lds[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) first = fmaxf(first, lds[i]);
+    __syncthreads();
+    SoftmaxSums<DT, ENT> s;
+    s.begin(first, c);
+    stream_row<DT, THREADS, 4>(row, V, [&](const float *v, int64_t) { s.add(v); });
+    return merge_sums<THREADS>(s, lds);
+}
+
+template <int DT, int THREADS, bool ENT>
+__global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, const uint8_t *mask, LogProbOutputs o)
+{
+    __shared__ float lds[3 * THREADS / 64];
+    const int64_t row = blockIdx.x;
+    typedef typename Elem<DT>::type elem;
+    const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
+    if (mask && mask[row] == 0) {
+        if (threadIdx.x == 0) {
+            o.logp[row] = 0.0f;
+            if (o.stats) o.stats[2 * row] = o.stats[2 * row + 1] = 0.0f;
+            if (o.entropy) o.entropy[row] = 0.0f;
+            o.flags[row] = 0;
+        }
+        return;
+    }
+    const TokenRow r = load_token_row(b, row);
+    const float x_t = r.token_ok ? Elem<DT>::to_float(x[r.t]) : 0.0f;
+    const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, lds);
+    if (threadIdx.x == 0) {
+        const RowResult q = row_result(r, s, x_t);
+        o.logp[row] = (float)q.logp;
+        if (o.stats) {
+            o.stats[2 * row] = s.ref;
+            o.stats[2 * row + 1] = (float)s.S;
+        }
+        if (o.entropy) o.entropy[row] = (float)q.H;
+        o.flags[row] = (uint8_t)q.flags;
+    }
+}
+
+// The gradient of a row from its statistics: every workgroup has a stretch of it.
+constexpr int kGradVectors = 8;  // of each thread
+
+template <int DT, bool ENT>
+__global__ __launch_bounds__(kBlock) void token_grad_kernel(TokenRows b, const float *stats, const float *entropy, const float *grad_logp,
+                                                            const float *grad_entropy, void *grad, int64_t ld_grad)
+{
+    constexpr int E = Elem<DT>::kPerVec;
+    typedef typename Elem<DT>::type elem;
+    const int64_t row = blockIdx.y;
+    const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
+    elem *g = reinterpret_cast<elem *>(grad) + row * ld_grad;
+    const int64_t first = (int64_t)blockIdx.x * (kBlock * kGradVectors), total = (b.V + E - 1) / E;
+    const int64_t last = first + kBlock * kGradVectors < total ? first + kBlock * kGradVectors : total;
+    double a = grad_logp[row];
+    const double bb = ENT ? (double)grad_entropy[row] : 0.0;
+    if (a == 0.0 && bb == 0.0) {
+        for (int64_t i = first + threadIdx.x; i < last; i += kBlock) store_vector<DT>(g, i, b.V, u32x4{0u, 0u, 0u, 0u});
+        return;
+    }
+    const TokenRow r = load_token_row(b, row);
+    if (!r.token_ok && a != 0.0) a = __builtin_nan("");
+    const float ref = stats[2 * row];
+    const double S = stats[2 * row + 1], T = r.T;
+    const bool here = r.token_ok && r.t >= first * E && r.t < last * E;
+    const double logp = here ? row_log_prob(Elem<DT>::to_float(x[r.t]), ref, S, T) : 0.0;
+    RowGrad k;
+    k.set(ref, r.c, S, T, a, bb, ENT ? (double)entropy[row] : 0.0, logp);
+    __syncthreads();  // in place: the token's logit is read before its place is written
+    for (int64_t i = first + threadIdx.x; i < last; i += kBlock) {
+        float v[E];
+        unpack_vector<DT>(row_vector<DT>(x, i, b.V), v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = k.operator()<ENT>(v[j]);
+        if (here && i == r.t / E) {
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (r.t % E == j) v[j] = (float)k.at_token;
+        }
+        store_vector<DT>(g, i, b.V, pack_vector<DT>(v));
+    }
+}
+
+// A row's part of the clipped policy loss, and what flows back into its log-probability and entropy (without the row's weight).
+struct PolicyRow {
+    double loss, kl, a;
+    uint32_t flags;
+};
+__device__ __forceinline__ PolicyRow policy_row(const PolicyParams &p, int64_t row, double logp, double H)
+{
+    PolicyRow o;
+    const double A = p.advantages[row];
+    const double ratio = p.old_logp ? exp(logp - (double)p.old_logp[row]) : (logp == logp ? 1.0 : logp);
+    const double lo = 1.0 - p.clip_low, hi = 1.0 + p.clip_high;
+    const double inside = ratio < lo ? lo : (ratio > hi ? hi : ratio);
+    const bool clipped = ratio * A > inside * A;
+    o.flags = clipped ? kFlagClipped : 0u;
+    o.loss = clipped ? -(inside * A) : -(ratio * A);
+    o.a = clipped ? 0.0 : -(ratio * A);
+    o.kl = 0.0;
+    if (p.ref_logp) {
+        const double d = (double)p.ref_logp[row] - logp, m = expm1(d);
+        o.kl = m - d;
+        if (p.kl_coef != 0.0) {
+            o.loss += p.kl_coef * o.kl;
+            o.a -= p.kl_coef * m;
+        }
+    }
+    if (p.entropy_coef != 0.0) o.loss -= p.entropy_coef * H;
+    return o;
+}
+
+// One workgroup a row, which it reads twice: the row's sums, then the gradient.
+template <int DT, int THREADS, bool ENT>
+__global__ __launch_bounds__(THREADS) void policy_kernel(TokenRows b, PolicyParams p, PolicyOutputs o)
+{
+    constexpr int E = Elem<DT>::kPerVec;
+    __shared__ float lds[3 * THREADS / 64];
+    __shared__ RowGrad lds_grad;
+    const int64_t row = blockIdx.x;
+    typedef typename Elem<DT>::type elem;
+    const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
+    elem *g = reinterpret_cast<elem *>(o.grad) + row * o.ld_grad;
+    const double w = p.weights ? (double)p.weights[row] : 1.0 / (double)b.N;
+    if (w == 0.0) {  // left out
+        if (threadIdx.x == 0) {
+            o.row.logp[row] = o.token_loss[row] = 0.0f;
+            if (o.row.entropy) o.row.entropy[row] = 0.0f;
+            if (o.kl) o.kl[row] = 0.0f;
+            o.row.flags[row] = 0;
+        }
+        if (o.grad) {
+            const int64_t total = (b.V + E - 1) / E;
+            for (int64_t i = threadIdx.x; i < total; i += THREADS) store_vector<DT>(g, i, b.V, u32x4{0u, 0u, 0u, 0u});
+        }
+        return;
+    }
+    const TokenRow r = load_token_row(b, row);
+    const float x_t = r.token_ok ? Elem<DT>::to_float(x[r.t]) : 0.0f;
+    const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, lds);
+    if (threadIdx.x == 0) {
+        const RowResult q = row_result(r, s, x_t);
+        const PolicyRow l = policy_row(p, row, q.logp, q.H);
+        o.row.logp[row] = (float)q.logp;
+        o.token_loss[row] = (float)l.loss;
+        if (o.row.entropy) o.row.entropy[row] = (float)q.H;
+        if (o.kl) o.kl[row] = (float)l.kl;
+        o.row.flags[row] = (uint8_t)(q.flags | l.flags);
+        lds_grad.set(s.ref, r.c, s.S, (double)r.T, w * l.a, -p.entropy_coef * w, q.H, q.logp);
+    }
+    if (!o.grad) return;
+    __syncthreads();
+    const RowGrad k = lds_grad;
+    stream_row<DT, THREADS, 4>(x, b.V, [&](const float *v, int64_t i) {
+        float d[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) d[j] = k.operator()<ENT>(v[j]);
+        if (r.token_ok && i == r.t / E) {
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (r.t % E == j) d[j] = (float)k.at_token;
+        }
+        if (i * E < b.V) store_vector<DT>(g, i, b.V, pack_vector<DT>(d));
+    });
+}
+
+// sum_n weight[n] value[n] by one workgroup, in 64 bits and a fixed order.  A weight of 0 leaves its value out.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void weighted_sum_kernel(const float *value, const float *weight, double every, int64_t n, float *out)
+{
+    __shared__ double lds[kSumThreads / 64];
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += kSumThreads) {
+        const double w = weight ? (double)weight[i] : every;
+        if (w != 0.0) sum += w * (double)value[i];
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double s = lds[0];
+        for (int i = 1; i < kSumThreads / 64; ++i) s += lds[i];
+        *out = (float)s;
+    }
+}
+
+// ---- pairs ----
+
+// The pair of sequences 2 p (chosen) and 2 p + 1 (rejected): log-probabilities summed in 64 bits and a fixed order, the loss, and
+// what flows back into each log-probability.
+__global__ __launch_bounds__(kBlock) void pair_kernel(int64_t N, PreferenceParams p, PreferenceOutputs o)
+{
+    __shared__ double lds_sum[2][kWaves], lds_back[2];
+    __shared__ int lds_count[2][kWaves];
+    const int64_t pair = blockIdx.x;
+    const int tid = threadIdx.x;
+    int64_t lo[2], hi[2];
+    for (int side = 0; side < 2; ++side) {
+        lo[side] = max(p.seq_offsets[2 * pair + side], (int64_t)0);
+        hi[side] = min(p.seq_offsets[2 * pair + side + 1], N);
+        double sum = 0.0;
+        int count = 0;
+        for (int64_t n = lo[side] + tid; n < hi[side]; n += kBlock)
+            if (!p.mask || p.mask[n]) {
+                sum += (double)o.row.logp[n];
+                ++count;
+            }
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) {
+            sum += __shfl_xor(sum, off, 64);
+            count += __shfl_xor(count, off, 64);
+        }
+        if ((tid & 63) == 0) {
+            lds_sum[side][tid >> 6] = sum;
+            lds_count[side][tid >> 6] = count;
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        double ratio[2], share[2];
+        for (int side = 0; side < 2; ++side) {
+            const double *l = lds_sum[side];
+            const int *k = lds_count[side];
+            const int count = k[0] + k[1] + k[2] + k[3];
+            share[side] = p.average && count ? 1.0 / count : 1.0;
+            const double total = ((l[0] + l[1]) + (l[2] + l[3])) * share[side];
+            o.seq_logp[2 * pair + side] = (float)total;
+            ratio[side] = total - (p.ref_seq_logp ? (double)p.ref_seq_logp[2 * pair + side] : 0.0);
+        }
+        const double h = p.beta * (ratio[0] - ratio[1]) - p.margin, eps = p.label_smoothing;
+        const double soft = log1p(exp(-fabs(h)));  // -ln sigma(h) = soft + max(-h, 0)
+        const double up = h >= 0.0 ? 1.0 / (1.0 + exp(-h)) : exp(h) / (1.0 + exp(h));
+        const double down = h >= 0.0 ? exp(-h) / (1.0 + exp(-h)) : 1.0 / (1.0 + exp(h));
+        o.pair_loss[pair] = (float)((1.0 - eps) * (soft + (h < 0.0 ? -h : 0.0)) + eps * (soft + (h > 0.0 ? h : 0.0)));
+        const double w = p.pair_weights ? (double)p.pair_weights[pair] : 2.0 / (double)p.S;
+        const double back = w == 0.0 ? 0.0 : w * p.beta * (eps * up - (1.0 - eps) * down);
+        lds_back[0] = back * share[0];
+        lds_back[1] = -back * share[1];
+    }
+    if (!o.grad_logp) return;
+    __syncthreads();
+    for (int side = 0; side < 2; ++side) {
+        const float back = (float)lds_back[side];
+        for (int64_t n = lo[side] + tid; n < hi[side]; n += kBlock) o.grad_logp[n] = !p.mask || p.mask[n] ? back : 0.0f;
+    }
+}
+
+__global__ __launch_bounds__(kBlock) void zero_outside_kernel(int64_t N, const int64_t *seq_offsets, int64_t S, float *grad_logp)
+{
+    const int64_t n = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (n < N && (S == 0 || n < seq_offsets[0] || n >= seq_offsets[S])) grad_logp[n] = 0.0f;
+}
+
+// ---- launches ----
+
+static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
+
+template <int DT, bool ENT>
+static void run_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, hipStream_t stream)
+{
+    token_logprob_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, mask, o);
+}
+
+int launch_token_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, hipStream_t stream)
+{
+    if (b.dtype == 0)
+        o.entropy ? run_logprob<0, true>(b, mask, o, stream) : run_logprob<0, false>(b, mask, o, stream);
+    else
+        o.entropy ? run_logprob<1, true>(b, mask, o, stream) : run_logprob<1, false>(b, mask, o, stream);
+    return launched();
+}
+
+int launch_token_logprob_backward(const TokenRows &b, const float *stats, const float *entropy, const float *grad_logp,
+                                  const float *grad_entropy, void *grad, int64_t ld_grad, hipStream_t stream)
+{
+    const int64_t E = b.dtype == 0 ? 8 : 4, vectors = (b.V + E - 1) / E, per = kBlock * kGradVectors;
+    constexpr int64_t kMostRows = 65535;  // of a launch: the grid's second dimension
+    for (int64_t n = 0; n < b.N; n += kMostRows) {
+        TokenRows part = b;
+        part.N = b.N - n < kMostRows ? b.N - n : kMostRows;
+        part.logits = (const char *)b.logits + n * b.ld * (b.dtype == 0 ? 2 : 4);
+        part.tokens = b.tokens + n;
+        if (b.temperatures) part.temperatures = b.temperatures + n;
+        void *g = (char *)grad + n * ld_grad * (b.dtype == 0 ? 2 : 4);
+        const dim3 grid((unsigned)((vectors + per - 1) / per), (unsigned)part.N);
+        const float *ent = entropy ? entropy + n : nullptr, *ge = grad_entropy ? grad_entropy + n : nullptr;
+#define RUN(DT, ENT) token_grad_kernel<DT, ENT><<<grid, dim3(kBlock), 0, stream>>>(part, stats + 2 * n, ent, grad_logp + n, ge, g, ld_grad)
+        if (b.dtype == 0)
+            ge ? RUN(0, true) : RUN(0, false);
+        else
+            ge ? RUN(1, true) : RUN(1, false);
+#undef RUN
+    }
+    return launched();
+}
+
+int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, hipStream_t stream)
+{
+    if (b.N > 0) {
+        const bool ent = o.row.entropy || p.entropy_coef != 0.0;
+#define RUN(DT, ENT) policy_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, p, o)
+        if (b.dtype == 0)
+            ent ? RUN(0, true) : RUN(0, false);
+        else
+            ent ? RUN(1, true) : RUN(1, false);
+#undef RUN
+    }
+    weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(o.token_loss, p.weights, b.N ? 1.0 / (double)b.N : 0.0, b.N, o.loss);
+    return launched();
+}
+
+int launch_preference_loss(const TokenRows &b, const PreferenceParams &p, const PreferenceOutputs &o, hipStream_t stream)
+{
+    const int64_t pairs = p.S / 2;
+    if (b.N > 0 && launch_token_logprob(b, p.mask, o.row, stream)) return 1;
+    if (o.grad && b.N > 0)
+        zero_outside_kernel<<<dim3((unsigned)((b.N + kBlock - 1) / kBlock)), dim3(kBlock), 0, stream>>>(b.N, p.seq_offsets, p.S, o.grad_logp);
+    if (pairs > 0) pair_kernel<<<dim3((unsigned)pairs), dim3(kBlock), 0, stream>>>(b.N, p, o);
+    weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(o.pair_loss, p.pair_weights, pairs ? 1.0 / (double)pairs : 0.0, pairs, o.loss);
+    if (o.grad && b.N > 0) return launch_token_logprob_backward(b, o.row.stats, nullptr, o.grad_logp, nullptr, o.grad, o.ld_grad, stream);
+    return launched();
+}
+
+}  // namespace difr
