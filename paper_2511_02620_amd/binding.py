@@ -103,7 +103,7 @@ class _Preference(C.Structure):
 
 EXPORTS = ("difr_gumbel_score", "difr_debug_gumbel_score_unfiltered", "difr_ipt_score", "difr_score_both", "difr_score_both_peaked", "difr_score_both_admissible", "difr_admissible_count", "difr_gumbel_likelihood", "difr_ipt_score_filtered", "difr_score_both_filtered", "difr_lmhead_score", "difr_lmhead_score_static", "difr_lmhead_workspace_bytes", "difr_split_workspace_bytes", "difr_score_split", "difr_classify", "difr_seq_reduce",
            "difr_token_logprob", "difr_token_logprob_backward", "difr_policy_loss", "difr_preference_loss", "difr_mx4_padded",
-           "difr_mx4_quantize", "difr_mx4_dequantize", "difr_mx4_product", "difr_debug_noise", "difr_debug_gumbel_map",
+           "difr_mx4_quantize", "difr_mx4_dequantize", "difr_mx4_product_workspace_bytes", "difr_mx4_product", "difr_debug_noise", "difr_debug_gumbel_map",
            "difr_philox4x32_10", "difr_status_string", "difr_version")
 
 
@@ -165,7 +165,9 @@ def load_library():
     lib.difr_mx4_padded.restype = C.c_int64
     lib.difr_mx4_quantize.argtypes = [vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, vp, vp, vp]
     lib.difr_mx4_dequantize.argtypes = [vp, vp, C.c_int64, C.c_int64, vp, C.c_int32, C.c_int64, vp]
-    lib.difr_mx4_product.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_int64, C.c_int64, vp, C.c_int32, C.c_int64, vp]
+    lib.difr_mx4_product_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int64]
+    lib.difr_mx4_product_workspace_bytes.restype = C.c_size_t
+    lib.difr_mx4_product.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_int64, C.c_int64, vp, C.c_int32, C.c_int64, vp, C.c_size_t, vp]
     for name in ("token_logprob", "token_logprob_backward", "policy_loss", "preference_loss", "mx4_quantize", "mx4_dequantize",
                  "mx4_product"):
         getattr(lib, "difr_" + name).restype = C.c_int

@@ -574,20 +574,32 @@ int difr_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N, 
     return difr::launch_mx4_dequantize(codes, scales, N, d, x, dtype, ld, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
 }
 
-int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
-                     int64_t V, int64_t K, void *out, int32_t dtype, int64_t ld, void *hip_stream)
+static bool mx4_product_shape(int64_t N, int64_t V, int64_t K)
 {
-    if (N < 0 || V < 0 || ld < V || N >= (int64_t)1 << 31 || V >= (int64_t)1 << 31) return DIFR_ERR_SHAPE;
-    if (K < difr::kMxSlab || K % difr::kMxSlab || K >= (int64_t)1 << 24) return DIFR_ERR_SHAPE;
+    return N >= 0 && V >= 0 && N < (int64_t)1 << 31 && V < (int64_t)1 << 31 && K >= difr::kMxSlab && K % difr::kMxSlab == 0 && K < (int64_t)1 << 24;
+}
+
+size_t difr_mx4_product_workspace_bytes(int64_t N, int64_t V, int64_t K)
+{
+    return !mx4_product_shape(N, V, K) || N == 0 || V == 0 ? 0 : difr::mx4_product_workspace_bytes(N, V, K);
+}
+
+int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
+                     int64_t V, int64_t K, void *out, int32_t dtype, int64_t ld, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!mx4_product_shape(N, V, K) || ld < V) return DIFR_ERR_SHAPE;
     if (dtype != DIFR_BF16 && dtype != DIFR_F32) return DIFR_ERR_DTYPE;
     if (N == 0 || V == 0) return DIFR_OK;
     if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return DIFR_ERR_NULL;
-    if (((uintptr_t)a_codes | (uintptr_t)b_codes) % 16u || ((uintptr_t)a_scales | (uintptr_t)b_scales) % 4u ||
+    if (((uintptr_t)a_codes | (uintptr_t)b_codes | (uintptr_t)workspace) % 16u || ((uintptr_t)a_scales | (uintptr_t)b_scales) % 4u ||
         (uintptr_t)out % (dtype == DIFR_BF16 ? 2u : 4u))
         return DIFR_ERR_ALIGN;
+    const size_t need = difr::mx4_product_workspace_bytes(N, V, K);
+    if (workspace_bytes < need) return DIFR_ERR_SHAPE;
+    if (need && !workspace) return DIFR_ERR_NULL;
     int rc = check_device();
     if (rc != DIFR_OK) return rc;
-    return difr::launch_mx4_product(a_codes, a_scales, N, b_codes, b_scales, V, K, out, dtype, ld, (hipStream_t)hip_stream)
+    return difr::launch_mx4_product(a_codes, a_scales, N, b_codes, b_scales, V, K, out, dtype, ld, workspace, (hipStream_t)hip_stream)
                ? DIFR_ERR_LAUNCH
                : DIFR_OK;
 }

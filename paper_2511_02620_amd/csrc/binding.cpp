@@ -49,6 +49,7 @@ namespace {
     X(difr_mx4_padded)                                                                                                  \
     X(difr_mx4_quantize)                                                                                                \
     X(difr_mx4_dequantize)                                                                                              \
+    X(difr_mx4_product_workspace_bytes)                                                                                 \
     X(difr_mx4_product)
 
 struct Entries {
@@ -765,9 +766,13 @@ PyObject *mx4_product(PyObject *const *a)
             throw Refused();
         if (x.rows > 1) ld = t.stride(0);
     }
+    const size_t need = lib.difr_mx4_product_workspace_bytes(x.rows, y.rows, x.K);
+    at::Tensor ws;
+    if (need) ws = o.make(at::kByte, {(int64_t)need});
+    void *wsp = need ? ws.data_ptr() : nullptr;
     const int rc = enter(x.dev, [&](void *s) {
         return lib.difr_mx4_product(x.codes, x.scales, x.rows, y.codes, y.scales, y.rows, x.K, t.data_ptr(), f32 ? DIFR_F32 : DIFR_BF16,
-                                    ld, s);
+                                    ld, wsp, need, s);
     });
     return wrapped(rc, t);
 }

@@ -10,6 +10,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+#include <utility>
+
 namespace difr {
 
 constexpr int kBlock = 256;          // threads per workgroup: 4 wavefronts of 64
@@ -25,6 +28,19 @@ constexpr uint32_t kFlagClipped = 16u;
 
 constexpr float kLn2 = 0.693147180559945309417f;
 constexpr float kLog2e = 1.44269504088896340736f;
+
+// f(integral_constant<int, 0>()), ..., f(integral_constant<int, N - 1>()): a loop whose index is a compile-time
+// constant in the body (register numbers and instruction immediates depend on it)
+template <int... Is, class F>
+__device__ __forceinline__ void static_for_impl(std::integer_sequence<int, Is...>, F &&f)
+{
+    (f(std::integral_constant<int, Is>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F &&f)
+{
+    static_for_impl(std::make_integer_sequence<int, N>(), f);
+}
 
 // Kernel-side image of difr_rows.
 struct RowBatch {

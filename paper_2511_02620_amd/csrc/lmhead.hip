@@ -36,19 +36,6 @@ __host__ __device__ constexpr int copy_at_slot(int n)
     return -1;
 }
 
-// f(integral_constant<int, 0>()), ..., f(integral_constant<int, N - 1>()): a loop whose index is a compile-time
-// constant in the body (register numbers and instruction immediates depend on it)
-template <int... Is, class F>
-__device__ __forceinline__ void static_for_impl(std::integer_sequence<int, Is...>, F &&f)
-{
-    (f(std::integral_constant<int, Is>()), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void static_for(F &&f)
-{
-    static_for_impl(std::make_integer_sequence<int, N>(), f);
-}
-
 struct TokInfo {
     PhiloxKey key;
     uint32_t pos, seq;

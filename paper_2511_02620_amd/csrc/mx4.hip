@@ -1,4 +1,5 @@
-// Microscaled 4-bit floating point (E2M1 elements, one power-of-two scale for each 32 of a row): quantisation, values, product.
+// Microscaled 4-bit floating point (E2M1 elements, one power-of-two scale for each 32 of a row): quantisation and values
+// (the product: mx4_product.hip).
 // Format and formulas at the entry points in difr.h.
 #include "difr_host.hpp"
 #include "softmax_row.hpp"
@@ -6,8 +7,6 @@
 
 namespace difr {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // The code of x 2^-e: round to nearest, ties to even, everything from 5 on is 6.
 __device__ __forceinline__ uint32_t e2m1_code(float v)
@@ -85,32 +84,6 @@ __global__ __launch_bounds__(kBlock) void mx4_dequantize_kernel(const uint8_t *c
     for (int j = 0; j < 8; j += E) store_vector<DT>(x + row * ld, (k + j) / E, d, pack_vector<DT>(v + j));
 }
 
-// out[n][v] = sum_k a[n][k] b[v][k].  A wave has 16 rows of b and 16 of a.
-template <int DT>
-__global__ __launch_bounds__(kBlock) void mx4_product_kernel(const uint8_t *a, const uint8_t *as, int64_t N, const uint8_t *b, const uint8_t *bs,
-                                                             int64_t V, int64_t K, typename Elem<DT>::type *out, int64_t ld)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t n = (int64_t)blockIdx.y * 16 + (lane & 15), v0 = ((int64_t)blockIdx.x * kWaves + wave) * 16;
-    const int64_t v = v0 + (lane & 15);
-    const int64_t nr = n < N ? n : N - 1, vr = v < V ? v : V - 1;
-    const int g = lane >> 4;
-    const uint8_t *pa = a + nr * (K / 2) + g * 16, *pb = b + vr * (K / 2) + g * 16;
-    const uint8_t *qa = as + nr * (K / 32) + g, *qb = bs + vr * (K / 32) + g;
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t k = 0; k < K; k += kMxSlab) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(pa + k / 2), y = *reinterpret_cast<const u32x4 *>(pb + k / 2);
-        const i32x8 fx = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0}, fy = {(int)y.x, (int)y.y, (int)y.z, (int)y.w, 0, 0, 0, 0};
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fy, fx, acc, 4, 4, 0, (int)qb[k / 32], 0, (int)qa[k / 32]);
-    }
-    if (n >= N) return;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t c = v0 + 4 * g + i;
-        if (c < V) store_element<DT>(out + n * ld + c, acc[i]);
-    }
-}
-
 static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 
 int launch_mx4_quantize(const void *x, int dtype, int64_t N, int64_t d, int64_t ld, uint8_t *codes, uint8_t *scales, hipStream_t stream)
@@ -133,17 +106,6 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N
         mx4_dequantize_kernel<0><<<grid, dim3(kBlock), 0, stream>>>(codes, scales, N, d, blocks, (uint16_t *)x, ld);
     else
         mx4_dequantize_kernel<1><<<grid, dim3(kBlock), 0, stream>>>(codes, scales, N, d, blocks, (float *)x, ld);
-    return launched();
-}
-
-int launch_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
-                       int64_t V, int64_t K, void *out, int dtype, int64_t ld, hipStream_t stream)
-{
-    const dim3 grid((unsigned)((V + 16 * kWaves - 1) / (16 * kWaves)), (unsigned)((N + 15) / 16));
-    if (dtype == 0)
-        mx4_product_kernel<0><<<grid, dim3(kBlock), 0, stream>>>(a_codes, a_scales, N, b_codes, b_scales, V, K, (uint16_t *)out, ld);
-    else
-        mx4_product_kernel<1><<<grid, dim3(kBlock), 0, stream>>>(a_codes, a_scales, N, b_codes, b_scales, V, K, (float *)out, ld);
     return launched();
 }
 

@@ -1,0 +1,376 @@
+// The product of two matrices in microscaled 4-bit floating point, out[n][v] = sum_k a[n][k] b[v][k]: hidden states by an LM head.
+// Elements stay as they are stored until the matrix cores take them, 32 with their scale at a time; accumulation is in fp32.
+#include "difr_host.hpp"
+#include "softmax_row.hpp"
+#include "token_loss.hpp"
+
+namespace difr {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct Mx4Product {
+    const uint8_t *a, *as;  // [N][K / 2] codes and [N][K / 32] scales of the hidden states
+    const uint8_t *b, *bs;  // [V] of the head
+    int64_t N, V, K;
+    void *out;
+    int64_t ld;
+    const uint8_t *ta, *tb;  // the scales by tiles and slabs (mx4_tile_scales_kernel)
+};
+
+constexpr int kMxTile = 256;       // rows of either matrix that a workgroup multiplies
+constexpr int kMxSlabBytes = 128;  // of a row, staged through LDS per step: 256 elements
+
+// How the product is cut: token blocks of kMxTile rows of a, times `splits` contiguous ranges of tiles of kMxTile rows of b.
+struct Mx4Plan {
+    int n_tb, n_vt, splits;
+};
+
+// Eight 4-byte codes of a fragment and nothing above them: the instruction reads the lower half only for this type.
+__device__ __forceinline__ i32x8 fp4_operand(i32x4 v) { return __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1); }
+
+// acc += a b for fragments of 32 x 64 elements; byte STEP of the two scale registers is the scale of the lane's 32.
+template <int STEP>
+__device__ __forceinline__ f32x16 fp4_mfma(i32x4 a, i32x4 b, f32x16 acc, int scale_a, int scale_b)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(a), fp4_operand(b), acc, 4, 4, STEP, scale_a, STEP, scale_b);
+}
+
+// The scales of a matrix in the order the product's tiles want them: for each tile of 256 rows and each slab of 256 elements, 8 bytes a
+// row, those of the slab's even blocks and then those of its odd ones.  A lane of the product has the even or the odd ones, and one
+// 4-byte read serves it for four steps; a tile's share of a slab is 2 KB without gaps, where the rows themselves would have to be
+// gathered 8 bytes at a time.  Rows and blocks that are not there get 0.  One workgroup a tile and four slabs.
+constexpr int kScaleSlabs = 4;
+__global__ __launch_bounds__(kBlock) void mx4_tile_scales_kernel(const uint8_t *a, int64_t N, const uint8_t *b, int64_t V, int64_t K, int n_tb,
+                                                                 uint8_t *out)
+{
+    const int tile = blockIdx.x, nk = (int)((K + 255) / 256), blocks = (int)(K / 32);
+    const uint8_t *m = tile < n_tb ? a : b;
+    const int64_t row = (int64_t)(tile < n_tb ? tile : tile - n_tb) * kMxTile + threadIdx.x, rows = tile < n_tb ? N : V;
+    const int first = blockIdx.y * kScaleSlabs;
+#pragma unroll
+    for (int i = 0; i < kScaleSlabs; ++i) {
+        const int k = first + i;
+        if (k >= nk) return;
+        uint32_t lo = 0, hi = 0;
+        if (row < rows) {
+            const uint8_t *p = m + row * blocks + 8 * k;
+            lo = *reinterpret_cast<const uint32_t *>(p);
+            if (8 * k + 4 < blocks) hi = *reinterpret_cast<const uint32_t *>(p + 4);
+        }
+        const uint2 w = {__builtin_amdgcn_perm(hi, lo, 0x06040200u), __builtin_amdgcn_perm(hi, lo, 0x07050301u)};
+        *reinterpret_cast<uint2 *>(out + (((int64_t)tile * nk + k) * kMxTile + threadIdx.x) * 8) = w;
+    }
+}
+
+// Stores one 32 x 32 block of accumulators: this lane's are row p of the output, columns v(r) = v + 8 (r / 4) + (r % 4) (v holds the lane's
+// half).  Lanes l and l + 32 have the same row and four columns each in turn; they trade, so that each stores eight in a row.
+template <int DT, bool AGPR>
+__device__ __forceinline__ void store_block(const f32x16 acc, typename Elem<DT>::type *p, int32_t v, int lh, int32_t V, bool whole, bool live)
+{
+    float x[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        if constexpr (AGPR)
+            asm("v_accvgpr_read_b32 %0, %1" : "=v"(x[r]) : "a"(acc[r]));
+        else
+            x[r] = acc[r];
+    }
+    if constexpr (DT == 0) {
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+            u32x4 q;
+            const auto s0 = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * g], x[4 * g + 1]), pack_bf16(x[4 * g + 4], x[4 * g + 5]), false, false);
+            const auto s1 = __builtin_amdgcn_permlane32_swap(pack_bf16(x[4 * g + 2], x[4 * g + 3]), pack_bf16(x[4 * g + 6], x[4 * g + 7]), false, false);
+            q = u32x4{s0[0], s1[0], s0[1], s1[1]};
+            const int32_t c = v + 8 * g + 8 * lh;
+            if (live) {
+                if (whole || c + 8 <= V) {
+                    *reinterpret_cast<u32x4_any *>(p + c) = q;
+                } else {
+                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < V) p[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int32_t c = v + 8 * g + 4 * lh;
+            if (live) {
+                if (whole || c + 4 <= V) {
+                    *reinterpret_cast<u32x4_any *>(p + c) = u32x4{__float_as_uint(x[4 * g]), __float_as_uint(x[4 * g + 1]),
+                                                                  __float_as_uint(x[4 * g + 2]), __float_as_uint(x[4 * g + 3])};
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (c + j < V) p[c + j] = x[4 * g + j];
+                }
+            }
+        }
+    }
+}
+
+// When the 16 copies of a slab go out, as in the fused LM head: copy c after matrix instruction kCopySlot[c] of the 48 of the fourth k
+// step of one slab and the first two of the next.
+__host__ __device__ constexpr int copy_at_slot(int n)
+{
+    constexpr int kCopySlot[16] = {0, 3, 5, 8, 10, 13, 15, 18, 20, 23, 25, 28, 30, 33, 35, 38};
+    for (int c = 0; c < 16; ++c)
+        if (kCopySlot[c] == n) return c;
+    return -1;
+}
+
+// 256 threads = 4 waves, 2 (rows of b) x 2 (rows of a), each with a 128 x 128 sub-tile of 4 x 4 accumulator blocks.  One wave per SIMD.
+// LDS: two stages of [256 rows][128 bytes] for either operand; the eight 16-byte chunks of a row, one block of 32 elements each, are
+// permuted by (row / 2) % 8, so that the reads of 16 consecutive rows spread over the banks.  A slab is four k steps of 64 elements, a
+// lane's share of a step one chunk of one row.  The scales of a slab go through LDS too (8 bytes a row).
+//
+// Where K is an odd number of 128s the last slab of a row is half a slab: its copies fetch its four chunks twice, and its last two k steps
+// multiply zeros.
+template <int DT>
+__global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx4Plan plan)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t lds_b[2][kMxTile * kMxSlabBytes];  // 32 KB per stage
+    __shared__ __attribute__((aligned(16))) uint8_t lds_a[2][kMxTile * kMxSlabBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_s[2][2 * kMxTile * 8];          // scales: rows of a, rows of b
+    typedef typename Elem<DT>::type elem;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int wv = wave >> 1, wt = wave & 1;
+    const int l32 = lane & 31, lh = lane >> 5;
+
+    // Consecutive workgroup ids go to different XCDs; each XCD takes a compact set of token blocks across the ranges of b, so that its
+    // L2 sees a tile from several workgroups at about the same time.
+    const int G = plan.n_tb * plan.splits;
+    int q = blockIdx.x;
+    if (G % 8 == 0) q = (q % 8) * (G / 8) + q / 8;
+    const int tb = q / plan.splits, sp = q % plan.splits;
+    const int vt0 = (int)((int64_t)sp * plan.n_vt / plan.splits), vt1 = (int)((int64_t)(sp + 1) * plan.n_vt / plan.splits);
+    const int64_t n0 = (int64_t)tb * kMxTile;
+    const uint32_t pitch = (uint32_t)(m.K / 2);  // bytes of a row's codes
+    const int nk = (int)((m.K + 255) / 256);
+    const bool half = m.K % 256 != 0;
+    const int32_t V = (int32_t)m.V;
+
+    // ---- copies: global memory straight into LDS.  Lane i of a copy lands in chunk i % 8 of row i / 8 and fetches the chunk that the
+    // permutation puts there; thread -> rows (tid / 8) + 32 p.  Uniform base plus an invariant lane offset.
+    const int crow = tid >> 3;
+    const int cchunk = (tid & 7) ^ ((crow >> 1) & 7);
+    const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+    const uint32_t last_a = (uint32_t)((m.N - n0 < kMxTile ? m.N - n0 : kMxTile) - 1);
+    uint32_t aoff[8], boff[8];
+#pragma unroll
+    for (int p = 0; p < 8; ++p) aoff[p] = min((uint32_t)(crow + 32 * p), last_a) * pitch + (uint32_t)cchunk * 16u;
+    auto set_boff = [&](int vt) {
+        const int64_t left = m.V - (int64_t)vt * kMxTile;
+        const uint32_t last_b = (uint32_t)((left < kMxTile ? left : kMxTile) - 1);
+#pragma unroll
+        for (int p = 0; p < 8; ++p) boff[p] = min((uint32_t)(crow + 32 * p), last_b) * pitch + (uint32_t)cchunk * 16u;
+    };
+    set_boff(vt0);
+    // what a lane's offset is less by: in a half slab the upper chunks are those of the lower half again
+    const uint32_t back_in_half = half && cchunk >= 4 ? 64u : 0u;
+    uint32_t back = nk == 1 ? back_in_half : 0u;
+    int l_vt = vt0, l_kt = 0;  // the next slab to fetch; past the end it stays on the last tile
+    auto advance_cursor = [&]() {
+        const bool wrap = (l_kt + 1 == nk);
+        l_kt = wrap ? 0 : l_kt + 1;
+        back = l_kt + 1 == nk ? back_in_half : 0u;
+        if (wrap && l_vt + 1 < vt1) {
+            ++l_vt;
+            if ((int64_t)(l_vt + 1) * kMxTile > m.V) set_boff(l_vt);  // the ragged tile, at most once
+        }
+    };
+    const uint8_t *const abase = m.a + n0 * pitch;
+    // chunk i (0-7: rows of b, 8-15: rows of a) of the cursor's slab -> LDS stage buf (M0 carries the LDS address of lane 0)
+    auto copy_chunk = [&](auto I, int buf) {
+        constexpr int i = decltype(I)::value;
+        const uint8_t *sbase = i < 8 ? m.b + (int64_t)l_vt * kMxTile * pitch + (int64_t)l_kt * kMxSlabBytes : abase + (int64_t)l_kt * kMxSlabBytes;
+        const uint32_t voff = (i < 8 ? boff[i & 7] : aoff[i & 7]) - back;
+        const uint8_t *stage = (i < 8 ? &lds_b[buf][0] : &lds_a[buf][0]) + 8 * wave_u * kMxSlabBytes;
+        const uint32_t lds_base = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)stage;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+        asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0"
+                     :
+                     : "s"(sbase), "v"(voff), "s"(lds_base), "n"(32 * (i & 7) * kMxSlabBytes)
+                     : "memory", "m0", "scc");
+#pragma clang diagnostic pop
+    };
+    auto copies_landed = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    // the cursor's scales: 4 KB, a copy for each wave
+    auto copy_scales = [&](int buf) {
+        const uint8_t *sbase = wave_u < 2 ? m.ta + ((int64_t)tb * nk + l_kt) * (kMxTile * 8) + wave_u * 1024
+                                          : m.tb + ((int64_t)l_vt * nk + l_kt) * (kMxTile * 8) + (wave_u - 2) * 1024;
+        const uint32_t voff = (uint32_t)lane * 16u;
+        const uint8_t *stage = &lds_s[buf][0] + wave_u * 1024;
+        const uint32_t lds_base = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)stage;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(sbase), "v"(voff), "s"(lds_base) : "memory", "m0");
+#pragma clang diagnostic pop
+    };
+
+    // ---- fragments: lane -> row l32 of a 32-row block, chunk 2 step + lh
+    const int sw = (l32 >> 1) & 7;
+    const int b_row = (wv * 128 + l32) * kMxSlabBytes, a_row = (wt * 128 + l32) * kMxSlabBytes;
+    struct Frag {
+        i32x4 b[4], a[4];
+    };
+    auto read_frag = [&](Frag &f, int i, int buf, int step) {
+        const int off = ((2 * step + lh) ^ sw) * 16;
+        if (i < 4)
+            f.b[i] = *reinterpret_cast<const i32x4 *>(&lds_b[buf][b_row + i * 32 * kMxSlabBytes + off]);
+        else
+            f.a[i - 4] = *reinterpret_cast<const i32x4 *>(&lds_a[buf][a_row + (i - 4) * 32 * kMxSlabBytes + off]);
+    };
+
+    struct Scales {
+        int b[4], a[4];
+    };
+    auto read_scales = [&](Scales &f, int buf) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f.a[j] = *reinterpret_cast<const int *>(&lds_s[buf][(wt * 128 + j * 32 + l32) * 8 + 4 * lh]);
+            f.b[j] = *reinterpret_cast<const int *>(&lds_s[buf][(kMxTile + wv * 128 + j * 32 + l32) * 8 + 4 * lh]);
+        }
+    };
+
+    f32x16 acc[4][4];
+    Frag F0, F1;
+    Scales sc, sc_next;
+    auto kstep = [&](auto STEP, const Frag &cur, Frag &nxt, int buf_next, int step_next, auto &&extra) {
+        constexpr int step = decltype(STEP)::value;
+        static_for<8>([&](auto I) {
+            constexpr int i = decltype(I)::value, e0 = 2 * i, e1 = 2 * i + 1;
+            acc[e0 >> 2][e0 & 3] = fp4_mfma<step>(cur.b[e0 >> 2], cur.a[e0 & 3], acc[e0 >> 2][e0 & 3], sc.b[e0 >> 2], sc.a[e0 & 3]);
+            extra(std::integral_constant<int, e0>());
+            acc[e1 >> 2][e1 & 3] = fp4_mfma<step>(cur.b[e1 >> 2], cur.a[e1 & 3], acc[e1 >> 2][e1 & 3], sc.b[e1 >> 2], sc.a[e1 & 3]);
+            extra(std::integral_constant<int, e1>());
+            read_frag(nxt, i, buf_next, step_next);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    auto nothing = [&](Frag &f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f.a[j] = i32x4{0, 0, 0, 0};
+    };
+    int par = 0;  // LDS stage of the slab being multiplied
+    const std::integral_constant<int, 0> k0;
+    const std::integral_constant<int, 1> k1;
+    const std::integral_constant<int, 2> k2;
+    const std::integral_constant<int, 3> k3;
+    auto cp = [&](auto PH, int buf) {
+        return [&, buf](auto E) {
+            constexpr int c = copy_at_slot(16 * decltype(PH)::value + decltype(E)::value);
+            if constexpr (c >= 0) copy_chunk(std::integral_constant<int, c>(), buf);
+        };
+    };
+    // One slab.  The stage of slab g is last read in its third k step, so after the barrier that follows it is free, and the copies of
+    // slab g + 2 go into it during the fourth step of slab g and the first two of slab g + 1; each wave waits for its own copies before
+    // the barrier of slab g + 1.  The first fragments of the next slab, of the next tile too, are read in the fourth step.
+    auto slab = [&](bool short_slab) {
+        kstep(k0, F0, F1, par, 1, cp(k1, par ^ 1));
+        kstep(k1, F1, F0, par, 2, cp(k2, par ^ 1));
+        copy_scales(par ^ 1);
+        advance_cursor();
+        if (short_slab) nothing(F0);
+        kstep(k2, F0, F1, par, 3, [&](auto) {});
+        copies_landed();
+        barrier();
+        read_scales(sc_next, par ^ 1);
+        if (short_slab) nothing(F1);
+        kstep(k3, F1, F0, par ^ 1, 0, cp(k0, par));
+        sc = sc_next;
+        par ^= 1;
+    };
+
+    // prologue: slab 0 whole, and of slab 1 what the fourth k step of a slab before it would have issued
+    static_for<16>([&](auto I) { copy_chunk(I, 0); });
+    copy_scales(0);
+    advance_cursor();
+    static_for<16>([&](auto E) { cp(k0, 1)(E); });
+    copies_landed();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) read_frag(F0, i, 0, 0);
+    read_scales(sc, 0);
+
+    for (int vt = vt0; vt < vt1; ++vt) {
+        const int64_t v0 = (int64_t)vt * kMxTile;
+        const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = zero;
+        for (int kt = 0; kt < nk; ++kt) slab(half && kt + 1 == nk);
+
+        const bool whole = v0 + kMxTile <= m.V;
+        static_for<4>([&](auto JB) {
+            constexpr int jb = decltype(JB)::value;
+            const int64_t n = n0 + wt * 128 + jb * 32 + l32;
+            const bool live = n < m.N;
+            elem *p = reinterpret_cast<elem *>(m.out) + (live ? n : 0) * m.ld;
+            static_for<4>([&](auto IB) {
+                constexpr int ib = decltype(IB)::value;
+                store_block<DT, true>(acc[ib][jb], p, (int32_t)v0 + wv * 128 + ib * 32, lh, V, whole, live);
+                __builtin_amdgcn_sched_barrier(0);  // (left to itself the compiler fetches many blocks before it stores one)
+            });
+        });
+    }
+    copies_landed();  // nothing may still be on its way into LDS that the next workgroup has
+}
+
+// Ranges so that the rounds of workgroups (one to a compute unit) times the tiles of the longest range are fewest; the fewest ranges of
+// those, because each fills its pipeline anew.
+static Mx4Plan mx4_plan(int64_t N, int64_t V)
+{
+    Mx4Plan p;
+    p.n_tb = (int)((N + kMxTile - 1) / kMxTile);
+    p.n_vt = (int)((V + kMxTile - 1) / kMxTile);
+    int64_t best = INT64_MAX;
+    p.splits = 1;
+    for (int s = 1; s <= p.n_vt && s <= 512; ++s) {
+        const int64_t rounds = ((int64_t)p.n_tb * s + 255) / 256, cost = rounds * ((p.n_vt + s - 1) / s);
+        if (cost < best) {
+            best = cost;
+            p.splits = s;
+        }
+    }
+    return p;
+}
+
+size_t mx4_product_workspace_bytes(int64_t N, int64_t V, int64_t K)
+{
+    const Mx4Plan p = mx4_plan(N, V);
+    return (size_t)(p.n_tb + (int64_t)p.n_vt) * (size_t)((K + 255) / 256) * (kMxTile * 8);
+}
+
+int launch_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
+                       int64_t V, int64_t K, void *out, int dtype, int64_t ld, void *workspace, hipStream_t stream)
+{
+    const Mx4Plan plan = mx4_plan(N, V);
+    const int nk = (int)((K + 255) / 256);
+    uint8_t *const tiled = (uint8_t *)workspace;
+    const Mx4Product m{a_codes, a_scales, b_codes, b_scales, N, V, K, out, ld, tiled, tiled + (int64_t)plan.n_tb * nk * (kMxTile * 8)};
+    mx4_tile_scales_kernel<<<dim3((unsigned)(plan.n_tb + plan.n_vt), (unsigned)((nk + kScaleSlabs - 1) / kScaleSlabs)), dim3(kBlock), 0, stream>>>(
+        a_scales, N, b_scales, V, K, plan.n_tb, tiled);
+    const dim3 grid((unsigned)((int64_t)plan.n_tb * plan.splits));
+    if (dtype == 0)
+        mx4_product_kernel<0><<<grid, dim3(kBlock), 0, stream>>>(m, plan);
+    else
+        mx4_product_kernel<1><<<grid, dim3(kBlock), 0, stream>>>(m, plan);
+    return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+
+}  // namespace difr

@@ -93,14 +93,21 @@ def test_arguments_of_the_4_bit_calls():
                          (dict(s=0x1002), ALIGN), (dict(N=0), OK)):
             assert f(**kw) == want, kw
 
-    def product(a=FAKE, sa=FAKE, N=4, b=FAKE, sb=FAKE, V=8, K=256, out=FAKE, t=0, ld=8):
-        return lib.difr_mx4_product(a, sa, N, b, sb, V, K, out, t, ld, None)
+    def product(a=FAKE, sa=FAKE, N=4, b=FAKE, sb=FAKE, V=8, K=256, out=FAKE, t=0, ld=8, ws=FAKE, n=1 << 20):
+        return lib.difr_mx4_product(a, sa, N, b, sb, V, K, out, t, ld, ws, n, None)
 
     for kw, want in ((dict(N=-1), SHAPE), (dict(V=-1), SHAPE), (dict(ld=7), SHAPE), (dict(K=0), SHAPE), (dict(K=64), SHAPE),
                      (dict(K=200), SHAPE), (dict(K=1 << 24), SHAPE), (dict(N=1 << 31), SHAPE), (dict(V=1 << 31, ld=1 << 31), SHAPE),
                      (dict(t=2), DTYPE), (dict(a=None), NULL), (dict(sb=None), NULL), (dict(out=None), NULL), (dict(a=0x1008), ALIGN),
-                     (dict(sb=0x1002), ALIGN), (dict(out=0x1001), ALIGN), (dict(N=0), OK), (dict(V=0), OK)):
+                     (dict(sb=0x1002), ALIGN), (dict(out=0x1001), ALIGN), (dict(N=0), OK), (dict(V=0), OK),
+                     (dict(ws=0x1008), ALIGN)):
         assert product(**kw) == want, kw
+    need = lib.difr_mx4_product_workspace_bytes
+    assert need(0, 8, 256) == need(4, 0, 256) == need(4, 8, 200) == need(-1, 8, 256) == 0
+    big = need(4096, 5000, 640)
+    assert big > 0
+    assert product(N=4096, V=5000, ld=5000, K=640, n=big - 1) == SHAPE
+    assert product(N=4096, V=5000, ld=5000, K=640, n=big, ws=None) == NULL
 
 
 def test_host_tensors_are_refused():
