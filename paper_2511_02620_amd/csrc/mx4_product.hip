@@ -131,7 +131,7 @@ __host__ __device__ constexpr int copy_at_slot(int n)
 //
 // Where K is an odd number of 128s the last slab of a row is half a slab: its copies fetch its four chunks twice, and its last two k steps
 // multiply zeros.
-template <int DT>
+template <int DT, bool HALF>
 __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx4Plan plan)
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds_b[2][kMxTile * kMxSlabBytes];  // 32 KB per stage
@@ -153,7 +153,6 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
     const int64_t n0 = (int64_t)tb * kMxTile;
     const uint32_t pitch = (uint32_t)(m.K / 2);  // bytes of a row's codes
     const int nk = (int)((m.K + 255) / 256);
-    const bool half = m.K % 256 != 0;
     const int32_t V = (int32_t)m.V;
 
     // ---- copies: global memory straight into LDS.  Lane i of a copy lands in chunk i % 8 of row i / 8 and fetches the chunk that the
@@ -165,32 +164,33 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
     uint32_t aoff[8], boff[8];
 #pragma unroll
     for (int p = 0; p < 8; ++p) aoff[p] = min((uint32_t)(crow + 32 * p), last_a) * pitch + (uint32_t)cchunk * 16u;
-    auto set_boff = [&](int vt) {
-        const int64_t left = m.V - (int64_t)vt * kMxTile;
-        const uint32_t last_b = (uint32_t)((left < kMxTile ? left : kMxTile) - 1);
 #pragma unroll
-        for (int p = 0; p < 8; ++p) boff[p] = min((uint32_t)(crow + 32 * p), last_b) * pitch + (uint32_t)cchunk * 16u;
+    for (int p = 0; p < 8; ++p) boff[p] = (uint32_t)(crow + 32 * p) * pitch + (uint32_t)cchunk * 16u;
+    // rows past the end of b (its last tile) re-read the last row
+    uint32_t most_b;
+    auto set_most = [&](int vt) {
+        const int32_t left = (V - vt * kMxTile < kMxTile ? V - vt * kMxTile : kMxTile) - 1;
+        most_b = (uint32_t)left * pitch + (uint32_t)cchunk * 16u;
     };
-    set_boff(vt0);
+    set_most(vt0);
     // what a lane's offset is less by: in a half slab the upper chunks are those of the lower half again
-    const uint32_t back_in_half = half && cchunk >= 4 ? 64u : 0u;
+    const uint32_t back_in_half = HALF && cchunk >= 4 ? 64u : 0u;
     uint32_t back = nk == 1 ? back_in_half : 0u;
     int l_vt = vt0, l_kt = 0;  // the next slab to fetch; past the end it stays on the last tile
+    // (no branches: the compiler would carry the matrix instructions before one past it and issue them in one piece)
     auto advance_cursor = [&]() {
-        const bool wrap = (l_kt + 1 == nk);
+        const bool wrap = l_kt + 1 == nk;
         l_kt = wrap ? 0 : l_kt + 1;
-        back = l_kt + 1 == nk ? back_in_half : 0u;
-        if (wrap && l_vt + 1 < vt1) {
-            ++l_vt;
-            if ((int64_t)(l_vt + 1) * kMxTile > m.V) set_boff(l_vt);  // the ragged tile, at most once
-        }
+        l_vt += wrap && l_vt + 1 < vt1 ? 1 : 0;
+        set_most(l_vt);
+        if (HALF) back = l_kt + 1 == nk ? back_in_half : 0u;
     };
     const uint8_t *const abase = m.a + n0 * pitch;
     // chunk i (0-7: rows of b, 8-15: rows of a) of the cursor's slab -> LDS stage buf (M0 carries the LDS address of lane 0)
     auto copy_chunk = [&](auto I, int buf) {
         constexpr int i = decltype(I)::value;
         const uint8_t *sbase = i < 8 ? m.b + (int64_t)l_vt * kMxTile * pitch + (int64_t)l_kt * kMxSlabBytes : abase + (int64_t)l_kt * kMxSlabBytes;
-        const uint32_t voff = (i < 8 ? boff[i & 7] : aoff[i & 7]) - back;
+        const uint32_t voff = (i < 8 ? min(boff[i & 7], most_b) : aoff[i & 7]) - (HALF ? back : 0u);
         const uint8_t *stage = (i < 8 ? &lds_b[buf][0] : &lds_a[buf][0]) + 8 * wave_u * kMxSlabBytes;
         const uint32_t lds_base = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)stage;
 #pragma clang diagnostic push
@@ -261,9 +261,9 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    auto nothing = [&](Frag &f) {
+    auto drop = [&](Frag &f, int keep) {  // keep: -1, or 0
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f.a[j] = i32x4{0, 0, 0, 0};
+        for (int j = 0; j < 4; ++j) f.a[j] &= keep;
     };
     int par = 0;  // LDS stage of the slab being multiplied
     const std::integral_constant<int, 0> k0;
@@ -279,17 +279,17 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
     // One slab.  The stage of slab g is last read in its third k step, so after the barrier that follows it is free, and the copies of
     // slab g + 2 go into it during the fourth step of slab g and the first two of slab g + 1; each wave waits for its own copies before
     // the barrier of slab g + 1.  The first fragments of the next slab, of the next tile too, are read in the fourth step.
-    auto slab = [&](bool short_slab) {
+    auto slab = [&](int keep) {
         kstep(k0, F0, F1, par, 1, cp(k1, par ^ 1));
         kstep(k1, F1, F0, par, 2, cp(k2, par ^ 1));
         copy_scales(par ^ 1);
         advance_cursor();
-        if (short_slab) nothing(F0);
+        if (HALF) drop(F0, keep);
         kstep(k2, F0, F1, par, 3, [&](auto) {});
         copies_landed();
         barrier();
         read_scales(sc_next, par ^ 1);
-        if (short_slab) nothing(F1);
+        if (HALF) drop(F1, keep);
         kstep(k3, F1, F0, par ^ 1, 0, cp(k0, par));
         sc = sc_next;
         par ^= 1;
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = zero;
-        for (int kt = 0; kt < nk; ++kt) slab(half && kt + 1 == nk);
+        for (int kt = 0; kt < nk; ++kt) slab(kt + 1 == nk ? 0 : -1);
 
         const bool whole = v0 + kMxTile <= m.V;
         static_for<4>([&](auto JB) {
@@ -366,10 +366,12 @@ int launch_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t 
     mx4_tile_scales_kernel<<<dim3((unsigned)(plan.n_tb + plan.n_vt), (unsigned)((nk + kScaleSlabs - 1) / kScaleSlabs)), dim3(kBlock), 0, stream>>>(
         a_scales, N, b_scales, V, K, plan.n_tb, tiled);
     const dim3 grid((unsigned)((int64_t)plan.n_tb * plan.splits));
+#define RUN(DT, HALF) mx4_product_kernel<DT, HALF><<<grid, dim3(kBlock), 0, stream>>>(m, plan)
     if (dtype == 0)
-        mx4_product_kernel<0><<<grid, dim3(kBlock), 0, stream>>>(m, plan);
+        K % 256 ? RUN(0, true) : RUN(0, false);
     else
-        mx4_product_kernel<1><<<grid, dim3(kBlock), 0, stream>>>(m, plan);
+        K % 256 ? RUN(1, true) : RUN(1, false);
+#undef RUN
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
