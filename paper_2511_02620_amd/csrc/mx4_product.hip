@@ -40,27 +40,31 @@ __device__ __forceinline__ f32x16 fp4_mfma(i32x4 a, i32x4 b, f32x16 acc, int sca
 // The scales of a matrix in the order the product's tiles want them: for each tile of 256 rows and each slab of 256 elements, 8 bytes a
 // row, those of the slab's even blocks and then those of its odd ones.  A lane of the product has the even or the odd ones, and one
 // 4-byte read serves it for four steps; a tile's share of a slab is 2 KB without gaps, where the rows themselves would have to be
-// gathered 8 bytes at a time.  Rows and blocks that are not there get 0.  One workgroup a tile and four slabs.
-constexpr int kScaleSlabs = 4;
+// gathered 8 bytes at a time.  Rows and blocks that are not there get 0.  One workgroup 32 rows and 16 slabs: rows are read 128 bytes at
+// a time, turned in LDS, and written 256 bytes at a time.
+constexpr int kScaleRows = 32, kScaleSlabs = 16;
 __global__ __launch_bounds__(kBlock) void mx4_tile_scales_kernel(const uint8_t *a, int64_t N, const uint8_t *b, int64_t V, int64_t K, int n_tb,
                                                                  uint8_t *out)
 {
-    const int tile = blockIdx.x, nk = (int)((K + 255) / 256), blocks = (int)(K / 32);
-    const uint8_t *m = tile < n_tb ? a : b;
-    const int64_t row = (int64_t)(tile < n_tb ? tile : tile - n_tb) * kMxTile + threadIdx.x, rows = tile < n_tb ? N : V;
-    const int first = blockIdx.y * kScaleSlabs;
+    __shared__ uint32_t lds[kScaleRows][2 * kScaleSlabs + 1];
+    const int tile = blockIdx.x / (kMxTile / kScaleRows), row0 = blockIdx.x % (kMxTile / kScaleRows) * kScaleRows, slab0 = blockIdx.y * kScaleSlabs;
+    const int nk = (int)((K + 255) / 256), words = (int)(K / 128);  // slabs, and 4-byte words of scales of a row
+    const bool is_a = tile < n_tb;
+    const int64_t first = (int64_t)(is_a ? tile : tile - n_tb) * kMxTile + row0, rows = is_a ? N : V;
+    const uint32_t *m = reinterpret_cast<const uint32_t *>(is_a ? a : b);
 #pragma unroll
-    for (int i = 0; i < kScaleSlabs; ++i) {
-        const int k = first + i;
-        if (k >= nk) return;
-        uint32_t lo = 0, hi = 0;
-        if (row < rows) {
-            const uint8_t *p = m + row * blocks + 8 * k;
-            lo = *reinterpret_cast<const uint32_t *>(p);
-            if (8 * k + 4 < blocks) hi = *reinterpret_cast<const uint32_t *>(p + 4);
-        }
+    for (int i = 0; i < kScaleRows * 2 * kScaleSlabs / kBlock; ++i) {
+        const int e = threadIdx.x + i * kBlock, r = e / (2 * kScaleSlabs), w = e % (2 * kScaleSlabs), word = 2 * slab0 + w;
+        lds[r][w] = first + r < rows && word < words ? m[(first + r) * words + word] : 0u;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kScaleRows * kScaleSlabs / kBlock; ++i) {
+        const int e = threadIdx.x + i * kBlock, r = e % kScaleRows, k = e / kScaleRows;
+        if (slab0 + k >= nk) continue;
+        const uint32_t lo = lds[r][2 * k], hi = lds[r][2 * k + 1];
         const uint2 w = {__builtin_amdgcn_perm(hi, lo, 0x06040200u), __builtin_amdgcn_perm(hi, lo, 0x07050301u)};
-        *reinterpret_cast<uint2 *>(out + (((int64_t)tile * nk + k) * kMxTile + threadIdx.x) * 8) = w;
+        *reinterpret_cast<uint2 *>(out + (((int64_t)tile * nk + slab0 + k) * kMxTile + row0 + r) * 8) = w;
     }
 }
 
@@ -118,7 +122,7 @@ __device__ __forceinline__ void store_block(const f32x16 acc, typename Elem<DT>:
 // step of one slab and the first two of the next.
 __host__ __device__ constexpr int copy_at_slot(int n)
 {
-    constexpr int kCopySlot[16] = {0, 3, 5, 8, 10, 13, 15, 18, 20, 23, 25, 28, 30, 33, 35, 38};
+    constexpr int kCopySlot[16] = {0, 2, 4, 6, 8, 10, 12, 14, 16, 18, 20, 22, 24, 26, 28, 30};
     for (int c = 0; c < 16; ++c)
         if (kCopySlot[c] == n) return c;
     return -1;
@@ -280,9 +284,9 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
     // slab g + 2 go into it during the fourth step of slab g and the first two of slab g + 1; each wave waits for its own copies before
     // the barrier of slab g + 1.  The first fragments of the next slab, of the next tile too, are read in the fourth step.
     auto slab = [&](int keep) {
+        copy_scales(par ^ 1);
         kstep(k0, F0, F1, par, 1, cp(k1, par ^ 1));
         kstep(k1, F1, F0, par, 2, cp(k2, par ^ 1));
-        copy_scales(par ^ 1);
         advance_cursor();
         if (HALF) drop(F0, keep);
         kstep(k2, F0, F1, par, 3, [&](auto) {});
@@ -363,7 +367,7 @@ int launch_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t 
     const int nk = (int)((K + 255) / 256);
     uint8_t *const tiled = (uint8_t *)workspace;
     const Mx4Product m{a_codes, a_scales, b_codes, b_scales, N, V, K, out, ld, tiled, tiled + (int64_t)plan.n_tb * nk * (kMxTile * 8)};
-    mx4_tile_scales_kernel<<<dim3((unsigned)(plan.n_tb + plan.n_vt), (unsigned)((nk + kScaleSlabs - 1) / kScaleSlabs)), dim3(kBlock), 0, stream>>>(
+    mx4_tile_scales_kernel<<<dim3((unsigned)((plan.n_tb + plan.n_vt) * (kMxTile / kScaleRows)), (unsigned)((nk + kScaleSlabs - 1) / kScaleSlabs)), dim3(kBlock), 0, stream>>>(
         a_scales, N, b_scales, V, K, plan.n_tb, tiled);
     const dim3 grid((unsigned)((int64_t)plan.n_tb * plan.splits));
 #define RUN(DT, HALF) mx4_product_kernel<DT, HALF><<<grid, dim3(kBlock), 0, stream>>>(m, plan)
