@@ -576,7 +576,8 @@ int difr_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N, 
 
 static bool mx4_product_shape(int64_t N, int64_t V, int64_t K)
 {
-    return N >= 0 && V >= 0 && N < (int64_t)1 << 31 && V < (int64_t)1 << 31 && K >= difr::kMxSlab && K % difr::kMxSlab == 0 && K < (int64_t)1 << 24;
+    const int64_t most = ((int64_t)1 << 31) - 1024;  // (row numbers of whole tiles stay in 32 bits)
+    return N >= 0 && V >= 0 && N <= most && V <= most && K >= difr::kMxSlab && K % difr::kMxSlab == 0 && K < (int64_t)1 << 24;
 }
 
 size_t difr_mx4_product_workspace_bytes(int64_t N, int64_t V, int64_t K)

@@ -335,6 +335,165 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
     copies_landed();  // nothing may still be on its way into LDS that the next workgroup has
 }
 
+// ---- up to 128 rows of a ----
+//
+// What bounds these is reading b once: the tile is as wide as the batch (T = 32, 64 or 128 rows of a), and the matrix instructions of a
+// slab take a fraction of the time its share of the memory bandwidth does.  A workgroup's four waves own 32 R rows of b each and all rows
+// of a.  S LDS stages, so that S - 1 slabs are in flight while one is multiplied, one barrier per slab: wait for the wave's own copies of
+// slab s (those of the slabs after it may be in flight), barrier: slab s is in LDS whole, and every wave is done with slab s - 1, whose
+// stage takes slab s + S - 1.  Scales are fetched as they are stored, 4 bytes a lane.
+//
+// The rows of b are dealt out in blocks of 32, so that no workgroup has more than one block beyond another; a workgroup's last tile is
+// as short as its blocks say, and re-reads its last row (from the L2) for what is missing.
+template <int DT, int T, int R, bool NT>
+__global__ __launch_bounds__(kBlock, T <= 64 && R == 1 ? 2 : 1) void mx4_small_kernel(Mx4Product m)
+{
+    typedef typename Elem<DT>::type elem;
+    constexpr int kRows = 128 * R, TB = T / 32, kStages = (T == 128 && R == 1) || (T == 32 && R == 2) ? 4 : 3;
+    constexpr int kCopies = 4 * R + TB + R + 1;  // per wave and slab
+    __shared__ __attribute__((aligned(16))) uint8_t lds_b[kStages][kRows * kMxSlabBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_a[kStages][T * kMxSlabBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_sb[kStages][kRows * 8];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_sa[kStages][T * 8];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int l32 = lane & 31, lh = lane >> 5;
+    const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+    const uint32_t pitch = (uint32_t)(m.K / 2), spitch = (uint32_t)(m.K / 32);
+    const int nk = (int)((m.K + 255) / 256);
+    const bool half = m.K % 256 != 0;
+    const int64_t blocks = (m.V + 31) / 32;
+    const int32_t row0 = (int32_t)(32 * (blocks * blockIdx.x / gridDim.x)), V = (int32_t)m.V;
+    const int64_t row_end = 32 * (blocks * (blockIdx.x + 1) / gridDim.x);
+    const int32_t row1 = row_end < m.V ? (int32_t)row_end : V;
+    const int tiles = (row1 - row0 + kRows - 1) / kRows, total = tiles * nk;
+
+    const int crow = tid >> 3;
+    const int cchunk = (tid & 7) ^ ((crow >> 1) & 7);
+    const uint32_t chunk0 = (uint32_t)cchunk * 16u, off0 = (uint32_t)crow * pitch + chunk0, most_a = (uint32_t)(m.N - 1) * pitch + chunk0;
+    const uint32_t word = (uint32_t)(lane & 1) * 4u;
+    const int srow_b = wave * 32 * R + (lane >> 1), srow_a = (wave & (TB - 1)) * 32 + (lane >> 1);
+    const uint32_t soff_a = (uint32_t)(srow_a < m.N ? srow_a : (int)m.N - 1) * spitch + word;
+    // in a half slab the upper chunks and the upper four scales are those of the lower half again
+    const uint32_t back_in_half = half && cchunk >= 4 ? 64u : 0u, sback_in_half = half ? word : 0u;
+
+    int f_row = row0, f_kt = 0, f_stage = 0;  // the next slab to fetch and the stage it goes to
+    auto copy16 = [&](const uint8_t *sbase, uint32_t voff, const uint8_t *stage, auto PAST) {
+        const uint32_t to = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)stage;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+        if constexpr (decltype(PAST)::value)
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0 nt" : : "s"(sbase), "v"(voff), "s"(to) : "memory", "m0");
+        else
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(sbase), "v"(voff), "s"(to) : "memory", "m0");
+#pragma clang diagnostic pop
+    };
+    auto copy4 = [&](const uint8_t *sbase, uint32_t voff, const uint8_t *stage) {
+        const uint32_t to = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)stage;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, %0" : : "s"(sbase), "v"(voff), "s"(to) : "memory", "m0");
+#pragma clang diagnostic pop
+    };
+    auto fetch_slab = [&]() {
+        const int32_t last = (row1 - f_row < kRows ? row1 - f_row : kRows) - 1;
+        const bool short_slab = half && f_kt + 1 == nk;
+        const uint32_t back = short_slab ? back_in_half : 0u, sback = short_slab ? sback_in_half : 0u;
+        const uint32_t most_b = (uint32_t)last * pitch + chunk0;
+        const uint8_t *cb = m.b + (int64_t)f_row * pitch + (int64_t)f_kt * kMxSlabBytes, *ca = m.a + (int64_t)f_kt * kMxSlabBytes;
+        const uint8_t *sb = m.bs + (int64_t)f_row * spitch + (int64_t)f_kt * 8, *sa = m.as + (int64_t)f_kt * 8;
+        static_for<4 * R>([&](auto P) {
+            constexpr int p = decltype(P)::value;
+            copy16(cb, min(off0 + (uint32_t)(32 * p) * pitch, most_b) - back, &lds_b[f_stage][(8 * wave_u + 32 * p) * kMxSlabBytes],
+                   std::integral_constant<bool, NT>());
+        });
+        static_for<TB>([&](auto P) {
+            constexpr int p = decltype(P)::value;
+            copy16(ca, min(off0 + (uint32_t)(32 * p) * pitch, most_a) - back, &lds_a[f_stage][(8 * wave_u + 32 * p) * kMxSlabBytes], std::false_type());
+        });
+        static_for<R>([&](auto P) {
+            constexpr int p = decltype(P)::value;
+            copy4(sb, (uint32_t)min(srow_b + 32 * p, (int)last) * spitch + word - sback, &lds_sb[f_stage][(wave_u * R + p) * 256]);
+        });
+        copy4(sa, soff_a - sback, &lds_sa[f_stage][(wave_u & (TB - 1)) * 256]);
+        f_stage = f_stage + 1 == kStages ? 0 : f_stage + 1;
+        if (++f_kt == nk) {
+            f_kt = 0;
+            f_row += kRows;
+        }
+    };
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    for (int i = 0; i < kStages - 1 && i < total; ++i) fetch_slab();
+    const int sw = (l32 >> 1) & 7;
+    int stage = 0, done = 0;  // stage of the next slab to multiply, slabs multiplied
+    for (int tile = 0; tile < tiles; ++tile) {
+        const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        f32x16 acc[R][TB];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) acc[i][j] = zero;
+        for (int kt = 0; kt < nk; ++kt) {
+            if (done + kStages - 1 <= total)  // the slabs up to done + kStages - 2 are on their way
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((kStages - 2) * kCopies) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            barrier();
+            if (done + kStages - 1 < total) fetch_slab();
+            const int keep = half && kt + 1 == nk ? 0 : -1;
+            uint2 sa[TB], sb[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                sb[i] = *reinterpret_cast<const uint2 *>(&lds_sb[stage][((wave * R + i) * 32 + l32) * 8]);
+                sb[i].x >>= 8 * lh;
+                sb[i].y >>= 8 * lh;
+            }
+#pragma unroll
+            for (int j = 0; j < TB; ++j) {
+                sa[j] = *reinterpret_cast<const uint2 *>(&lds_sa[stage][(j * 32 + l32) * 8]);
+                sa[j].x >>= 8 * lh;
+                sa[j].y >>= 8 * lh;
+            }
+            static_for<4>([&](auto STEP) {
+                constexpr int step = decltype(STEP)::value;
+                const int off = ((2 * step + lh) ^ sw) * 16;
+                i32x4 fb[R], fa[TB];
+#pragma unroll
+                for (int i = 0; i < R; ++i) fb[i] = *reinterpret_cast<const i32x4 *>(&lds_b[stage][((wave * R + i) * 32 + l32) * kMxSlabBytes + off]);
+#pragma unroll
+                for (int j = 0; j < TB; ++j) {
+                    fa[j] = *reinterpret_cast<const i32x4 *>(&lds_a[stage][(j * 32 + l32) * kMxSlabBytes + off]);
+                    if (step >= 2) fa[j] &= keep;
+                }
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int j = 0; j < TB; ++j)
+                        acc[i][j] = fp4_mfma<2 * (step & 1)>(fb[i], fa[j], acc[i][j], (int)(step < 2 ? sb[i].x : sb[i].y), (int)(step < 2 ? sa[j].x : sa[j].y));
+            });
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+            ++done;
+        }
+        const int32_t v0 = row0 + tile * kRows;
+        const bool whole = v0 + kRows <= row1;
+        static_for<TB>([&](auto JB) {
+            constexpr int jb = decltype(JB)::value;
+            const int n = jb * 32 + l32;
+            elem *p = reinterpret_cast<elem *>(m.out) + (int64_t)n * m.ld;
+            static_for<R>([&](auto IB) {
+                constexpr int ib = decltype(IB)::value;
+                store_block<DT, false>(acc[ib][jb], p, v0 + (wave * R + ib) * 32, lh, row1, whole, n < m.N);
+            });
+        });
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing may still be on its way into LDS that the next workgroup has
+}
+
 // Ranges so that the rounds of workgroups (one to a compute unit) times the tiles of the longest range are fewest; the fewest ranges of
 // those, because each fills its pipeline anew.
 static Mx4Plan mx4_plan(int64_t N, int64_t V)
@@ -354,15 +513,46 @@ static Mx4Plan mx4_plan(int64_t N, int64_t V)
     return p;
 }
 
+constexpr int64_t kMxSmallMost = 128;  // most rows of a of the kernel that reads b once
+
 size_t mx4_product_workspace_bytes(int64_t N, int64_t V, int64_t K)
 {
+    if (N <= kMxSmallMost) return 0;
     const Mx4Plan p = mx4_plan(N, V);
     return (size_t)(p.n_tb + (int64_t)p.n_vt) * (size_t)((K + 255) / 256) * (kMxTile * 8);
+}
+
+template <int DT, int T>
+static void run_small(const Mx4Product &m, hipStream_t stream)
+{
+    // One workgroup to a compute unit with tiles of 256 rows of b where each of them has that many, two with tiles of 128 below.  A
+    // matrix larger than the 256 MB Infinity Cache is read past it, as in the fused LM head.
+    const int64_t blocks = (m.V + 31) / 32;
+    if (blocks >= 256 * 8) {
+        const dim3 grid(256);
+        if (m.V * m.K / 2 > (int64_t)256 << 20)
+            mx4_small_kernel<DT, T, 2, true><<<grid, dim3(kBlock), 0, stream>>>(m);
+        else
+            mx4_small_kernel<DT, T, 2, false><<<grid, dim3(kBlock), 0, stream>>>(m);
+    } else {
+        const int64_t most = T <= 64 ? 512 : 256;
+        mx4_small_kernel<DT, T, 1, false><<<dim3((unsigned)(blocks < most ? blocks : most)), dim3(kBlock), 0, stream>>>(m);
+    }
 }
 
 int launch_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
                        int64_t V, int64_t K, void *out, int dtype, int64_t ld, void *workspace, hipStream_t stream)
 {
+    if (N <= kMxSmallMost) {
+        const Mx4Product m{a_codes, a_scales, b_codes, b_scales, N, V, K, out, ld, nullptr, nullptr};
+#define RUN(DT) N <= 32 ? run_small<DT, 32>(m, stream) : N <= 64 ? run_small<DT, 64>(m, stream) : run_small<DT, 128>(m, stream)
+        if (dtype == 0)
+            RUN(0);
+        else
+            RUN(1);
+#undef RUN
+        return hipGetLastError() == hipSuccess ? 0 : 1;
+    }
     const Mx4Plan plan = mx4_plan(N, V);
     const int nk = (int)((K + 255) / 256);
     uint8_t *const tiled = (uint8_t *)workspace;
