@@ -319,6 +319,8 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
             for (int j = 0; j < 4; ++j) acc[i][j] = zero;
         for (int kt = 0; kt < nk; ++kt) slab(kt + 1 == nk ? 0 : -1);
 
+        // (the accumulators are fetched by assembly statements, which the compiler does not keep away from the matrix instructions that
+        // write them: the first one read was written fifteen instructions ago, the last four are read hundreds of cycles later)
         const bool whole = v0 + kMxTile <= m.V;
         static_for<4>([&](auto JB) {
             constexpr int jb = decltype(JB)::value;
