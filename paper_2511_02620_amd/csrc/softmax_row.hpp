@@ -93,7 +93,7 @@ struct RowSums {
     double S, A;
 };
 
-// The waves' sums in a fixed order; every thread gets them.  lds: 3 floats for each wave.
+// The waves' sums in a fixed order, for the lanes of the first wave (the others get nothing of use).  lds: 3 floats for each wave.
 template <int THREADS, int DT, bool ENT>
 __device__ __forceinline__ RowSums merge_sums(const SoftmaxSums<DT, ENT> &w, float *lds)
 {
@@ -106,28 +106,53 @@ __device__ __forceinline__ RowSums merge_sums(const SoftmaxSums<DT, ENT> &w, flo
         lds[3 * wave + 2] = A;
     }
     __syncthreads();
-    float ref = lds[0];
+    RowSums r{kNoLogit, 0.0, 0.0};
+    if (wave != 0) return r;
+    const int i = threadIdx.x & (W - 1);  // a lane for each wave's sums, and copies of them
+    const float from = lds[3 * i];
+    r.ref = from;
 #pragma unroll
-    for (int i = 1; i < W; ++i) ref = fmaxf(ref, lds[3 * i]);
-    RowSums r{ref, 0.0, 0.0};
+    for (int off = W / 2; off >= 1; off >>= 1) r.ref = fmaxf(r.ref, __shfl_xor(r.ref, off, 64));
+    r.S = lds[3 * i + 1], r.A = lds[3 * i + 2];
+    if (__builtin_amdgcn_ballot_w64(from != r.ref) != 0ull) {
+        const double d = from == kNoLogit ? 0.0 : fmax(((double)from - (double)r.ref) * (double)w.c, -1000.0);
+        const double k = rint(d), f = ldexp((double)fast_exp2((float)(d - k)), (int)k);  // (a wave without a reference has seen nothing)
+        r.A = f * (r.A + d * r.S);
+        r.S *= f;
+    }
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-        const float from = lds[3 * i];
-        double s = lds[3 * i + 1], a = lds[3 * i + 2];
-        if (from != ref) {  // uniform; a wave without a reference has seen nothing
-            const double d = from == kNoLogit ? 0.0 : fmax(((double)from - (double)ref) * (double)w.c, -1000.0);
-            const double f = exp2(d);
-            a = f * (a + d * s);
-            s *= f;
-        }
-        r.S += s;
-        r.A += a;
+    for (int off = W / 2; off >= 1; off >>= 1) {
+        r.S += __shfl_xor(r.S, off, 64);
+        if (ENT) r.A += __shfl_xor(r.A, off, 64);
     }
     return r;
 }
 
-// ln p of a logit, and the entropy, in 64 bits
-__device__ __forceinline__ double row_log_prob(float x, float ref, double S, double T) { return ((double)x - (double)ref) / T - log(S); }
+// Functions of 64-bit arguments to 1e-7 of the value (of 1, for the logarithm): the part that is a power of two is taken off in 64
+// bits, the rest is small and goes through the fp32 function.  One wave evaluates them while the others wait; the 64-bit functions of
+// the library take ten times as long.
+__device__ __forceinline__ double ln_of(double S)
+{
+    const int k = S > 0.0 && S < (double)__builtin_inff() ? ilogb(S * 1.41421356) : 0;  // S 2^-k in [0.707, 1.414)
+    return (double)k * 0.69314718055994530942 + (double)logf((float)ldexp(S, -k));
+}
+__device__ __forceinline__ double exp_of(double u)
+{
+    if (!(u < 700.0)) return u;  // inf, NaN (a ratio this large is beyond fp32)
+    if (u < -700.0) return 0.0;
+    const double k = rint(u * 1.44269504088896340736);
+    return ldexp((double)expf((float)(u - k * 0.69314718055994530942)), (int)k);
+}
+__device__ __forceinline__ double expm1_of(double u) { return fabs(u) < 0.35 ? (double)expm1f((float)u) : exp_of(u) - 1.0; }
+// e^d - d - 1, by its series where the difference would cancel (the terms left out are below 1e-8 of the sum)
+__device__ __forceinline__ double exp_less_line(double d)
+{
+    if (fabs(d) >= 0.35) return exp_of(d) - d - 1.0;
+    return d * d * (0.5 + d * (1.0 / 6 + d * (1.0 / 24 + d * (1.0 / 120 + d * (1.0 / 720 + d * (1.0 / 5040 + d * (1.0 / 40320)))))));
+}
+
+// ln p of a logit
+__device__ __forceinline__ double row_log_prob(float x, float ref, double S, double T) { return ((double)x - (double)ref) / T - ln_of(S); }
 
 // Upstream gradients a (of ln p_t) and b (of the entropy) to the gradient in the logits:
 //   g_j = (1/T) [ a (1[j = t] - p_j) - b p_j (ln p_j + H) ] = e_j (k0 + k1 t_j)  for j != t
@@ -139,9 +164,9 @@ struct RowGrad {
         base = ref == kNoLogit ? 0.0f : ref;
         c = c_;
         const double z = 1.0 / (S * T);
-        k0 = (float)(z * (-a - (b != 0.0 ? b * (H - log(S)) : 0.0)));
+        k0 = (float)(z * (-a - (b != 0.0 ? b * (H - ln_of(S)) : 0.0)));
         k1 = (float)(z * -b * 0.69314718055994530942);
-        at_token = (-a * expm1(logp) - (b != 0.0 && logp > -700.0 ? b * exp(logp) * (logp + H) : 0.0)) / T;
+        at_token = (-a * expm1_of(logp) - (b != 0.0 && logp > -700.0 ? b * exp_of(logp) * (logp + H) : 0.0)) / T;
     }
     template <bool ENT>
     __device__ __forceinline__ float operator()(float x) const

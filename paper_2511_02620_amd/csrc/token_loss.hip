@@ -10,6 +10,14 @@ namespace difr {
 
 constexpr double kLn2d = 0.69314718055994530942;
 
+// An element at a uniform index of an array that the kernel does not write: a scalar load, which does not queue behind the row's.
+template <class T>
+__device__ __forceinline__ T uniform_load(const T *p, int64_t i)
+{
+    typedef const T __attribute__((address_space(4))) *constant;
+    return ((constant)(uintptr_t)p)[i];
+}
+
 // Per-row scalars.
 struct TokenRow {
     float T, c;
@@ -19,9 +27,9 @@ struct TokenRow {
 __device__ __forceinline__ TokenRow load_token_row(const TokenRows &b, int64_t row)
 {
     TokenRow r;
-    r.T = b.temperatures ? b.temperatures[row] : b.temperature;
+    r.T = b.temperatures ? uniform_load(b.temperatures, row) : b.temperature;
     r.temp_ok = r.T > 0.0f && r.T < __builtin_inff();
-    r.t = b.tokens[row];
+    r.t = uniform_load(b.tokens, row);
     r.token_ok = r.t >= 0 && (int64_t)r.t < b.V;
     r.c = r.temp_ok ? kLog2e / r.T : __builtin_nanf("");
     return r;
@@ -39,7 +47,7 @@ __device__ __forceinline__ RowResult row_result(const TokenRow &r, const RowSums
     const bool ok = r.temp_ok && s.S > 0.0 && s.S < (double)__builtin_inff();
     o.flags = (ok ? 0u : kFlagNonfinite) | (r.token_ok ? 0u : kFlagInvalidClaim);
     o.logp = ok && r.token_ok ? row_log_prob(x_t, s.ref, s.S, (double)r.T) : nan;
-    o.H = ok ? log(s.S) - kLn2d * s.A / s.S : nan;
+    o.H = ok ? ln_of(s.S) - kLn2d * s.A / s.S : nan;
     return o;
 }
 
@@ -69,7 +77,7 @@ __device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, i
     }
 }
 
-// The row's sums, by all threads of the workgroup.
+// The row's sums, by all threads of the workgroup, for the first wave.
 template <int DT, int THREADS, bool ENT>
 __device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, float c, float *lds)
 {
@@ -171,8 +179,8 @@ struct PolicyRow {
 __device__ __forceinline__ PolicyRow policy_row(const PolicyParams &p, int64_t row, double logp, double H)
 {
     PolicyRow o;
-    const double A = p.advantages[row];
-    const double ratio = p.old_logp ? exp(logp - (double)p.old_logp[row]) : (logp == logp ? 1.0 : logp);
+    const double A = uniform_load(p.advantages, row);
+    const double ratio = p.old_logp ? exp_of(logp - (double)uniform_load(p.old_logp, row)) : (logp == logp ? 1.0 : logp);
     const double lo = 1.0 - p.clip_low, hi = 1.0 + p.clip_high;
     const double inside = ratio < lo ? lo : (ratio > hi ? hi : ratio);
     const bool clipped = ratio * A > inside * A;
@@ -181,8 +189,8 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyParams &p, int64_t r
     o.a = clipped ? 0.0 : -(ratio * A);
     o.kl = 0.0;
     if (p.ref_logp) {
-        const double d = (double)p.ref_logp[row] - logp, m = expm1(d);
-        o.kl = m - d;
+        const double d = (double)uniform_load(p.ref_logp, row) - logp, m = expm1_of(d);
+        o.kl = exp_less_line(d);
         if (p.kl_coef != 0.0) {
             o.loss += p.kl_coef * o.kl;
             o.a -= p.kl_coef * m;
@@ -190,6 +198,157 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyParams &p, int64_t r
     }
     if (p.entropy_coef != 0.0) o.loss -= p.entropy_coef * H;
     return o;
+}
+
+// What one wave makes of a row's sums: its outputs, and the coefficients of its gradient.
+__device__ __forceinline__ RowGrad policy_finish(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, int64_t row, const TokenRow &r,
+                                                 const RowSums &s, float x_t, double w)
+{
+    const RowResult q = row_result(r, s, x_t);
+    const PolicyRow l = policy_row(p, row, q.logp, q.H);
+    o.row.logp[row] = (float)q.logp;
+    o.token_loss[row] = (float)l.loss;
+    if (o.row.entropy) o.row.entropy[row] = (float)q.H;
+    if (o.kl) o.kl[row] = (float)l.kl;
+    o.row.flags[row] = (uint8_t)(q.flags | l.flags);
+    RowGrad k;
+    k.set(s.ref, r.c, s.S, (double)r.T, w * l.a, -p.entropy_coef * w, q.H, q.logp);
+    return k;
+}
+
+__device__ __forceinline__ void policy_left_out(const PolicyOutputs &o, int64_t row)
+{
+    o.row.logp[row] = o.token_loss[row] = 0.0f;
+    if (o.row.entropy) o.row.entropy[row] = 0.0f;
+    if (o.kl) o.kl[row] = 0.0f;
+    o.row.flags[row] = 0;
+}
+
+template <int DT, int THREADS>
+__device__ __forceinline__ void zero_row(typename Elem<DT>::type *g, int64_t V)
+{
+    const int64_t total = (V + Elem<DT>::kPerVec - 1) / Elem<DT>::kPerVec;
+    for (int64_t i = threadIdx.x; i < total; i += THREADS) store_vector<DT>(g, i, V, u32x4{0u, 0u, 0u, 0u});
+}
+
+// Loss and gradient of rows that fit a workgroup's registers: a row is read once and its gradient written once, which is all the memory
+// traffic there has to be.  A thread holds R vectors of 16 bytes and one more of the row's ragged end; `full`, the number of vectors that
+// every thread has, is R - 8 to R.  A compute unit's registers hold one row of 150,000 bf16 logits (512 threads of 256 registers: with
+// 1024 of 128 each what is not the row does not fit), or a few shorter ones, so a workgroup keeps the memory busy by itself: as it
+// forms the gradient of a row, vector by vector, the registers that come free take the next row.
+template <int DT, int THREADS, int R, bool ENT>
+__global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_held_kernel(TokenRows b, PolicyParams p, PolicyOutputs o, int full)
+{
+    constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64;
+    typedef typename Elem<DT>::type elem;
+    __shared__ float lds_first[W], lds[3 * W];
+    __shared__ RowGrad lds_grad;
+    const int tid = threadIdx.x;
+    const int64_t step = gridDim.x, V = b.V;
+    const bool every = p.weights == nullptr;
+    const double share = 1.0 / (double)b.N;
+    const elem *const logits = reinterpret_cast<const elem *>(b.logits);
+    elem *const grad = reinterpret_cast<elem *>(o.grad);
+
+    u32x4 q[R], q_end;
+    // a thread's vector in round r of them: a uniform address (kept from the compiler, which would carry 64-bit addresses for every
+    // round in vector registers) and the same offset always
+    const uint32_t off = (uint32_t)tid * 16u;
+    auto round_of = [&](const elem *x, int r) {
+        uint64_t a = (uint64_t)(uintptr_t)x + (uint64_t)(r * (THREADS * 16));
+        asm("" : "+s"(a));
+        return (__attribute__((address_space(1))) char *)a;
+    };
+    typedef __attribute__((address_space(1))) u32x4_any global_vector;
+    auto load = [&](const elem *x, int r) { return __builtin_nontemporal_load((const global_vector *)(round_of(x, r) + off)); };
+    // the next row that counts, from `row` on; those before it get their zeros
+    auto next_live = [&](int64_t row, float &w) {
+        while (row < b.N) {
+            w = every ? 1.0f : uniform_load(p.weights, row);
+            if (w != 0.0f) break;
+            if (tid == 0) policy_left_out(o, row);
+            zero_row<DT, THREADS>(grad + row * o.ld_grad, V);
+            row += step;
+        }
+        return row;
+    };
+    float w;
+    int64_t row = next_live(blockIdx.x, w);
+    if (row < b.N) {
+        const elem *x = logits + row * b.ld;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < R - 8 || r < full) q[r] = load(x, r);
+        q_end = row_vector<DT>(x, (int64_t)full * THREADS + tid, V);
+    }
+    while (row < b.N) {
+        const TokenRow t = load_token_row(b, row);
+        const elem x_t = logits[row * b.ld + (t.token_ok ? t.t : 0)];
+        // the reference, of the row's first and last entries
+        {
+            float y[E];
+            unpack_vector<DT>(q_end, y);
+            float m = vector_max<DT>(y);
+            if (full > 0) {
+                unpack_vector<DT>(q[0], y);
+                m = fmaxf(m, vector_max<DT>(y));
+            }
+            m = wave_max(m);
+            if ((tid & 63) == 0) lds_first[tid >> 6] = m;
+        }
+        __syncthreads();
+        float first = lds_first[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) first = fmaxf(first, lds_first[i]);
+        SoftmaxSums<DT, ENT> s;
+        s.begin(first, t.c);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < R - 8 || r < full) {
+                float y[E];
+                unpack_vector<DT>(q[r], y);
+                s.add(y);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        {
+            float y[E];
+            unpack_vector<DT>(q_end, y);
+            s.add(y);
+        }
+        const RowSums sums = merge_sums<THREADS>(s, lds);
+        if (tid == 0) lds_grad = policy_finish(b, p, o, row, t, sums, Elem<DT>::to_float(x_t), every ? share : (double)w);
+        float w_next = 0.0f;
+        const int64_t next = next_live(row + step, w_next);
+        __syncthreads();
+        const RowGrad k = lds_grad;
+        elem *const g = grad + row * o.ld_grad;
+        const bool more = next < b.N;
+        const elem *const xn = logits + (more ? next : row) * b.ld;  // (the last row is read again, and not used, rather than branched round)
+        auto form = [&](u32x4 v) {
+            float y[E];
+            asm volatile("" : "+v"(v));  // unpacked anew: the compiler would keep the values from the first time, twice the registers
+            unpack_vector<DT>(v, y);
+#pragma unroll
+            for (int j = 0; j < E; ++j) y[j] = k.operator()<ENT>(y[j]);
+            return pack_vector<DT>(y);
+        };
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < R - 8 || r < full) {
+                *(global_vector *)(round_of(g, r) + off) = form(q[r]);
+                q[r] = load(xn, r);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        {
+            const int64_t i = (int64_t)full * THREADS + tid;
+            if (i * E < V) store_vector<DT>(g, i, V, form(q_end));
+            if (more) q_end = row_vector<DT>(xn, i, V);
+        }
+        // the token's own entry, by the thread that has written its vector (a wave's stores to one address keep their order)
+        if (t.token_ok && (t.t / E) % THREADS == tid) store_element<DT>(g + t.t, (float)k.at_token);
+        row = next;
+        w = w_next;
+    }
 }
 
 // One workgroup a row, which it reads twice: the row's sums, then the gradient.
@@ -203,33 +362,16 @@ __global__ __launch_bounds__(THREADS) void policy_kernel(TokenRows b, PolicyPara
     typedef typename Elem<DT>::type elem;
     const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
     elem *g = reinterpret_cast<elem *>(o.grad) + row * o.ld_grad;
-    const double w = p.weights ? (double)p.weights[row] : 1.0 / (double)b.N;
+    const double w = p.weights ? (double)uniform_load(p.weights, row) : 1.0 / (double)b.N;
     if (w == 0.0) {  // left out
-        if (threadIdx.x == 0) {
-            o.row.logp[row] = o.token_loss[row] = 0.0f;
-            if (o.row.entropy) o.row.entropy[row] = 0.0f;
-            if (o.kl) o.kl[row] = 0.0f;
-            o.row.flags[row] = 0;
-        }
-        if (o.grad) {
-            const int64_t total = (b.V + E - 1) / E;
-            for (int64_t i = threadIdx.x; i < total; i += THREADS) store_vector<DT>(g, i, b.V, u32x4{0u, 0u, 0u, 0u});
-        }
+        if (threadIdx.x == 0) policy_left_out(o, row);
+        if (o.grad) zero_row<DT, THREADS>(g, b.V);
         return;
     }
     const TokenRow r = load_token_row(b, row);
     const float x_t = r.token_ok ? Elem<DT>::to_float(x[r.t]) : 0.0f;
     const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, lds);
-    if (threadIdx.x == 0) {
-        const RowResult q = row_result(r, s, x_t);
-        const PolicyRow l = policy_row(p, row, q.logp, q.H);
-        o.row.logp[row] = (float)q.logp;
-        o.token_loss[row] = (float)l.loss;
-        if (o.row.entropy) o.row.entropy[row] = (float)q.H;
-        if (o.kl) o.kl[row] = (float)l.kl;
-        o.row.flags[row] = (uint8_t)(q.flags | l.flags);
-        lds_grad.set(s.ref, r.c, s.S, (double)r.T, w * l.a, -p.entropy_coef * w, q.H, q.logp);
-    }
+    if (threadIdx.x == 0) lds_grad = policy_finish(b, p, o, row, r, s, x_t, w);
     if (!o.grad) return;
     __syncthreads();
     const RowGrad k = lds_grad;
@@ -377,16 +519,41 @@ int launch_token_logprob_backward(const TokenRows &b, const float *stats, const 
     return launched();
 }
 
+template <int DT, bool ENT>
+static void run_policy(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, hipStream_t stream)
+{
+    constexpr int E = Elem<DT>::kPerVec;
+    const int64_t vectors = b.V / E;
+    // vectors that every thread has, for workgroups of so many threads; a row is held up to 38 of them
+    const int64_t f256 = vectors / 256, f512 = vectors / 512;
+    if (o.grad && f512 <= 38) {
+        const bool wide = f256 > 38 || (b.N <= 256 && f512 > 0);  // a row or fewer to a compute unit: more threads for it
+        const int64_t full = wide ? f512 : f256;
+#define RUN(THREADS, R)                                                                                                          \
+    {                                                                                                                            \
+        const int64_t most = (int64_t)256 * ((R <= 8 ? 1024 : R <= 16 ? 768 : 512) / THREADS);                                   \
+        policy_held_kernel<DT, THREADS, R, ENT><<<dim3((unsigned)(b.N < most ? b.N : most)), dim3(THREADS), 0, stream>>>(b, p, o, (int)full); \
+        return;                                                                                                                  \
+    }
+#define RUN_R(R)                       \
+    if (full <= R) {                   \
+        if (wide) RUN(512, R) else RUN(256, R) \
+    }
+        RUN_R(8) RUN_R(16) RUN_R(24) RUN_R(31) RUN_R(38)
+#undef RUN_R
+#undef RUN
+    }
+    policy_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, p, o);
+}
+
 int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, hipStream_t stream)
 {
     if (b.N > 0) {
         const bool ent = o.row.entropy || p.entropy_coef != 0.0;
-#define RUN(DT, ENT) policy_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, p, o)
         if (b.dtype == 0)
-            ent ? RUN(0, true) : RUN(0, false);
+            ent ? run_policy<0, true>(b, p, o, stream) : run_policy<0, false>(b, p, o, stream);
         else
-            ent ? RUN(1, true) : RUN(1, false);
-#undef RUN
+            ent ? run_policy<1, true>(b, p, o, stream) : run_policy<1, false>(b, p, o, stream);
     }
     weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(o.token_loss, p.weights, b.N ? 1.0 / (double)b.N : 0.0, b.N, o.loss);
     return launched();

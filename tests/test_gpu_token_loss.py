@@ -223,8 +223,12 @@ def test_policy_loss(difr, N, V, dtype, old, refl, weights, eta):
     slack = (wt.double() * lb * (r * A.abs() + (beta * (r_l.double() - want["logp"]).exp() if refl else 0))).nan_to_num(0)[:, None] / T[:, None]
     lim = ref.grad_bound(grad, want["lp"], want["H"], T, want["a"], want["b"] if eta else None, dtype) + slack
     ref.assert_within(got["grad"], grad, lim, "gradient")
+    # without the gradient the row is summed in another order: two sums of the same bound
     again = difr.policy_loss(xd, 1.0, dev(tok), dev(A), want_entropy=True, want_grad=False, **call)
-    assert "grad" not in again and all(torch.equal(again[k], got[k]) for k in again), "the gradient changes nothing else"
+    assert "grad" not in again and torch.equal(again["flags"], got["flags"])
+    ref.assert_within(again["logp"], want["logp"], lb)
+    ref.assert_within(again["token_loss"], want["token_loss"], each_bound)
+    ref.assert_within(again["loss"], want["loss"], total + e * want["loss"].abs() + 1e-37)
     if torch.isnan(x).any():
         return
     same = _on_device(x, 1, 2)
