@@ -235,10 +235,16 @@ __device__ __forceinline__ void zero_row(typename Elem<DT>::type *g, int64_t V)
 // traffic there has to be.  A thread holds R vectors of 16 bytes and one more of the row's ragged end; `full`, the number of vectors that
 // every thread has, is R - 8 to R.  A compute unit's registers hold one row of 150,000 bf16 logits (512 threads of 256 registers: with
 // 1024 of 128 each what is not the row does not fit), or a few shorter ones, so a workgroup keeps the memory busy by itself: as it
-// forms the gradient of a row, vector by vector, the registers that come free take the next row.
-template <int DT, int THREADS, int R, bool ENT>
-__global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_held_kernel(TokenRows b, PolicyParams p, PolicyOutputs o, int full)
+// forms the gradient of a row, vector by vector, the registers that come free take the next row.  LDS: what a longer row has beyond its
+// registers, up to 17 rounds of vectors, is held in LDS, copied there by the memory system; a thread's vectors are its own there too.
+// Stores go past the caches, loads do not: the gradient is not read soon, the logits may have been written just now (8192 x 151,936 bf16,
+// us: stores through the caches 1105, past them 1045, loads too 1042; 256 rows that lie in the Infinity Cache 44, loads past it 50).
+constexpr int kLdsRounds = 17;
+template <int DT, int THREADS, int R, bool ENT, bool LDS>
+__global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_held_kernel(TokenRows b, PolicyParams p, PolicyOutputs o, int full,
+                                                                                            int lds_rounds)
 {
+    __shared__ __attribute__((aligned(16))) uint8_t lds_row[LDS ? kLdsRounds * THREADS * 16 : 16];
     constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64;
     typedef typename Elem<DT>::type elem;
     __shared__ float lds_first[W], lds[3 * W];
@@ -260,7 +266,20 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
         return (__attribute__((address_space(1))) char *)a;
     };
     typedef __attribute__((address_space(1))) u32x4_any global_vector;
-    auto load = [&](const elem *x, int r) { return __builtin_nontemporal_load((const global_vector *)(round_of(x, r) + off)); };
+    auto load = [&](const elem *x, int r) { return *((const global_vector *)(round_of(x, r) + off)); };
+    // LDS round l of a row is its round R + l
+    const int wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+    auto copy_rounds = [&](const elem *x) {
+        for (int l = 0; l < lds_rounds; ++l) {
+            const char *from = reinterpret_cast<const char *>(x) + (int64_t)(R + l) * (THREADS * 16);
+            const uint32_t to = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds_row + (uint32_t)(l * THREADS * 16 + wave_u * 1024);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(from), "v"(off), "s"(to) : "memory", "m0");
+#pragma clang diagnostic pop
+        }
+    };
+    auto lds_vector = [&](int l) { return *reinterpret_cast<const u32x4 *>(lds_row + (l * THREADS + tid) * 16); };
     // the next row that counts, from `row` on; those before it get their zeros
     auto next_live = [&](int64_t row, float &w) {
         while (row < b.N) {
@@ -276,10 +295,11 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
     int64_t row = next_live(blockIdx.x, w);
     if (row < b.N) {
         const elem *x = logits + row * b.ld;
+        if (LDS) copy_rounds(x);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < R - 8 || r < full) q[r] = load(x, r);
-        q_end = row_vector<DT>(x, (int64_t)full * THREADS + tid, V);
+        q_end = row_vector<DT>(x, (int64_t)(full + lds_rounds) * THREADS + tid, V);
     }
     while (row < b.N) {
         const TokenRow t = load_token_row(b, row);
@@ -302,6 +322,15 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
         for (int i = 1; i < W; ++i) first = fmaxf(first, lds_first[i]);
         SoftmaxSums<DT, ENT> s;
         s.begin(first, t.c);
+        if (LDS) {
+            // (memory operations end in order: the copies are older than the loads and stores of the rounds that every row has)
+            asm volatile("s_waitcnt vmcnt(%0)" : : "n"(R - 8) : "memory");
+            for (int l = 0; l < lds_rounds; ++l) {
+                float y[E];
+                unpack_vector<DT>(lds_vector(l), y);
+                s.add(y);
+            }
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < R - 8 || r < full) {
@@ -332,15 +361,21 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
             for (int j = 0; j < E; ++j) y[j] = k.operator()<ENT>(y[j]);
             return pack_vector<DT>(y);
         };
+        if (LDS) {
+            for (int l = 0; l < lds_rounds; ++l)
+                __builtin_nontemporal_store(form(lds_vector(l)), (global_vector *)(round_of(g, R + l) + off));
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every vector has been read before its place is copied to
+            copy_rounds(xn);
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < R - 8 || r < full) {
-                *(global_vector *)(round_of(g, r) + off) = form(q[r]);
+                __builtin_nontemporal_store(form(q[r]), (global_vector *)(round_of(g, r) + off));
                 q[r] = load(xn, r);
                 __builtin_amdgcn_sched_barrier(0);
             }
         {
-            const int64_t i = (int64_t)full * THREADS + tid;
+            const int64_t i = (int64_t)(full + lds_rounds) * THREADS + tid;
             if (i * E < V) store_vector<DT>(g, i, V, form(q_end));
             if (more) q_end = row_vector<DT>(xn, i, V);
         }
@@ -349,11 +384,13 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
         row = next;
         w = w_next;
     }
+    if (LDS) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy is on its way into LDS that the next workgroup has
 }
 
-// One workgroup a row, which it reads twice: the row's sums, then the gradient.
+// One workgroup a row, which it reads twice: the row's sums, then the gradient.  For rows that do not fit a compute unit, and for the
+// loss alone.
 template <int DT, int THREADS, bool ENT>
-__global__ __launch_bounds__(THREADS) void policy_kernel(TokenRows b, PolicyParams p, PolicyOutputs o)
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THREADS == 1024 ? 4 : 8))) void policy_kernel(TokenRows b, PolicyParams p, PolicyOutputs o)
 {
     constexpr int E = Elem<DT>::kPerVec;
     __shared__ float lds[3 * THREADS / 64];
@@ -524,26 +561,32 @@ static void run_policy(const TokenRows &b, const PolicyParams &p, const PolicyOu
 {
     constexpr int E = Elem<DT>::kPerVec;
     const int64_t vectors = b.V / E;
-    // vectors that every thread has, for workgroups of so many threads; a row is held up to 38 of them
+    // vectors that every thread has, for workgroups of so many threads; a row is held up to 38 of them, and 17 more in LDS
     const int64_t f256 = vectors / 256, f512 = vectors / 512;
-    if (o.grad && f512 <= 38) {
+    if (o.grad && f512 <= 38 + kLdsRounds) {
         const bool wide = f256 > 38 || (b.N <= 256 && f512 > 0);  // a row or fewer to a compute unit: more threads for it
-        const int64_t full = wide ? f512 : f256;
-#define RUN(THREADS, R)                                                                                                          \
+        const int full = (int)(wide ? f512 : f256);
+#define RUN(THREADS, R, LDS)                                                                                                     \
     {                                                                                                                            \
         const int64_t most = (int64_t)256 * ((R <= 8 ? 1024 : R <= 16 ? 768 : 512) / THREADS);                                   \
-        policy_held_kernel<DT, THREADS, R, ENT><<<dim3((unsigned)(b.N < most ? b.N : most)), dim3(THREADS), 0, stream>>>(b, p, o, (int)full); \
+        policy_held_kernel<DT, THREADS, R, ENT, LDS><<<dim3((unsigned)(b.N < most ? b.N : most)), dim3(THREADS), 0, stream>>>(   \
+            b, p, o, full < R ? full : R, full < R ? 0 : full - R);                                                              \
         return;                                                                                                                  \
     }
-#define RUN_R(R)                       \
-    if (full <= R) {                   \
-        if (wide) RUN(512, R) else RUN(256, R) \
+#define RUN_R(R)                                             \
+    if (full <= R) {                                         \
+        if (wide) RUN(512, R, false) else RUN(256, R, false) \
     }
         RUN_R(8) RUN_R(16) RUN_R(24) RUN_R(31) RUN_R(38)
+        RUN(512, 38, true)
 #undef RUN_R
 #undef RUN
     }
-    policy_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, p, o);
+    // With the gradient one workgroup to a compute unit, so that the rows stay in the Infinity Cache until they are read again.
+    if (o.grad)
+        policy_kernel<DT, 1024, ENT><<<dim3((unsigned)b.N), dim3(1024), 0, stream>>>(b, p, o);
+    else
+        policy_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, p, o);
 }
 
 int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, hipStream_t stream)

@@ -177,7 +177,9 @@ def _policy_ref(x, T, tok, A, w, old, refl, lo, hi, beta, eta):
                 clipped=clipped & live, a=torch.where(live, w * a, zero), b=-eta * w, lp=lp, H=H)
 
 
-@pytest.mark.parametrize("N,V", [(1, 1), (2, 50), (33, 1024), (5, 8197), (3, 40001), (2, 151936), (300, 515)])
+# (rows of a workgroup's registers in all their lengths, from one vector to a compute unit's; with LDS; longer ones)
+@pytest.mark.parametrize("N,V", [(1, 1), (2, 50), (33, 1024), (5, 8197), (3, 40001), (2, 151936), (300, 515), (259, 20003), (3, 75000),
+                                 (3, 100001), (2, 165000), (2, 230001)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("old,refl,weights,eta", [(1, 1, 1, 0.0), (1, 1, 1, 0.02), (0, 0, 0, 0.0), (1, 0, 1, 0.01), (0, 1, 0, 0.0)])
 def test_policy_loss(difr, N, V, dtype, old, refl, weights, eta):
@@ -229,7 +231,7 @@ def test_policy_loss(difr, N, V, dtype, old, refl, weights, eta):
     ref.assert_within(again["logp"], want["logp"], lb)
     ref.assert_within(again["token_loss"], want["token_loss"], each_bound)
     ref.assert_within(again["loss"], want["loss"], total + e * want["loss"].abs() + 1e-37)
-    if torch.isnan(x).any():
+    if torch.isnan(x).any() or V > 160000:
         return
     same = _on_device(x, 1, 2)
     o = difr.policy_loss(same, 1.0, dev(tok), dev(A), out=same, **call)
