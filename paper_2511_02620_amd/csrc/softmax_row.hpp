@@ -154,6 +154,12 @@ __device__ __forceinline__ double exp_less_line(double d)
 // ln p of a logit
 __device__ __forceinline__ double row_log_prob(float x, float ref, double S, double T) { return ((double)x - (double)ref) / T - ln_of(S); }
 
+// g_t of the token, for upstream gradients a (of ln p_t) and b (of the entropy)
+__device__ __forceinline__ double token_entry(double a, double b, double H, double logp, double T)
+{
+    return (-a * expm1_of(logp) - (b != 0.0 && logp > -700.0 ? b * exp_of(logp) * (logp + H) : 0.0)) / T;
+}
+
 // Upstream gradients a (of ln p_t) and b (of the entropy) to the gradient in the logits:
 //   g_j = (1/T) [ a (1[j = t] - p_j) - b p_j (ln p_j + H) ] = e_j (k0 + k1 t_j)  for j != t
 struct RowGrad {
@@ -166,7 +172,16 @@ struct RowGrad {
         const double z = 1.0 / (S * T);
         k0 = (float)(z * (-a - (b != 0.0 ? b * (H - ln_of(S)) : 0.0)));
         k1 = (float)(z * -b * 0.69314718055994530942);
-        at_token = (-a * expm1_of(logp) - (b != 0.0 && logp > -700.0 ? b * exp_of(logp) * (logp + H) : 0.0)) / T;
+        at_token = token_entry(a, b, H, logp, T);
+    }
+    // the same in fp32 and without the token's entry, for a stretch of a row (k0 and k1 to some 1e-7)
+    __device__ __forceinline__ void set_stretch(float ref, float c_, float S, float T, float a, float b, float H)
+    {
+        base = ref == kNoLogit ? 0.0f : ref;
+        c = c_;
+        const float z = 1.0f / S / T;
+        k0 = z * (-a - (b != 0.0f ? b * (H - logf(S)) : 0.0f));
+        k1 = z * -b * kLn2;
     }
     template <bool ENT>
     __device__ __forceinline__ float operator()(float x) const
