@@ -51,8 +51,9 @@ __device__ __forceinline__ RowResult row_result(const TokenRow &r, const RowSums
     return o;
 }
 
-// The row in vectors of 16 bytes, U of a thread's in flight; f(values, index of the vector) is called by whole waves.
-template <int DT, int THREADS, int U, class F>
+// The row in vectors of 16 bytes, U of a thread's in flight; f(values, index of the vector) is called by whole waves.  PAST: past the
+// caches.
+template <int DT, int THREADS, int U, bool PAST, class F>
 __device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, int64_t V, F &&f)
 {
     constexpr int E = Elem<DT>::kPerVec;
@@ -62,7 +63,10 @@ __device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, i
     for (; i + (int64_t)U * THREADS <= nvec; i += (int64_t)U * THREADS) {
         u32x4 q[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) q[u] = *reinterpret_cast<const u32x4_any *>(row + (i + u * THREADS + tid) * E);
+        for (int u = 0; u < U; ++u) {
+            const u32x4_any *p = reinterpret_cast<const u32x4_any *>(row + (i + u * THREADS + tid) * E);
+            q[u] = PAST ? __builtin_nontemporal_load(p) : *p;
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float x[E];
@@ -79,7 +83,7 @@ __device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, i
 
 // The row's sums, by all threads of the workgroup, for the first wave.
 template <int DT, int THREADS, bool ENT>
-__device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, float c, float *lds)
+__device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, float c, bool past, float *lds)
 {
     constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64;
     float x[E];
@@ -93,8 +97,19 @@ __device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, 
     __syncthreads();
     SoftmaxSums<DT, ENT> s;
     s.begin(first, c);
-    stream_row<DT, THREADS, 4>(row, V, [&](const float *v, int64_t) { s.add(v); });
+    if (past)
+        stream_row<DT, THREADS, 4, true>(row, V, [&](const float *v, int64_t) { s.add(v); });
+    else
+        stream_row<DT, THREADS, 4, false>(row, V, [&](const float *v, int64_t) { s.add(v); });
     return merge_sums<THREADS>(s, lds);
+}
+
+// Whether a row is read past the caches: all but the last 192 MB of the logits, which the 256 MB Infinity Cache may hold - they were
+// written last, and a gradient that follows begins with them.  Forward pass, us, through the caches / past them: 8192 x 128,256 bf16 (2.1
+// GB) 362 / 323, 2048 x 151,936 (622 MB) 119 / 102, 2048 x 50,257 (206 MB, read again and again) 35.6 / 44.7.
+__device__ __forceinline__ bool read_past(const TokenRows &b, int64_t row)
+{
+    return (b.N - 1 - row) * b.ld * (b.dtype == 0 ? 2 : 4) > ((int64_t)192 << 20);
 }
 
 template <int DT, int THREADS, bool ENT>
@@ -115,7 +130,7 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, con
     }
     const TokenRow r = load_token_row(b, row);
     const float x_t = r.token_ok ? Elem<DT>::to_float(x[r.t]) : 0.0f;
-    const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, lds);
+    const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, read_past(b, row), lds);
     if (threadIdx.x == 0) {
         const RowResult q = row_result(r, s, x_t);
         o.logp[row] = (float)q.logp;
@@ -431,12 +446,12 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THRE
     }
     const TokenRow r = load_token_row(b, row);
     const float x_t = r.token_ok ? Elem<DT>::to_float(x[r.t]) : 0.0f;
-    const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, lds);
+    const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, !o.grad && read_past(b, row), lds);
     if (threadIdx.x == 0) lds_grad = policy_finish(b, p, o, row, r, s, x_t, w);
     if (!o.grad) return;
     __syncthreads();
     const RowGrad k = lds_grad;
-    stream_row<DT, THREADS, 4>(x, b.V, [&](const float *v, int64_t i) {
+    stream_row<DT, THREADS, 4, false>(x, b.V, [&](const float *v, int64_t i) {
         float d[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) d[j] = k.operator()<ENT>(v[j]);
