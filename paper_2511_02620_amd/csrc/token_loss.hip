@@ -85,7 +85,7 @@ __device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, i
 template <int DT, int THREADS, bool ENT>
 __device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, float c, bool past, float *lds)
 {
-    constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64;
+    constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64, U = 4;
     float x[E];
     unpack_vector<DT>(row_vector<DT>(row, threadIdx.x, V), x);
     const float m = wave_max(vector_max<DT>(x));
@@ -98,9 +98,9 @@ __device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, 
     SoftmaxSums<DT, ENT> s;
     s.begin(first, c);
     if (past)
-        stream_row<DT, THREADS, 4, true>(row, V, [&](const float *v, int64_t) { s.add(v); });
+        stream_row<DT, THREADS, U, true>(row, V, [&](const float *v, int64_t) { s.add(v); });
     else
-        stream_row<DT, THREADS, 4, false>(row, V, [&](const float *v, int64_t) { s.add(v); });
+        stream_row<DT, THREADS, U, false>(row, V, [&](const float *v, int64_t) { s.add(v); });
     return merge_sums<THREADS>(s, lds);
 }
 
@@ -119,6 +119,7 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, con
     const int64_t row = blockIdx.x;
     typedef typename Elem<DT>::type elem;
     const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
+    if (o.zero && threadIdx.x == 0) o.zero[row] = 0.0f;
     if (mask && mask[row] == 0) {
         if (threadIdx.x == 0) {
             o.logp[row] = 0.0f;
@@ -143,6 +144,35 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, con
     }
 }
 
+// sum_n weight[n] value[n] by one workgroup, in 64 bits and a fixed order.  A weight of 0 leaves its value out.
+struct WeightedSum {
+    const float *value, *weight;  // weight null: `every`
+    double every;
+    int64_t n;
+    float *out;
+};
+template <int THREADS>
+__device__ __forceinline__ void weighted_sum(const WeightedSum &w)
+{
+    __shared__ double lds[THREADS / 64];
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < w.n; i += THREADS) {
+        const double f = w.weight ? (double)w.weight[i] : w.every;
+        if (f != 0.0) sum += f * (double)w.value[i];
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double s = lds[0];
+        for (int i = 1; i < THREADS / 64; ++i) s += lds[i];
+        *w.out = (float)s;
+    }
+}
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void weighted_sum_kernel(WeightedSum w) { weighted_sum<kSumThreads>(w); }
+
 // The gradient of a row from its statistics: every workgroup has a stretch of 8 KB of it.  Bound by memory, and by how much of it is asked
 // for at a time: two vectors of a thread and six waves to a SIMD, 12 MB over the device.  8192 x 128,256 bf16, forward and backward with
 // the entropy / preference loss, us: 8 vectors in a loop 1178 / 1184; at once, eight waves: 4 vectors 1112 / 1122, 2 1073 / 1085,
@@ -153,10 +183,11 @@ constexpr int kGradVectors = 2;  // of each thread
 
 template <int DT, bool ENT>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6,6))) void token_grad_kernel(TokenRows b, const float *stats, const float *entropy, const float *grad_logp,
-                                                            const float *grad_entropy, void *grad, int64_t ld_grad)
+                                                            const float *grad_entropy, void *grad, int64_t ld_grad, WeightedSum sum)
 {
     constexpr int E = Elem<DT>::kPerVec;
     typedef typename Elem<DT>::type elem;
+    if (sum.out && blockIdx.x == 0 && blockIdx.y == 0) weighted_sum<kBlock>(sum);
     const int64_t row = b.N - 1 - blockIdx.y;
     const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
     elem *g = reinterpret_cast<elem *>(grad) + row * ld_grad;
@@ -464,27 +495,6 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THRE
     });
 }
 
-// sum_n weight[n] value[n] by one workgroup, in 64 bits and a fixed order.  A weight of 0 leaves its value out.
-constexpr int kSumThreads = 1024;
-__global__ __launch_bounds__(kSumThreads) void weighted_sum_kernel(const float *value, const float *weight, double every, int64_t n, float *out)
-{
-    __shared__ double lds[kSumThreads / 64];
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kSumThreads) {
-        const double w = weight ? (double)weight[i] : every;
-        if (w != 0.0) sum += w * (double)value[i];
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double s = lds[0];
-        for (int i = 1; i < kSumThreads / 64; ++i) s += lds[i];
-        *out = (float)s;
-    }
-}
-
 // ---- pairs ----
 
 // The pair of sequences 2 p (chosen) and 2 p + 1 (rejected): log-probabilities summed in 64 bits and a fixed order, the loss, and
@@ -546,12 +556,6 @@ __global__ __launch_bounds__(kBlock) void pair_kernel(int64_t N, PreferenceParam
     }
 }
 
-__global__ __launch_bounds__(kBlock) void zero_outside_kernel(int64_t N, const int64_t *seq_offsets, int64_t S, float *grad_logp)
-{
-    const int64_t n = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (n < N && (S == 0 || n < seq_offsets[0] || n >= seq_offsets[S])) grad_logp[n] = 0.0f;
-}
-
 // ---- launches ----
 
 static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
@@ -559,7 +563,11 @@ static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 template <int DT, bool ENT>
 static void run_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, hipStream_t stream)
 {
-    token_logprob_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, mask, o);
+    // Few long rows: all of a compute unit's threads that a workgroup can have for one.  (24 rows of 151,936 bf16 logits: 17 / 10 us a call)
+    if (b.N <= 512 && b.V >= 16384)
+        token_logprob_kernel<DT, 1024, ENT><<<dim3((unsigned)b.N), dim3(1024), 0, stream>>>(b, mask, o);
+    else
+        token_logprob_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, mask, o);
 }
 
 int launch_token_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, hipStream_t stream)
@@ -571,12 +579,13 @@ int launch_token_logprob(const TokenRows &b, const uint8_t *mask, const LogProbO
     return launched();
 }
 
-int launch_token_logprob_backward(const TokenRows &b, const float *stats, const float *entropy, const float *grad_logp,
-                                  const float *grad_entropy, void *grad, int64_t ld_grad, hipStream_t stream)
+// `sum`: formed beside the gradient (out null: none)
+static int run_backward(const TokenRows &b, const float *stats, const float *entropy, const float *grad_logp, const float *grad_entropy,
+                        void *grad, int64_t ld_grad, WeightedSum sum, hipStream_t stream)
 {
     const int64_t E = b.dtype == 0 ? 8 : 4, vectors = (b.V + E - 1) / E, per = kBlock * kGradVectors;
     constexpr int64_t kMostRows = 65535;  // of a launch: the grid's second dimension
-    for (int64_t n = 0; n < b.N; n += kMostRows) {
+    for (int64_t n = (b.N - 1) / kMostRows * kMostRows; n >= 0; n -= kMostRows) {
         TokenRows part = b;
         part.N = b.N - n < kMostRows ? b.N - n : kMostRows;
         part.logits = (const char *)b.logits + n * b.ld * (b.dtype == 0 ? 2 : 4);
@@ -585,14 +594,21 @@ int launch_token_logprob_backward(const TokenRows &b, const float *stats, const 
         void *g = (char *)grad + n * ld_grad * (b.dtype == 0 ? 2 : 4);
         const dim3 grid((unsigned)((vectors + per - 1) / per), (unsigned)part.N);
         const float *ent = entropy ? entropy + n : nullptr, *ge = grad_entropy ? grad_entropy + n : nullptr;
-#define RUN(DT, ENT) token_grad_kernel<DT, ENT><<<grid, dim3(kBlock), 0, stream>>>(part, stats + 2 * n, ent, grad_logp + n, ge, g, ld_grad)
+#define RUN(DT, ENT) token_grad_kernel<DT, ENT><<<grid, dim3(kBlock), 0, stream>>>(part, stats + 2 * n, ent, grad_logp + n, ge, g, ld_grad, sum)
         if (b.dtype == 0)
             ge ? RUN(0, true) : RUN(0, false);
         else
             ge ? RUN(1, true) : RUN(1, false);
 #undef RUN
+        sum.out = nullptr;
     }
     return launched();
+}
+
+int launch_token_logprob_backward(const TokenRows &b, const float *stats, const float *entropy, const float *grad_logp,
+                                  const float *grad_entropy, void *grad, int64_t ld_grad, hipStream_t stream)
+{
+    return run_backward(b, stats, entropy, grad_logp, grad_entropy, grad, ld_grad, WeightedSum{nullptr, nullptr, 0.0, 0, nullptr}, stream);
 }
 
 template <int DT, bool ENT>
@@ -637,19 +653,21 @@ int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOu
         else
             ent ? run_policy<1, true>(b, p, o, stream) : run_policy<1, false>(b, p, o, stream);
     }
-    weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(o.token_loss, p.weights, b.N ? 1.0 / (double)b.N : 0.0, b.N, o.loss);
+    weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(WeightedSum{o.token_loss, p.weights, b.N ? 1.0 / (double)b.N : 0.0, b.N, o.loss});
     return launched();
 }
 
 int launch_preference_loss(const TokenRows &b, const PreferenceParams &p, const PreferenceOutputs &o, hipStream_t stream)
 {
     const int64_t pairs = p.S / 2;
-    if (b.N > 0 && launch_token_logprob(b, p.mask, o.row, stream)) return 1;
-    if (o.grad && b.N > 0)
-        zero_outside_kernel<<<dim3((unsigned)((b.N + kBlock - 1) / kBlock)), dim3(kBlock), 0, stream>>>(b.N, p.seq_offsets, p.S, o.grad_logp);
+    const bool back = o.grad && b.N > 0;
+    LogProbOutputs row = o.row;
+    row.zero = back ? o.grad_logp : nullptr;  // rows outside all sequences keep that
+    if (b.N > 0 && launch_token_logprob(b, p.mask, row, stream)) return 1;
     if (pairs > 0) pair_kernel<<<dim3((unsigned)pairs), dim3(kBlock), 0, stream>>>(b.N, p, o);
-    weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(o.pair_loss, p.pair_weights, pairs ? 1.0 / (double)pairs : 0.0, pairs, o.loss);
-    if (o.grad && b.N > 0) return launch_token_logprob_backward(b, o.row.stats, nullptr, o.grad_logp, nullptr, o.grad, o.ld_grad, stream);
+    const WeightedSum sum{o.pair_loss, p.pair_weights, pairs ? 1.0 / (double)pairs : 0.0, pairs, o.loss};
+    if (back) return run_backward(b, o.row.stats, nullptr, o.grad_logp, nullptr, o.grad, o.ld_grad, sum, stream);
+    weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(sum);
     return launched();
 }
 

@@ -20,6 +20,7 @@ struct LogProbOutputs {
     float *stats;    // [N][2] reference logit, sum of exp((x - reference) / T); or null
     float *entropy;  // or null
     uint8_t *flags;
+    float *zero = nullptr;  // [N] written 0, or null
 };
 
 struct PolicyParams {
