@@ -479,6 +479,10 @@ int difr_seq_reduce(const float *scores, const uint8_t *row_flags, const int64_t
  * Gradients are written in the logits' type, rounded once; `grad` is [N, V] with row pitch ld_grad >= V and may be the logits
  * themselves (same address and pitch): the row is read before it is overwritten.  Any other overlap gives wrong results.
  * Sums of a row are formed in fp32 per thread and in fp64 from there on, in a fixed order; everything per row is fp64.
+ *
+ * workspace  DEVICE scratch of at least difr_token_workspace_bytes(N, V, dtype) bytes (host only, no device needed), 8-byte aligned,
+ * contents irrelevant before and after; calls that overlap in time need distinct workspaces.  Few long rows are shared among several
+ * workgroups whose sums it holds; 0: none is needed and NULL will do.  Too small: DIFR_ERR_SHAPE.
  */
 typedef struct {
     const void *logits;        /* as in difr_rows: [N, ld], base aligned to the element size */
@@ -496,7 +500,9 @@ typedef struct {
  * flags    [N]
  * One pass over the logits.
  */
-int difr_token_logprob(const difr_token_rows *in, float *logp, float *stats, float *entropy, uint8_t *flags, void *hip_stream);
+size_t difr_token_workspace_bytes(int64_t N, int64_t V, int32_t dtype);
+int difr_token_logprob(const difr_token_rows *in, float *logp, float *stats, float *entropy, uint8_t *flags, void *workspace,
+                       size_t workspace_bytes, void *hip_stream);
 
 /*
  * The gradient in the logits of a loss whose gradients in logp and entropy are grad_logp [N] and grad_entropy [N] (or NULL: none):
@@ -529,7 +535,7 @@ typedef struct {
 } difr_policy;
 
 int difr_policy_loss(const difr_token_rows *in, const difr_policy *p, float *loss, float *token_loss, float *logp, float *entropy,
-                     float *kl, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream);
+                     float *kl, uint8_t *flags, void *grad, int64_t ld_grad, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Preference loss over pairs of replies.  Rows of sequence s are [seq_offsets[s], seq_offsets[s + 1]) as in difr_seq_reduce;
@@ -555,7 +561,8 @@ typedef struct {
 } difr_preference;
 
 int difr_preference_loss(const difr_token_rows *in, const difr_preference *p, float *loss, float *pair_loss, float *seq_logp,
-                         float *logp, float *stats, float *grad_logp, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream);
+                         float *logp, float *stats, float *grad_logp, uint8_t *flags, void *grad, int64_t ld_grad, void *workspace,
+                         size_t workspace_bytes, void *hip_stream);
 
 /*
  * Microscaled 4-bit floating point, for LM heads that are served in it: a verifier that is to reproduce such a server's logits has to

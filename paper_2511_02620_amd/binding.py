@@ -102,7 +102,7 @@ class _Preference(C.Structure):
 
 
 EXPORTS = ("difr_gumbel_score", "difr_debug_gumbel_score_unfiltered", "difr_ipt_score", "difr_score_both", "difr_score_both_peaked", "difr_score_both_admissible", "difr_admissible_count", "difr_gumbel_likelihood", "difr_ipt_score_filtered", "difr_score_both_filtered", "difr_lmhead_score", "difr_lmhead_score_static", "difr_lmhead_workspace_bytes", "difr_split_workspace_bytes", "difr_score_split", "difr_classify", "difr_seq_reduce",
-           "difr_token_logprob", "difr_token_logprob_backward", "difr_policy_loss", "difr_preference_loss", "difr_mx4_padded",
+           "difr_token_workspace_bytes", "difr_token_logprob", "difr_token_logprob_backward", "difr_policy_loss", "difr_preference_loss", "difr_mx4_padded",
            "difr_mx4_quantize", "difr_mx4_dequantize", "difr_mx4_product_workspace_bytes", "difr_mx4_product", "difr_debug_noise", "difr_debug_gumbel_map",
            "difr_philox4x32_10", "difr_status_string", "difr_version")
 
@@ -157,10 +157,12 @@ def load_library():
     lib.difr_ipt_score.restype = C.c_int
     lib.difr_seq_reduce.argtypes = [vp, vp, vp, C.c_int64, C.c_int64, C.c_float, vp, vp, vp, vp, vp]
     lib.difr_seq_reduce.restype = C.c_int
-    lib.difr_token_logprob.argtypes = [C.POINTER(_TokenRows)] + [vp] * 5
+    lib.difr_token_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int32]
+    lib.difr_token_workspace_bytes.restype = C.c_size_t
+    lib.difr_token_logprob.argtypes = [C.POINTER(_TokenRows)] + [vp] * 5 + [C.c_size_t, vp]
     lib.difr_token_logprob_backward.argtypes = [C.POINTER(_TokenRows)] + [vp] * 5 + [C.c_int64, vp]
-    lib.difr_policy_loss.argtypes = [C.POINTER(_TokenRows), C.POINTER(_Policy)] + [vp] * 7 + [C.c_int64, vp]
-    lib.difr_preference_loss.argtypes = [C.POINTER(_TokenRows), C.POINTER(_Preference)] + [vp] * 8 + [C.c_int64, vp]
+    lib.difr_policy_loss.argtypes = [C.POINTER(_TokenRows), C.POINTER(_Policy)] + [vp] * 7 + [C.c_int64, vp, C.c_size_t, vp]
+    lib.difr_preference_loss.argtypes = [C.POINTER(_TokenRows), C.POINTER(_Preference)] + [vp] * 8 + [C.c_int64, vp, C.c_size_t, vp]
     lib.difr_mx4_padded.argtypes = [C.c_int64]
     lib.difr_mx4_padded.restype = C.c_int64
     lib.difr_mx4_quantize.argtypes = [vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, vp, vp, vp]

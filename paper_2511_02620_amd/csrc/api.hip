@@ -475,15 +475,30 @@ int difr_classify(const float *scores, const int32_t *ranks, int64_t N, float ta
                : DIFR_OK;
 }
 
-int difr_token_logprob(const difr_token_rows *in, float *logp, float *stats, float *entropy, uint8_t *flags, void *hip_stream)
+size_t difr_token_workspace_bytes(int64_t N, int64_t V, int32_t dtype)
+{
+    return N < 1 || V < 1 || (dtype != DIFR_BF16 && dtype != DIFR_F32) ? 0 : difr::token_workspace_bytes(N, V, dtype);
+}
+
+static int check_token_workspace(const difr::TokenRows &b, const void *workspace, size_t workspace_bytes)
+{
+    const size_t need = difr::token_workspace_bytes(b.N, b.V, b.dtype);
+    if (workspace_bytes < need) return DIFR_ERR_SHAPE;
+    if (need && !workspace) return DIFR_ERR_NULL;
+    return need && (uintptr_t)workspace % 8u ? DIFR_ERR_ALIGN : DIFR_OK;
+}
+
+int difr_token_logprob(const difr_token_rows *in, float *logp, float *stats, float *entropy, uint8_t *flags, void *workspace,
+                       size_t workspace_bytes, void *hip_stream)
 {
     difr::TokenRows b;
     int rc = validate_token_rows(in, &b);
     if (rc != DIFR_OK) return rc;
     if (b.N == 0) return DIFR_OK;
     if (!logp || !flags) return DIFR_ERR_NULL;
+    if ((rc = check_token_workspace(b, workspace, workspace_bytes)) != DIFR_OK) return rc;
     if ((rc = check_device()) != DIFR_OK) return rc;
-    return difr::launch_token_logprob(b, nullptr, difr::LogProbOutputs{logp, stats, entropy, flags}, (hipStream_t)hip_stream)
+    return difr::launch_token_logprob(b, nullptr, difr::LogProbOutputs{logp, stats, entropy, flags}, workspace, (hipStream_t)hip_stream)
                ? DIFR_ERR_LAUNCH
                : DIFR_OK;
 }
@@ -504,7 +519,7 @@ int difr_token_logprob_backward(const difr_token_rows *in, const float *stats, c
 }
 
 int difr_policy_loss(const difr_token_rows *in, const difr_policy *p, float *loss, float *token_loss, float *logp, float *entropy,
-                     float *kl, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream)
+                     float *kl, uint8_t *flags, void *grad, int64_t ld_grad, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     difr::TokenRows b;
     int rc = validate_token_rows(in, &b);
@@ -517,14 +532,16 @@ int difr_policy_loss(const difr_token_rows *in, const difr_policy *p, float *los
         if (!p->advantages || !token_loss || !logp || !flags) return DIFR_ERR_NULL;
         if (grad && (rc = validate_grad(b, grad, ld_grad)) != DIFR_OK) return rc;
     }
+    if ((rc = check_token_workspace(b, workspace, workspace_bytes)) != DIFR_OK) return rc;
     if ((rc = check_device()) != DIFR_OK) return rc;
     const difr::PolicyParams q{p->advantages, p->weights, p->old_logp, p->ref_logp, p->clip_low, p->clip_high, p->kl_coef, p->entropy_coef};
     const difr::PolicyOutputs o{loss, token_loss, {logp, nullptr, entropy, flags}, kl, grad, ld_grad};
-    return difr::launch_policy_loss(b, q, o, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+    return difr::launch_policy_loss(b, q, o, workspace, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
 }
 
 int difr_preference_loss(const difr_token_rows *in, const difr_preference *p, float *loss, float *pair_loss, float *seq_logp,
-                         float *logp, float *stats, float *grad_logp, uint8_t *flags, void *grad, int64_t ld_grad, void *hip_stream)
+                         float *logp, float *stats, float *grad_logp, uint8_t *flags, void *grad, int64_t ld_grad, void *workspace,
+                         size_t workspace_bytes, void *hip_stream)
 {
     difr::TokenRows b;
     int rc = validate_token_rows(in, &b);
@@ -538,11 +555,12 @@ int difr_preference_loss(const difr_token_rows *in, const difr_preference *p, fl
         if (grad && (!stats || !grad_logp)) return DIFR_ERR_NULL;
         if (grad && (rc = validate_grad(b, grad, ld_grad)) != DIFR_OK) return rc;
     }
+    if ((rc = check_token_workspace(b, workspace, workspace_bytes)) != DIFR_OK) return rc;
     if ((rc = check_device()) != DIFR_OK) return rc;
     const difr::PreferenceParams q{p->seq_offsets, p->S, p->mask, p->ref_seq_logp, p->pair_weights, p->beta, p->label_smoothing, p->margin,
                                    p->average != 0};
     const difr::PreferenceOutputs o{loss, pair_loss, seq_logp, {logp, stats, nullptr, flags}, grad ? grad_logp : nullptr, grad, ld_grad};
-    return difr::launch_preference_loss(b, q, o, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+    return difr::launch_preference_loss(b, q, o, workspace, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
 }
 
 int64_t difr_mx4_padded(int64_t d) { return d <= 0 ? 0 : (d + difr::kMxSlab - 1) / difr::kMxSlab * difr::kMxSlab; }

@@ -42,6 +42,7 @@ namespace {
     X(difr_lmhead_score)                                                                                                \
     X(difr_seq_reduce)                                                                                                  \
     X(difr_classify)                                                                                                    \
+    X(difr_token_workspace_bytes)                                                                                       \
     X(difr_token_logprob)                                                                                               \
     X(difr_token_logprob_backward)                                                                                      \
     X(difr_policy_loss)                                                                                                 \
@@ -593,6 +594,19 @@ struct Grad {
     }
 };
 
+// The workspace of a call on token rows.
+struct Scratch {
+    at::Tensor t;
+    void *data = nullptr;
+    size_t bytes;
+    Scratch(const TokenRows &r, Outputs &o) : bytes(lib.difr_token_workspace_bytes(r.in.N, r.in.V, r.in.dtype))
+    {
+        if (!bytes) return;
+        t = o.make(at::kByte, {(int64_t)bytes});
+        data = t.data_ptr();
+    }
+};
+
 // token rows, want_entropy
 PyObject *token_logprob(PyObject *const *a)
 {
@@ -602,7 +616,8 @@ PyObject *token_logprob(PyObject *const *a)
     float *stats = (float *)o.add(key::stats, at::kFloat, {r.N, 2});
     float *entropy = truth(a[kTokenRowArgs]) ? o.f32(key::entropy, r.N) : nullptr;
     uint8_t *flags = o.u8(key::flags, r.N);
-    return one(enter(r.dev, [&](void *s) { return lib.difr_token_logprob(&r.in, logp, stats, entropy, flags, s); }), o);
+    const Scratch w(r, o);
+    return one(enter(r.dev, [&](void *s) { return lib.difr_token_logprob(&r.in, logp, stats, entropy, flags, w.data, w.bytes, s); }), o);
 }
 
 // token rows, stats, grad_logp, entropy, grad_entropy, out
@@ -647,8 +662,9 @@ PyObject *policy_loss(PyObject *const *a)
         g.into(o);
     }
     if (!r.N) grad = nullptr;
+    const Scratch w(r, o);
     return one(enter(r.dev, [&](void *s) {
-                   return lib.difr_policy_loss(&r.in, &p, loss, token_loss, logp, entropy, kl, flags, grad, ld, s);
+                   return lib.difr_policy_loss(&r.in, &p, loss, token_loss, logp, entropy, kl, flags, grad, ld, w.data, w.bytes, s);
                }), o);
 }
 
@@ -680,8 +696,10 @@ PyObject *preference_loss(PyObject *const *a)
         g.into(o);
     }
     if (!r.N) grad = nullptr;
+    const Scratch w(r, o);
     return one(enter(r.dev, [&](void *s) {
-                   return lib.difr_preference_loss(&r.in, &p, loss, pair_loss, seq_logp, logp, stats, grad_logp, flags, grad, ld, s);
+                   return lib.difr_preference_loss(&r.in, &p, loss, pair_loss, seq_logp, logp, stats, grad_logp, flags, grad, ld, w.data,
+                                                   w.bytes, s);
                }), o);
 }
 

@@ -93,7 +93,28 @@ struct RowSums {
     double S, A;
 };
 
-// The waves' sums in a fixed order, for the lanes of the first wave (the others get nothing of use).  lds: 3 floats for each wave.
+// Sums that LANES neighbouring lanes hold, joined in a fixed order for all of them.
+template <int LANES, bool ENT>
+__device__ __forceinline__ RowSums join_sums(RowSums s, float c)
+{
+    RowSums r = s;
+#pragma unroll
+    for (int off = LANES / 2; off >= 1; off >>= 1) r.ref = fmaxf(r.ref, __shfl_xor(r.ref, off, 64));
+    if (__builtin_amdgcn_ballot_w64(s.ref != r.ref) != 0ull) {
+        const double d = s.ref == kNoLogit ? 0.0 : fmax(((double)s.ref - (double)r.ref) * (double)c, -1000.0);
+        const double k = rint(d), f = ldexp((double)fast_exp2((float)(d - k)), (int)k);  // (sums without a reference are 0)
+        r.A = f * (s.A + d * s.S);
+        r.S = f * s.S;
+    }
+#pragma unroll
+    for (int off = LANES / 2; off >= 1; off >>= 1) {
+        r.S += __shfl_xor(r.S, off, 64);
+        if (ENT) r.A += __shfl_xor(r.A, off, 64);
+    }
+    return r;
+}
+
+// The waves' sums, for the lanes of the first wave (the others get nothing of use).  lds: 3 floats for each wave.
 template <int THREADS, int DT, bool ENT>
 __device__ __forceinline__ RowSums merge_sums(const SoftmaxSums<DT, ENT> &w, float *lds)
 {
@@ -106,26 +127,9 @@ __device__ __forceinline__ RowSums merge_sums(const SoftmaxSums<DT, ENT> &w, flo
         lds[3 * wave + 2] = A;
     }
     __syncthreads();
-    RowSums r{kNoLogit, 0.0, 0.0};
-    if (wave != 0) return r;
+    if (wave != 0) return RowSums{kNoLogit, 0.0, 0.0};
     const int i = threadIdx.x & (W - 1);  // a lane for each wave's sums, and copies of them
-    const float from = lds[3 * i];
-    r.ref = from;
-#pragma unroll
-    for (int off = W / 2; off >= 1; off >>= 1) r.ref = fmaxf(r.ref, __shfl_xor(r.ref, off, 64));
-    r.S = lds[3 * i + 1], r.A = lds[3 * i + 2];
-    if (__builtin_amdgcn_ballot_w64(from != r.ref) != 0ull) {
-        const double d = from == kNoLogit ? 0.0 : fmax(((double)from - (double)r.ref) * (double)w.c, -1000.0);
-        const double k = rint(d), f = ldexp((double)fast_exp2((float)(d - k)), (int)k);  // (a wave without a reference has seen nothing)
-        r.A = f * (r.A + d * r.S);
-        r.S *= f;
-    }
-#pragma unroll
-    for (int off = W / 2; off >= 1; off >>= 1) {
-        r.S += __shfl_xor(r.S, off, 64);
-        if (ENT) r.A += __shfl_xor(r.A, off, 64);
-    }
-    return r;
+    return join_sums<W, ENT>(RowSums{lds[3 * i], lds[3 * i + 1], lds[3 * i + 2]}, w.c);
 }
 
 // Functions of 64-bit arguments to 1e-7 of the value (of 1, for the logarithm): the part that is a power of two is taken off in 64

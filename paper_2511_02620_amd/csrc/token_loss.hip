@@ -112,6 +112,25 @@ __device__ __forceinline__ bool read_past(const TokenRows &b, int64_t row)
     return (b.N - 1 - row) * b.ld * (b.dtype == 0 ? 2 : 4) > ((int64_t)192 << 20);
 }
 
+__device__ __forceinline__ void logprob_store(const LogProbOutputs &o, int64_t row, const TokenRow &r, const RowSums &s, float x_t)
+{
+    const RowResult q = row_result(r, s, x_t);
+    o.logp[row] = (float)q.logp;
+    if (o.stats) {
+        o.stats[2 * row] = s.ref;
+        o.stats[2 * row + 1] = (float)s.S;
+    }
+    if (o.entropy) o.entropy[row] = (float)q.H;
+    o.flags[row] = (uint8_t)q.flags;
+}
+__device__ __forceinline__ void logprob_left_out(const LogProbOutputs &o, int64_t row)
+{
+    o.logp[row] = 0.0f;
+    if (o.stats) o.stats[2 * row] = o.stats[2 * row + 1] = 0.0f;
+    if (o.entropy) o.entropy[row] = 0.0f;
+    o.flags[row] = 0;
+}
+
 template <int DT, int THREADS, bool ENT>
 __global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, const uint8_t *mask, LogProbOutputs o)
 {
@@ -121,27 +140,92 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, con
     const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
     if (o.zero && threadIdx.x == 0) o.zero[row] = 0.0f;
     if (mask && mask[row] == 0) {
-        if (threadIdx.x == 0) {
-            o.logp[row] = 0.0f;
-            if (o.stats) o.stats[2 * row] = o.stats[2 * row + 1] = 0.0f;
-            if (o.entropy) o.entropy[row] = 0.0f;
-            o.flags[row] = 0;
-        }
+        if (threadIdx.x == 0) logprob_left_out(o, row);
         return;
     }
     const TokenRow r = load_token_row(b, row);
     const float x_t = r.token_ok ? Elem<DT>::to_float(x[r.t]) : 0.0f;
     const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, read_past(b, row), lds);
-    if (threadIdx.x == 0) {
-        const RowResult q = row_result(r, s, x_t);
-        o.logp[row] = (float)q.logp;
-        if (o.stats) {
-            o.stats[2 * row] = s.ref;
-            o.stats[2 * row + 1] = (float)s.S;
+    if (threadIdx.x == 0) logprob_store(o, row, r, s, x_t);
+}
+
+// ---- few long rows: a row's sums by several workgroups ----
+
+// A workgroup for every four rounds of a workgroup over the row, 64 to a row and 1024 in all at the most.  Two rounds and 2048, eight and
+// 1024, eight and 512 are as fast where it counts.
+constexpr int kPartRounds = 4, kMostParts = 64, kMostPartBlocks = 1024;
+struct SplitRows {
+    RowSums *sums;  // [N][parts]
+    float *stats, *entropy, *grad_logp, *grad_entropy;  // [N][2], [N]: for the gradient of the policy loss
+    int parts;
+};
+
+// One workgroup of `parts` to a row: the sums of its stretch, for a second kernel.  Rows that mask or weights leave out are not read.
+template <int DT, bool ENT>
+__global__ __launch_bounds__(kBlock) void row_part_kernel(TokenRows b, const uint8_t *mask, const float *weights, RowSums *sums, int parts)
+{
+    constexpr int E = Elem<DT>::kPerVec, U = 4;
+    typedef typename Elem<DT>::type elem;
+    __shared__ float lds_first[kWaves], lds[3 * kWaves];
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x / parts;
+    const int part = blockIdx.x % parts;
+    if ((mask && mask[row] == 0) || (weights && uniform_load(weights, row) == 0.0f)) return;
+    const int64_t nvec = b.V / E, begin = nvec * part / parts, end = nvec * (part + 1) / parts;
+    const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld + begin * E;
+    const int64_t len = part + 1 == parts ? b.V - begin * E : (end - begin) * E, total = (len + E - 1) / E;
+    const float T = b.temperatures ? uniform_load(b.temperatures, row) : b.temperature;
+    SoftmaxSums<DT, ENT> s;
+    for (int64_t i = 0; i < total; i += U * kBlock) {
+        u32x4 q[U];
+        if ((i + U * kBlock) * E <= len) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) q[u] = *reinterpret_cast<const u32x4_any *>(x + (i + u * kBlock + tid) * E);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) q[u] = row_vector<DT>(x, i + u * kBlock + tid, len);
         }
-        if (o.entropy) o.entropy[row] = (float)q.H;
-        o.flags[row] = (uint8_t)q.flags;
+        float y[E];
+        if (i == 0) {
+            unpack_vector<DT>(q[0], y);
+            const float m = wave_max(vector_max<DT>(y));
+            if ((tid & 63) == 0) lds_first[tid >> 6] = m;
+            __syncthreads();
+            s.begin(fmaxf(fmaxf(lds_first[0], lds_first[1]), fmaxf(lds_first[2], lds_first[3])), T > 0.0f && T < __builtin_inff() ? kLog2e / T : __builtin_nanf(""));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u * kBlock < total) {
+                unpack_vector<DT>(q[u], y);
+                s.add(y);
+            }
     }
+    const RowSums r = merge_sums<kBlock>(s, lds);
+    if (tid == 0) sums[blockIdx.x] = r;
+}
+
+// The sums of a row's parts (64 or fewer), for all lanes of a wave.
+template <bool ENT>
+__device__ __forceinline__ RowSums joined(const RowSums *sums, int parts, int64_t row, float c)
+{
+    const int lane = threadIdx.x;
+    return join_sums<64, ENT>(lane < parts ? sums[row * parts + lane] : RowSums{kNoLogit, 0.0, 0.0}, c);
+}
+
+template <int DT, bool ENT>
+__global__ __launch_bounds__(64) void logprob_join_kernel(TokenRows b, const uint8_t *mask, LogProbOutputs o, const RowSums *sums, int parts)
+{
+    const int64_t row = blockIdx.x;
+    const bool left_out = mask && mask[row] == 0;
+    const TokenRow r = load_token_row(b, row);
+    const float x_t = r.token_ok && !left_out ? Elem<DT>::to_float(reinterpret_cast<const typename Elem<DT>::type *>(b.logits)[row * b.ld + r.t]) : 0.0f;
+    const RowSums s = joined<ENT>(sums, parts, row, r.c);
+    if (threadIdx.x != 0) return;
+    if (o.zero) o.zero[row] = 0.0f;
+    if (left_out)
+        logprob_left_out(o, row);
+    else
+        logprob_store(o, row, r, s, x_t);
 }
 
 // sum_n weight[n] value[n] by one workgroup, in 64 bits and a fixed order.  A weight of 0 leaves its value out.
@@ -271,16 +355,21 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyParams &p, int64_t r
 }
 
 // What one wave makes of a row's sums: its outputs, and the coefficients of its gradient.
-__device__ __forceinline__ RowGrad policy_finish(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, int64_t row, const TokenRow &r,
-                                                 const RowSums &s, float x_t, double w)
+__device__ __forceinline__ PolicyRow policy_store(const PolicyParams &p, const PolicyOutputs &o, int64_t row, const RowResult &q)
 {
-    const RowResult q = row_result(r, s, x_t);
     const PolicyRow l = policy_row(p, row, q.logp, q.H);
     o.row.logp[row] = (float)q.logp;
     o.token_loss[row] = (float)l.loss;
     if (o.row.entropy) o.row.entropy[row] = (float)q.H;
     if (o.kl) o.kl[row] = (float)l.kl;
     o.row.flags[row] = (uint8_t)(q.flags | l.flags);
+    return l;
+}
+__device__ __forceinline__ RowGrad policy_finish(const PolicyParams &p, const PolicyOutputs &o, int64_t row, const TokenRow &r, const RowSums &s,
+                                                 float x_t, double w)
+{
+    const RowResult q = row_result(r, s, x_t);
+    const PolicyRow l = policy_store(p, o, row, q);
     RowGrad k;
     k.set(s.ref, r.c, s.S, (double)r.T, w * l.a, -p.entropy_coef * w, q.H, q.logp);
     return k;
@@ -292,6 +381,31 @@ __device__ __forceinline__ void policy_left_out(const PolicyOutputs &o, int64_t 
     if (o.row.entropy) o.row.entropy[row] = 0.0f;
     if (o.kl) o.kl[row] = 0.0f;
     o.row.flags[row] = 0;
+}
+
+// The same for rows whose sums several workgroups have formed, with what token_grad_kernel needs.
+template <int DT, bool ENT>
+__global__ __launch_bounds__(64) void policy_join_kernel(TokenRows b, PolicyParams p, PolicyOutputs o, SplitRows ws)
+{
+    const int64_t row = blockIdx.x;
+    const double w = p.weights ? (double)uniform_load(p.weights, row) : 1.0 / (double)b.N;
+    const TokenRow r = load_token_row(b, row);
+    const float x_t = r.token_ok && w != 0.0 ? Elem<DT>::to_float(reinterpret_cast<const typename Elem<DT>::type *>(b.logits)[row * b.ld + r.t]) : 0.0f;
+    const RowSums s = joined<ENT>(ws.sums, ws.parts, row, r.c);
+    if (threadIdx.x != 0) return;
+    float a = 0.0f, h = 0.0f;
+    if (w == 0.0) {
+        policy_left_out(o, row);
+    } else {
+        const RowResult q = row_result(r, s, x_t);
+        a = (float)(w * policy_store(p, o, row, q).a);
+        h = (float)(-p.entropy_coef * w);
+        ws.stats[2 * row] = s.ref;
+        ws.stats[2 * row + 1] = (float)s.S;
+        ws.entropy[row] = (float)q.H;
+    }
+    ws.grad_logp[row] = a;
+    ws.grad_entropy[row] = h;
 }
 
 template <int DT, int THREADS>
@@ -415,7 +529,7 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
             s.add(y);
         }
         const RowSums sums = merge_sums<THREADS>(s, lds);
-        if (tid == 0) lds_grad = policy_finish(b, p, o, row, t, sums, Elem<DT>::to_float(x_t), every ? share : (double)w);
+        if (tid == 0) lds_grad = policy_finish(p, o, row, t, sums, Elem<DT>::to_float(x_t), every ? share : (double)w);
         float w_next = 0.0f;
         const int64_t next = next_live(row + step, w_next);
         __syncthreads();
@@ -478,7 +592,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THRE
     const TokenRow r = load_token_row(b, row);
     const float x_t = r.token_ok ? Elem<DT>::to_float(x[r.t]) : 0.0f;
     const RowSums s = row_sums<DT, THREADS, ENT>(x, b.V, r.c, !o.grad && read_past(b, row), lds);
-    if (threadIdx.x == 0) lds_grad = policy_finish(b, p, o, row, r, s, x_t, w);
+    if (threadIdx.x == 0) lds_grad = policy_finish(p, o, row, r, s, x_t, w);
     if (!o.grad) return;
     __syncthreads();
     const RowGrad k = lds_grad;
@@ -560,22 +674,60 @@ __global__ __launch_bounds__(kBlock) void pair_kernel(int64_t N, PreferenceParam
 
 static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 
-template <int DT, bool ENT>
-static void run_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, hipStream_t stream)
+// How many workgroups share a row.  One compute unit takes 10 us and more for the exponentials of a long row, two launches and a workspace
+// cost 4 us of the host's time and 2 of the device's.  One workgroup a row / several, us a call (in a captured graph), log-probability
+// with the entropy, policy loss with its gradient, bf16:  24 x 151,936 14.1 / 10.5 (13.7 / 8.3), 23.8 / 15.5 (23.2 / 12.4);  24 x 100,000
+// 10.8 / 10.6 (10.6 / 8.0), 18.2 / 15.5 (17.9 / 12.1);  64 x 151,936 14.3 / 11.1 (13.7 / 9.7), 24.5 / 19.1 (23.4 / 18.1);  128 x 151,936
+// 15.9 / 14.6, 28.0 / 28.0;  128 x 100,000 11.7 / 12.4, 20.2 / 22.7;  24 x 65,536 8.4 / 10.8 (8.1 / 6.8), 15.0 / 16.0 (14.5 / 10.7).
+int token_parts(int64_t N, int64_t V, int dtype)
 {
-    // Few long rows: all of a compute unit's threads that a workgroup can have for one.  (24 rows of 151,936 bf16 logits: 17 / 10 us a call)
-    if (b.N <= 512 && b.V >= 16384)
-        token_logprob_kernel<DT, 1024, ENT><<<dim3((unsigned)b.N), dim3(1024), 0, stream>>>(b, mask, o);
-    else
-        token_logprob_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, mask, o);
+    if (N < 1 || N > 64 || V < 98304) return 1;
+    const int64_t rounds = V / ((dtype == 0 ? 8 : 4) * kBlock);  // of a workgroup over a row
+    int64_t parts = rounds / kPartRounds;
+    if (parts > kMostParts) parts = kMostParts;
+    return (int)(parts * N > kMostPartBlocks ? kMostPartBlocks / N : parts);
 }
 
-int launch_token_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, hipStream_t stream)
+size_t token_workspace_bytes(int64_t N, int64_t V, int dtype)
 {
+    const int parts = token_parts(N, V, dtype);
+    return parts < 2 ? 0 : (size_t)N * (parts * sizeof(RowSums) + 5 * sizeof(float));
+}
+
+static SplitRows split_rows(const TokenRows &b, void *workspace)
+{
+    SplitRows ws;
+    ws.parts = token_parts(b.N, b.V, b.dtype);
+    ws.sums = (RowSums *)workspace;
+    ws.stats = (float *)(ws.sums + b.N * ws.parts);
+    ws.entropy = ws.stats + 2 * b.N;
+    ws.grad_logp = ws.entropy + b.N;
+    ws.grad_entropy = ws.grad_logp + b.N;
+    return ws;
+}
+
+template <int DT, bool ENT>
+static void run_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, const SplitRows &ws, hipStream_t stream)
+{
+    if (ws.parts > 1) {
+        row_part_kernel<DT, ENT><<<dim3((unsigned)(b.N * ws.parts)), dim3(kBlock), 0, stream>>>(b, mask, nullptr, ws.sums, ws.parts);
+        logprob_join_kernel<DT, ENT><<<dim3((unsigned)b.N), dim3(64), 0, stream>>>(b, mask, o, ws.sums, ws.parts);
+    } else if (b.N <= 512 && b.V >= 32768) {
+        // Long rows, two to a compute unit or fewer: all the threads that a workgroup can have for each.  256 / 1024 threads, us, bf16:
+        // 256 x 151,936 24.8 / 16.8, 512 x 32,000 10.0 / 9.7, 512 x 16,384 6.2 / 7.2.
+        token_logprob_kernel<DT, 1024, ENT><<<dim3((unsigned)b.N), dim3(1024), 0, stream>>>(b, mask, o);
+    } else {
+        token_logprob_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, mask, o);
+    }
+}
+
+int launch_token_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, void *workspace, hipStream_t stream)
+{
+    const SplitRows ws = split_rows(b, workspace);
     if (b.dtype == 0)
-        o.entropy ? run_logprob<0, true>(b, mask, o, stream) : run_logprob<0, false>(b, mask, o, stream);
+        o.entropy ? run_logprob<0, true>(b, mask, o, ws, stream) : run_logprob<0, false>(b, mask, o, ws, stream);
     else
-        o.entropy ? run_logprob<1, true>(b, mask, o, stream) : run_logprob<1, false>(b, mask, o, stream);
+        o.entropy ? run_logprob<1, true>(b, mask, o, ws, stream) : run_logprob<1, false>(b, mask, o, ws, stream);
     return launched();
 }
 
@@ -644,10 +796,26 @@ static void run_policy(const TokenRows &b, const PolicyParams &p, const PolicyOu
         policy_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, p, o);
 }
 
-int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, hipStream_t stream)
+template <int DT, bool ENT>
+static void run_policy_parts(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, const SplitRows &ws, hipStream_t stream)
 {
-    if (b.N > 0) {
-        const bool ent = o.row.entropy || p.entropy_coef != 0.0;
+    row_part_kernel<DT, ENT><<<dim3((unsigned)(b.N * ws.parts)), dim3(kBlock), 0, stream>>>(b, nullptr, p.weights, ws.sums, ws.parts);
+    policy_join_kernel<DT, ENT><<<dim3((unsigned)b.N), dim3(64), 0, stream>>>(b, p, o, ws);
+}
+
+int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, void *workspace, hipStream_t stream)
+{
+    const bool ent = o.row.entropy || p.entropy_coef != 0.0;
+    if (token_parts(b.N, b.V, b.dtype) > 1) {
+        const SplitRows ws = split_rows(b, workspace);
+        if (b.dtype == 0)
+            ent ? run_policy_parts<0, true>(b, p, o, ws, stream) : run_policy_parts<0, false>(b, p, o, ws, stream);
+        else
+            ent ? run_policy_parts<1, true>(b, p, o, ws, stream) : run_policy_parts<1, false>(b, p, o, ws, stream);
+        if (o.grad)
+            return run_backward(b, ws.stats, ws.entropy, ws.grad_logp, p.entropy_coef != 0.0 ? ws.grad_entropy : nullptr, o.grad, o.ld_grad,
+                                WeightedSum{o.token_loss, p.weights, 1.0 / (double)b.N, b.N, o.loss}, stream);
+    } else if (b.N > 0) {
         if (b.dtype == 0)
             ent ? run_policy<0, true>(b, p, o, stream) : run_policy<0, false>(b, p, o, stream);
         else
@@ -657,13 +825,13 @@ int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOu
     return launched();
 }
 
-int launch_preference_loss(const TokenRows &b, const PreferenceParams &p, const PreferenceOutputs &o, hipStream_t stream)
+int launch_preference_loss(const TokenRows &b, const PreferenceParams &p, const PreferenceOutputs &o, void *workspace, hipStream_t stream)
 {
     const int64_t pairs = p.S / 2;
     const bool back = o.grad && b.N > 0;
     LogProbOutputs row = o.row;
     row.zero = back ? o.grad_logp : nullptr;  // rows outside all sequences keep that
-    if (b.N > 0 && launch_token_logprob(b, p.mask, row, stream)) return 1;
+    if (b.N > 0 && launch_token_logprob(b, p.mask, row, workspace, stream)) return 1;
     if (pairs > 0) pair_kernel<<<dim3((unsigned)pairs), dim3(kBlock), 0, stream>>>(b.N, p, o);
     const WeightedSum sum{o.pair_loss, p.pair_weights, pairs ? 1.0 / (double)pairs : 0.0, pairs, o.loss};
     if (back) return run_backward(b, o.row.stats, nullptr, o.grad_logp, nullptr, o.grad, o.ld_grad, sum, stream);

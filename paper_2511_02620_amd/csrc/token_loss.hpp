@@ -53,11 +53,12 @@ struct PreferenceOutputs {
     int64_t ld_grad;
 };
 
-int launch_token_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, hipStream_t stream);
+size_t token_workspace_bytes(int64_t N, int64_t V, int dtype);
+int launch_token_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOutputs &o, void *workspace, hipStream_t stream);
 int launch_token_logprob_backward(const TokenRows &b, const float *stats, const float *entropy, const float *grad_logp,
                                   const float *grad_entropy, void *grad, int64_t ld_grad, hipStream_t stream);
-int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, hipStream_t stream);
-int launch_preference_loss(const TokenRows &b, const PreferenceParams &p, const PreferenceOutputs &o, hipStream_t stream);
+int launch_policy_loss(const TokenRows &b, const PolicyParams &p, const PolicyOutputs &o, void *workspace, hipStream_t stream);
+int launch_preference_loss(const TokenRows &b, const PreferenceParams &p, const PreferenceOutputs &o, void *workspace, hipStream_t stream);
 
 // Microscaled 4-bit floating point (mx4.hip).
 constexpr int kMxBlock = 32, kMxSlab = 128;  // elements that share a scale; rows of codes are whole slabs

@@ -34,7 +34,8 @@ def _on_device(x, offset=0, gap=0):
     return view
 
 
-SHAPES = [(1, 1), (3, 2), (2, 7), (4, 8), (5, 9), (3, 255), (4, 1000), (6, 1024), (3, 2049), (2, 8197), (3, 40001), (2, 151936), (700, 130)]
+SHAPES = [(1, 1), (3, 2), (2, 7), (4, 8), (5, 9), (3, 255), (4, 1000), (6, 1024), (3, 2049), (2, 8197), (3, 40001), (2, 151936), (700, 130),
+          (20, 100003), (64, 98304), (65, 98304)]
 
 
 @pytest.mark.parametrize("N,V", SHAPES)
@@ -67,7 +68,7 @@ def test_forward_and_backward(difr, N, V, dtype, offset, gap):
         assert torch.equal(same, got), "in place"
 
 
-@pytest.mark.parametrize("V", [17, 1024, 3001, 9000])
+@pytest.mark.parametrize("V", [17, 1024, 3001, 9000, 100003])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_masks_and_infinities(difr, V, dtype):
     x, tok, g = _logits(V, 12, V, dtype)
@@ -114,8 +115,9 @@ def test_masks_and_infinities(difr, V, dtype):
     assert got[[1, 4, 5, 10]].eq(0).all() and torch.isfinite(got[11]).all() == torch.isfinite(o["entropy"][11])
 
 
-def test_bad_temperatures_touch_their_rows_only(difr):
-    x, tok, _ = _logits(5, 5, 777, torch.bfloat16)
+@pytest.mark.parametrize("V", [777, 100003])
+def test_bad_temperatures_touch_their_rows_only(difr, V):
+    x, tok, _ = _logits(5, 5, V, torch.bfloat16)
     T = torch.tensor([1.0, 0.0, -1.0, math.nan, 2.0])
     o = difr.token_logprob(x.to(DEV), 1.0, tok.to(DEV), temperatures=T.to(DEV), want_entropy=True)
     assert torch.isnan(o["logp"]).tolist() == [False, True, True, True, False]
@@ -138,6 +140,37 @@ def test_low_and_high_temperatures(difr):
             got = difr.token_logprob_backward(x.to(DEV), T, tok.to(DEV), o["stats"], a.to(DEV))
             want = ref.gradient(lp, H, tok, Tq, a)
             ref.assert_within(got, want, ref.grad_bound(want, lp, H, Tq, a, None, dtype), "gradient")
+
+
+def test_rows_whose_parts_have_nothing_in_common(difr):
+    """Stretches of a long row that different workgroups sum, far apart in scale, without mass, or with a NaN in one entry of one."""
+    N, V = 9, 131072
+    for dtype in (torch.bfloat16, torch.float32):
+        x, tok, g = _logits(31, N, V, dtype)
+        ramp = torch.arange(V) // 4096
+        x[0] = (x[0].float() + 40.0 * ramp).to(dtype)          # each stretch far above the one before
+        x[1] = (x[1].float() - 40.0 * ramp).to(dtype)
+        x[2, : V - 3] = -INF
+        x[3, 5:] = LOWEST[dtype]
+        x[4, ::4096] = -INF
+        x[5, 70000] = math.nan
+        x[6, V - 1] = INF
+        x[7, 60000:61000] = math.nan
+        x[8, 4096:8192] = LOWEST[dtype]
+        tok[0], tok[2], tok[3] = V - 1, V - 2, 3
+        bad = torch.tensor([5, 6, 7])
+        logp, H, lp = ref.rows(x, 1.0, tok)
+        logp[bad], H[bad], lp[bad] = math.nan, math.nan, 0.0
+        o = difr.token_logprob(x.to(DEV), 1.0, tok.to(DEV), want_entropy=True)
+        assert [n for n in range(N) if o["flags"][n]] == bad.tolist()
+        ref.assert_within(o["logp"], logp, ref.logp_bound(lp, logp.nan_to_num(0, 0, 0)), "logp")
+        ref.assert_within(o["entropy"], H, 3 * ref.logp_bound(lp, lp.min(1).values.clamp(min=-60)), "entropy")
+        A = torch.randn(N, generator=g)
+        got = difr.policy_loss(x.to(DEV), 1.0, tok.to(DEV), A.to(DEV))["grad"]
+        want = ref.gradient(lp, H.nan_to_num(0), tok, 1.0, -A.double() / N)
+        lim = ref.grad_bound(want, lp, H.nan_to_num(0), 1.0, -A / N, None, dtype)
+        want[bad] = math.nan
+        ref.assert_within(got, want, lim, "gradient")
 
 
 def test_no_rows(difr):
@@ -179,7 +212,7 @@ def _policy_ref(x, T, tok, A, w, old, refl, lo, hi, beta, eta):
 
 # (rows of a workgroup's registers in all their lengths, from one vector to a compute unit's; with LDS; longer ones)
 @pytest.mark.parametrize("N,V", [(1, 1), (2, 50), (33, 1024), (5, 8197), (3, 40001), (2, 151936), (300, 515), (259, 20003), (3, 75000),
-                                 (3, 100001), (2, 165000), (2, 230001)])
+                                 (3, 100001), (2, 165000), (2, 230001), (66, 100001), (66, 151936), (64, 98304)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("old,refl,weights,eta", [(1, 1, 1, 0.0), (1, 1, 1, 0.02), (0, 0, 0, 0.0), (1, 0, 1, 0.01), (0, 1, 0, 0.0)])
 def test_policy_loss(difr, N, V, dtype, old, refl, weights, eta):
@@ -291,7 +324,7 @@ def _pairs_ref(x, T, tok, off, beta, mask, refs, pw, eps, margin, average):
 
 
 @pytest.mark.parametrize("off,N", [([0, 3, 7], 7), ([2, 2, 9, 9, 20], 24), ([0, 300, 301, 301, 640, 700, 900], 900), ([0, 1, 2], 2)])
-@pytest.mark.parametrize("V", [7, 1024, 20011])
+@pytest.mark.parametrize("V", [7, 1024, 20011, 100003])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("masked,refs,weights,eps,margin,average", [(1, 1, 1, 0.1, 0.5, 0), (0, 0, 0, 0.0, 0.0, 0), (1, 1, 0, 1.0, 0.0, 1),
                                                                     (1, 0, 1, 0.0, 1.0, 1)])
@@ -389,8 +422,9 @@ def test_gradients_are_the_slopes(difr):
 
 # ---- streams, graphs ----
 
-def test_other_streams_and_repeats(difr):
-    x, tok, g = _logits(8, 40, 30011, torch.bfloat16)
+@pytest.mark.parametrize("V", [30011, 100003])
+def test_other_streams_and_repeats(difr, V):
+    x, tok, g = _logits(8, 40, V, torch.bfloat16)
     xd, td, A = x.to(DEV), tok.to(DEV), torch.randn(40, generator=g).to(DEV)
     first = difr.policy_loss(xd, 1.0, td, A, want_entropy=True)
     torch.cuda.synchronize()
@@ -402,8 +436,9 @@ def test_other_streams_and_repeats(difr):
         assert torch.equal(first[k], other[k]), k
 
 
-def test_a_step_is_captured_and_replayed(difr):
-    N, V, S = 48, 5003, 4
+@pytest.mark.parametrize("V", [5003, 100003])
+def test_a_step_is_captured_and_replayed(difr, V):
+    N = 48
     off = torch.tensor([0, 10, 24, 30, 48], dtype=torch.int64, device=DEV)
     xd, td = torch.zeros(N, V, dtype=torch.bfloat16, device=DEV), torch.zeros(N, dtype=torch.int32, device=DEV)
     A, w = torch.zeros(N, device=DEV), torch.zeros(N, device=DEV)

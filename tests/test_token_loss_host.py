@@ -34,17 +34,17 @@ def _pref(**kw):
 
 
 def _calls(lib):
-    def logprob(r, logp=FAKE, flags=FAKE):
-        return lib.difr_token_logprob(C.byref(r), logp, None, None, flags, None)
+    def logprob(r, logp=FAKE, flags=FAKE, ws=None, n=0):
+        return lib.difr_token_logprob(C.byref(r), logp, None, None, flags, ws, n, None)
 
     def backward(r, stats=FAKE, ent=None, ga=FAKE, ge=None, grad=FAKE, ld=16):
         return lib.difr_token_logprob_backward(C.byref(r), stats, ent, ga, ge, grad, ld, None)
 
-    def policy(r, p=None, loss=FAKE, each=FAKE, kl=None, flags=FAKE, grad=None, ld=16):
-        return lib.difr_policy_loss(C.byref(r), C.byref(p or _policy()), loss, each, FAKE, None, kl, flags, grad, ld, None)
+    def policy(r, p=None, loss=FAKE, each=FAKE, kl=None, flags=FAKE, grad=None, ld=16, ws=None, n=0):
+        return lib.difr_policy_loss(C.byref(r), C.byref(p or _policy()), loss, each, FAKE, None, kl, flags, grad, ld, ws, n, None)
 
-    def pref(r, p=None, loss=FAKE, pair=FAKE, stats=FAKE, flags=FAKE, grad=None, ld=16):
-        return lib.difr_preference_loss(C.byref(r), C.byref(p or _pref()), loss, pair, FAKE, FAKE, stats, FAKE, flags, grad, ld, None)
+    def pref(r, p=None, loss=FAKE, pair=FAKE, stats=FAKE, flags=FAKE, grad=None, ld=16, ws=None, n=0):
+        return lib.difr_preference_loss(C.byref(r), C.byref(p or _pref()), loss, pair, FAKE, FAKE, stats, FAKE, flags, grad, ld, ws, n, None)
 
     return logprob, backward, policy, pref
 
@@ -80,6 +80,23 @@ def test_arguments_of_each_call():
     for kw in (dict(loss=None), dict(pair=None), dict(flags=None), dict(stats=None, grad=FAKE)):
         assert pref(_rows(), **kw) == NULL, kw
     assert pref(_rows(), grad=FAKE, ld=15) == SHAPE and pref(_rows(), grad=0x1001) == ALIGN
+
+
+def test_the_workspace_of_few_long_rows():
+    lib = binding.load_library()
+    logprob, _, policy, pref = _calls(lib)
+    need = lib.difr_token_workspace_bytes
+    assert need(0, 151936, 0) == need(-1, 151936, 0) == need(4, 0, 0) == need(4, 151936, 2) == need(4, 1000, 0) == need(65, 151936, 1) == need(1 << 31, 151936, 0) == 0
+    for N in (1, 4, 64):
+        for V in (100000, 151936, 1 << 24):
+            for dtype in (0, 1):
+                n = need(N, V, dtype)
+                assert 0 < n < 1 << 20
+                r = _rows(N=N, V=V, ld=V, dtype=dtype)
+                for call in (logprob, policy, pref):
+                    assert call(r, ws=FAKE, n=n - 1) == SHAPE
+                    assert call(r, n=n) == NULL
+                    assert call(r, ws=FAKE + 4, n=n) == ALIGN
 
 
 def test_arguments_of_the_4_bit_calls():
