@@ -2,6 +2,8 @@
 // term and the preference loss over pairs of replies.  Formulas at the entry points in difr.h and in softmax_row.hpp.
 #include <math.h>
 
+#include <type_traits>
+
 #include "difr_host.hpp"
 #include "softmax_row.hpp"
 #include "token_loss.hpp"
@@ -423,13 +425,18 @@ __device__ __forceinline__ void zero_row(typename Elem<DT>::type *g, int64_t V)
 // registers, up to 17 rounds of vectors, is held in LDS, copied there by the memory system; a thread's vectors are its own there too.
 // Stores go past the caches, loads do not: the gradient is not read soon, the logits may have been written just now (8192 x 151,936 bf16,
 // us: stores through the caches 1105, past them 1045, loads too 1042; 256 rows that lie in the Infinity Cache 44, loads past it 50).
-constexpr int kLdsRounds = 17;
+// AHEAD: a row that leaves LDS free, and has the compute unit to itself, has its first rounds copied there while the row before is still
+// summed, when nothing else would ask for memory; half of the loads are out of the way then when the stores come.  us, before / with it:
+// 8192 x 151,936 bf16 1059 / 1027 (a tenth of the tokens left out: 1049 / 985), x 128,256 875 / 813, x 100,000 727 / 629, 4096 x 65,536 fp32
+// 427 / 390;  shorter rows, two to a compute unit, which cover each other's sums already: 8192 x 50,257 376 / 392, without it.
+constexpr int kLdsRounds = 17, kAheadRounds = 19;
+constexpr int wait_for(int left) { return (left & 15) | 0x0F70 | (left >> 4) << 14; }  // s_waitcnt, vector memory: until so many are left
 template <int DT, int THREADS, int R, bool ENT, bool LDS>
 __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_held_kernel(TokenRows b, PolicyParams p, PolicyOutputs o, int full,
                                                                                             int lds_rounds)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t lds_row[LDS ? kLdsRounds * THREADS * 16 : 16];
-    constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64;
+    constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64, AHEAD = LDS || R < 24 || THREADS < 512 ? 0 : R - 8 < kAheadRounds ? R - 8 : kAheadRounds;
+    __shared__ __attribute__((aligned(16))) uint8_t lds_row[LDS ? kLdsRounds * THREADS * 16 : AHEAD ? AHEAD * THREADS * 16 : 16];
     typedef typename Elem<DT>::type elem;
     __shared__ float lds_first[W], lds[3 * W];
     __shared__ RowGrad lds_grad;
@@ -451,11 +458,11 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
     };
     typedef __attribute__((address_space(1))) u32x4_any global_vector;
     auto load = [&](const elem *x, int r) { return *((const global_vector *)(round_of(x, r) + off)); };
-    // LDS round l of a row is its round R + l
+    // rounds of a row from `first` on, into LDS
     const int wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
-    auto copy_rounds = [&](const elem *x) {
-        for (int l = 0; l < lds_rounds; ++l) {
-            const char *from = reinterpret_cast<const char *>(x) + (int64_t)(R + l) * (THREADS * 16);
+    auto copy_rounds = [&](const elem *x, int first, int rounds) {
+        for (int l = 0; l < rounds; ++l) {
+            const char *from = reinterpret_cast<const char *>(x) + (int64_t)(first + l) * (THREADS * 16);
             const uint32_t to = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds_row + (uint32_t)(l * THREADS * 16 + wave_u * 1024);
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
@@ -479,7 +486,7 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
     int64_t row = next_live(blockIdx.x, w);
     if (row < b.N) {
         const elem *x = logits + row * b.ld;
-        if (LDS) copy_rounds(x);
+        if (LDS) copy_rounds(x, R, lds_rounds);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < R - 8 || r < full) q[r] = load(x, r);
@@ -515,23 +522,39 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
                 s.add(y);
             }
         }
+        auto add_rounds = [&](auto first, auto end) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r < R - 8 || r < full) {
-                float y[E];
-                unpack_vector<DT>(q[r], y);
-                s.add(y);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int r = first; r < end; ++r)
+                if (r < R - 8 || r < full) {
+                    float y[E];
+                    unpack_vector<DT>(q[r], y);
+                    s.add(y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        };
+        float w_next = 0.0f;
+        int64_t next = 0;
+        add_rounds(std::integral_constant<int, 0>(), std::integral_constant<int, AHEAD>());
+        if (AHEAD) {
+            // every load of this row has ended before the next row's copies begin, so that no wait for a load is one for them
+            __builtin_amdgcn_s_waitcnt(wait_for(0));
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (nor is a vector that they overwrite still on its way to its register)
+            next = next_live(row + step, w_next);
+            if (next < b.N) copy_rounds(logits + next * b.ld, 0, AHEAD);
+        }
+        add_rounds(std::integral_constant<int, AHEAD>(), std::integral_constant<int, R>());
         {
             float y[E];
             unpack_vector<DT>(q_end, y);
             s.add(y);
         }
         const RowSums sums = merge_sums<THREADS>(s, lds);
+        if (AHEAD) {
+            __builtin_amdgcn_s_waitcnt(wait_for(0));
+            asm volatile("" ::: "memory");
+        }
         if (tid == 0) lds_grad = policy_finish(p, o, row, t, sums, Elem<DT>::to_float(x_t), every ? share : (double)w);
-        float w_next = 0.0f;
-        const int64_t next = next_live(row + step, w_next);
+        if (!AHEAD) next = next_live(row + step, w_next);
         __syncthreads();
         const RowGrad k = lds_grad;
         elem *const g = grad + row * o.ld_grad;
@@ -549,20 +572,24 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
             for (int l = 0; l < lds_rounds; ++l)
                 __builtin_nontemporal_store(form(lds_vector(l)), (global_vector *)(round_of(g, R + l) + off));
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every vector has been read before its place is copied to
-            copy_rounds(xn);
+            copy_rounds(xn, R, lds_rounds);
         }
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r < R - 8 || r < full) {
-                __builtin_nontemporal_store(form(q[r]), (global_vector *)(round_of(g, r) + off));
-                q[r] = load(xn, r);
-                __builtin_amdgcn_sched_barrier(0);
-            }
         {
             const int64_t i = (int64_t)(full + lds_rounds) * THREADS + tid;
             if (i * E < V) store_vector<DT>(g, i, V, form(q_end));
             if (more) q_end = row_vector<DT>(xn, i, V);
         }
+        auto next_vector = [&](int r) { return r < AHEAD ? lds_vector(r) : load(xn, r); };
+        auto form_rounds = [&](auto first, auto end) {
+#pragma unroll
+            for (int r = first; r < end; ++r)
+                if (r < R - 8 || r < full) {
+                    __builtin_nontemporal_store(form(q[r]), (global_vector *)(round_of(g, r) + off));
+                    q[r] = next_vector(r);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        };
+        form_rounds(std::integral_constant<int, 0>(), std::integral_constant<int, R>());
         // the token's own entry, by the thread that has written its vector (a wave's stores to one address keep their order)
         if (t.token_ok && (t.t / E) % THREADS == tid) store_element<DT>(g + t.t, (float)k.at_token);
         row = next;

@@ -271,6 +271,36 @@ def test_policy_loss(difr, N, V, dtype, old, refl, weights, eta):
     assert o["grad"].data_ptr() == same.data_ptr() and torch.equal(same, got["grad"]), "in place"
 
 
+@pytest.mark.parametrize("V", [50000, 80003, 128256, 151936])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_policy_rows_that_follow_each_other(difr, V, dtype):
+    """Rows that a workgroup takes one after another are those of smaller batches, to the bit, whatever lies between them.  (A batch of
+    256 rows or fewer gives a row of under 39 vectors of 16 bytes to each of 256 threads more threads, which sum it in another order.)"""
+    N = 700
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.randn(N, V + 3, generator=g, device=DEV).mul_(2).to(dtype)[:, :V]
+    tok = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    A, u = torch.randn(N, generator=g, device=DEV), torch.rand(N, generator=g, device=DEV)
+    w = torch.where(u < 0.3, torch.zeros_like(u), u)
+    x[u < 0.1], w[256:259] = math.nan, 0.0
+    old = torch.full((N,), -11.0, device=DEV)
+
+    def call(rows, **kw):
+        return difr.policy_loss(x[rows], 1.0, tok[rows], A[rows], w[rows], old_logp=old[rows], ref_logp=old[rows], kl_coef=0.1, **kw)
+
+    got = call(slice(0, N))
+    assert got["grad"][w == 0].eq(0).all() and torch.isfinite(got["grad"]).all()
+    step = 175 if V * x.element_size() >= 39 * 256 * 16 else 350
+    for first in range(0, N, step):
+        rows = slice(first, first + step)
+        part = call(rows)
+        for k in ("token_loss", "logp", "kl", "flags", "grad"):
+            assert torch.equal(part[k], got[k][rows]), (first, k)
+    del part
+    again = call(slice(0, N), out=x)
+    assert torch.equal(again["grad"], got["grad"]), "in place"
+
+
 def test_policy_rows_that_cannot_be_scored_are_loud(difr):
     x, tok, g = _logits(3, 6, 900, torch.bfloat16)
     x[1, 5], tok[2], x[3, :] = math.nan, 900, -INF
