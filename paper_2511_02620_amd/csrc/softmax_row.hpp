@@ -26,12 +26,53 @@ __device__ __forceinline__ u32x4 no_logits()
     return DT == 0 ? u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u} : u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u};
 }
 
-// Vector `i` (E entries) of a row of V; past its end, no logits.
+// Vector `i` (E entries) of a row of V; past its end, no logits.  A row that ends within a vector gives its last E entries, one load as for
+// any other vector, and `row_vector_end` makes the vector of them (entry by entry they would be E loads, some of them one after another:
+// the policy loss of 8000 x 5003 bf16 takes 50 us, 55 with those).
+template <int DT>
+__device__ __forceinline__ u32x4 row_vector_at(const typename Elem<DT>::type *row, int64_t i, int64_t V)
+{
+    constexpr int E = Elem<DT>::kPerVec;
+    const int64_t base = i * E;
+    if (base >= V) return no_logits<DT>();
+    if (V < E) return load_vector<DT>(row, base, V);
+    return *reinterpret_cast<const u32x4_any *>(row + (base < V - E ? base : V - E));
+}
+template <int DT>
+__device__ __forceinline__ u32x4 row_vector_end(u32x4 q, int64_t i, int64_t V)
+{
+    constexpr int E = Elem<DT>::kPerVec, kBytes = 16 / E;
+    const int64_t over = i * E + E - V;  // entries behind the row's end
+    if (V < E || over <= 0 || over >= E) return q;
+    const uint32_t none = no_logits<DT>().x, words = (uint32_t)over * kBytes / 4, bytes = (uint32_t)over * kBytes % 4;
+    uint32_t w[5] = {q.x, q.y, q.z, q.w, none};
+    if (words & 1) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = none;
+    if (words & 2) w[0] = w[2], w[1] = w[3], w[2] = w[3] = none;
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = __builtin_amdgcn_alignbyte(w[j + 1], w[j], bytes);
+    return r;
+}
 template <int DT>
 __device__ __forceinline__ u32x4 row_vector(const typename Elem<DT>::type *row, int64_t i, int64_t V)
 {
-    const int64_t base = i * Elem<DT>::kPerVec;
-    return base < V ? load_vector<DT>(row, base, V) : no_logits<DT>();
+    return row_vector_end<DT>(row_vector_at<DT>(row, i, V), i, V);
+}
+
+// A row from the 16 bytes on that its first entry lies in: `lead` entries that are not its own, and 16-byte loads that do not straddle
+// lines (read past the caches, those are fetched twice: log-probabilities of 8192 x 99,991 bf16 327 us by such loads, 257 by these, of 8192 x
+// 50,257 159 and 127).  The 16 bytes hold an entry of the row, so they can be read.
+template <int DT>
+struct AlignedRow {
+    const typename Elem<DT>::type *x;
+    int64_t V;
+    int lead;
+};
+template <int DT>
+__device__ __forceinline__ AlignedRow<DT> aligned_row(const typename Elem<DT>::type *row, int64_t V)
+{
+    const int lead = (int)((uintptr_t)row % 16u / sizeof(typename Elem<DT>::type));
+    return AlignedRow<DT>{row - lead, V + lead, lead};
 }
 
 template <int DT>

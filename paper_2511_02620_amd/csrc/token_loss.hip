@@ -53,15 +53,15 @@ __device__ __forceinline__ RowResult row_result(const TokenRow &r, const RowSums
     return o;
 }
 
-// The row in vectors of 16 bytes, U of a thread's in flight; f(values, index of the vector) is called by whole waves.  PAST: past the
-// caches.
+// The row in vectors of 16 bytes from vector `first` on, U of a thread's in flight; f(values, index of the vector) is called by whole
+// waves.  PAST: past the caches.
 template <int DT, int THREADS, int U, bool PAST, class F>
-__device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, int64_t V, F &&f)
+__device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, int64_t first, int64_t V, F &&f)
 {
     constexpr int E = Elem<DT>::kPerVec;
     const int tid = threadIdx.x;
     const int64_t nvec = V / E, total = (V + E - 1) / E;
-    int64_t i = 0;
+    int64_t i = first;
     for (; i + (int64_t)U * THREADS <= nvec; i += (int64_t)U * THREADS) {
         u32x4 q[U];
 #pragma unroll
@@ -83,13 +83,24 @@ __device__ __forceinline__ void stream_row(const typename Elem<DT>::type *row, i
     }
 }
 
+// A thread's first vector of a row with `lead` entries before it that are not its own.
+template <int DT>
+__device__ __forceinline__ void first_vector(u32x4 q, int lead, float x[Elem<DT>::kPerVec])
+{
+    unpack_vector<DT>(q, x);
+#pragma unroll
+    for (int j = 0; j < Elem<DT>::kPerVec - 1; ++j)
+        if (threadIdx.x == 0 && j < lead) x[j] = kNoLogit;
+}
+
 // The row's sums, by all threads of the workgroup, for the first wave.
 template <int DT, int THREADS, bool ENT>
 __device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, float c, bool past, float *lds)
 {
     constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64, U = 4;
+    const AlignedRow<DT> a = aligned_row<DT>(row, V);
     float x[E];
-    unpack_vector<DT>(row_vector<DT>(row, threadIdx.x, V), x);
+    first_vector<DT>(row_vector<DT>(a.x, threadIdx.x, a.V), a.lead, x);
     const float m = wave_max(vector_max<DT>(x));
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
     __syncthreads();
@@ -99,10 +110,11 @@ __device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, 
     __syncthreads();
     SoftmaxSums<DT, ENT> s;
     s.begin(first, c);
+    s.add(x);
     if (past)
-        stream_row<DT, THREADS, U, true>(row, V, [&](const float *v, int64_t) { s.add(v); });
+        stream_row<DT, THREADS, U, true>(a.x, THREADS, a.V, [&](const float *v, int64_t) { s.add(v); });
     else
-        stream_row<DT, THREADS, U, false>(row, V, [&](const float *v, int64_t) { s.add(v); });
+        stream_row<DT, THREADS, U, false>(a.x, THREADS, a.V, [&](const float *v, int64_t) { s.add(v); });
     return merge_sums<THREADS>(s, lds);
 }
 
@@ -173,9 +185,11 @@ __global__ __launch_bounds__(kBlock) void row_part_kernel(TokenRows b, const uin
     const int64_t row = blockIdx.x / parts;
     const int part = blockIdx.x % parts;
     if ((mask && mask[row] == 0) || (weights && uniform_load(weights, row) == 0.0f)) return;
-    const int64_t nvec = b.V / E, begin = nvec * part / parts, end = nvec * (part + 1) / parts;
-    const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld + begin * E;
-    const int64_t len = part + 1 == parts ? b.V - begin * E : (end - begin) * E, total = (len + E - 1) / E;
+    const AlignedRow<DT> a = aligned_row<DT>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, b.V);
+    const int64_t nvec = a.V / E, begin = nvec * part / parts, end = nvec * (part + 1) / parts;
+    const elem *x = a.x + begin * E;
+    const int64_t len = part + 1 == parts ? a.V - begin * E : (end - begin) * E, total = (len + E - 1) / E;
+    const int lead = part == 0 ? a.lead : 0;
     const float T = b.temperatures ? uniform_load(b.temperatures, row) : b.temperature;
     SoftmaxSums<DT, ENT> s;
     for (int64_t i = 0; i < total; i += U * kBlock) {
@@ -188,15 +202,16 @@ __global__ __launch_bounds__(kBlock) void row_part_kernel(TokenRows b, const uin
             for (int u = 0; u < U; ++u) q[u] = row_vector<DT>(x, i + u * kBlock + tid, len);
         }
         float y[E];
+        first_vector<DT>(q[0], i == 0 ? lead : 0, y);
         if (i == 0) {
-            unpack_vector<DT>(q[0], y);
             const float m = wave_max(vector_max<DT>(y));
             if ((tid & 63) == 0) lds_first[tid >> 6] = m;
             __syncthreads();
             s.begin(fmaxf(fmaxf(lds_first[0], lds_first[1]), fmaxf(lds_first[2], lds_first[3])), T > 0.0f && T < __builtin_inff() ? kLog2e / T : __builtin_nanf(""));
         }
+        s.add(y);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 1; u < U; ++u)
             if (i + u * kBlock < total) {
                 unpack_vector<DT>(q[u], y);
                 s.add(y);
@@ -448,6 +463,7 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
     elem *const grad = reinterpret_cast<elem *>(o.grad);
 
     u32x4 q[R], q_end;
+    const int64_t end = (int64_t)(full + lds_rounds) * THREADS + tid;
     // a thread's vector in round r of them: a uniform address (kept from the compiler, which would carry 64-bit addresses for every
     // round in vector registers) and the same offset always
     const uint32_t off = (uint32_t)tid * 16u;
@@ -490,11 +506,12 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < R - 8 || r < full) q[r] = load(x, r);
-        q_end = row_vector<DT>(x, (int64_t)(full + lds_rounds) * THREADS + tid, V);
+        q_end = row_vector_at<DT>(x, end, V);
     }
     while (row < b.N) {
         const TokenRow t = load_token_row(b, row);
         const elem x_t = logits[row * b.ld + (t.token_ok ? t.t : 0)];
+        q_end = row_vector_end<DT>(q_end, end, V);
         // the reference, of the row's first and last entries
         {
             float y[E];
@@ -575,9 +592,8 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
             copy_rounds(xn, R, lds_rounds);
         }
         {
-            const int64_t i = (int64_t)(full + lds_rounds) * THREADS + tid;
-            if (i * E < V) store_vector<DT>(g, i, V, form(q_end));
-            if (more) q_end = row_vector<DT>(xn, i, V);
+            if (end * E < V) store_vector<DT>(g, end, V, form(q_end));
+            if (more) q_end = row_vector_at<DT>(xn, end, V);
         }
         auto next_vector = [&](int r) { return r < AHEAD ? lds_vector(r) : load(xn, r); };
         auto form_rounds = [&](auto first, auto end) {
@@ -623,7 +639,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THRE
     if (!o.grad) return;
     __syncthreads();
     const RowGrad k = lds_grad;
-    stream_row<DT, THREADS, 4, false>(x, b.V, [&](const float *v, int64_t i) {
+    stream_row<DT, THREADS, 4, false>(x, 0, b.V, [&](const float *v, int64_t i) {
         float d[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) d[j] = k.operator()<ENT>(v[j]);
