@@ -3,7 +3,8 @@
 The product is ``libdifr.so`` (hand-written HIP kernels for gfx950 behind the C ABI of
 ``include/difr.h``).  This package is only its Python binding: one function per entry
 point, with the entry point's name less the ``difr_`` prefix (``score_both``,
-``gumbel_score``, ``ipt_score``, ``seq_reduce``, ``classify``, ``lmhead_score``, ...).
+``gumbel_score``, ``ipt_score``, ``seq_reduce``, ``classify``, ``lmhead_score``,
+``token_logprob``, ``policy_loss``, ``preference_loss``, ``mx4_product``, ...).
 Each marshals torch device tensors into the C call and returns torch tensors; every step
 of the computation runs in the library's kernels.  There is no CPU fallback: if the
 library is missing, ``load_library()`` - and with it every call - fails loudly.

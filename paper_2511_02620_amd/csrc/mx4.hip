@@ -7,12 +7,11 @@
 
 namespace difr {
 
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // A lane has eight elements of a row, four lanes a block of 32, whose largest magnitude they exchange; the conversion itself is the
-// machine's (round to nearest, ties to even, saturating), two elements an instruction.  Bound by memory.  One element at a time by
-// comparisons, a lane a block: 151,936 x 4096 bf16 390 us.
+// machine's (round to nearest, ties to even, saturating), two elements an instruction.  Bound by memory: 151,936 x 4096 bf16 258 us, 6.1
+// TB/s (one element at a time by comparisons, a lane a block, 390 us).
 constexpr int kQuantVectors = 2;  // of eight elements, of each thread
 
 template <int DT>
