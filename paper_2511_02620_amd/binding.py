@@ -576,6 +576,8 @@ def _token_rows(logits, V, tokens, temperatures):
     if tokens is None:
         raise ValueError("tokens must be a contiguous 1-D int32 tensor of %d elements" % N)
     _check(temperatures, torch.float32, N, "temperatures", dev)
+    if V is not None and int(V) > logits.shape[1]:
+        raise ValueError("V must be at most %d, the columns of logits" % logits.shape[1])
     return dev, N, logits.shape[1] if V is None else int(V)
 
 

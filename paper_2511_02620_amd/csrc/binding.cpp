@@ -547,6 +547,7 @@ struct TokenRows {
         in.logits = x.data_ptr();
         in.N = N;
         in.V = a[1] == Py_None ? x.size(1) : whole(a[1]);
+        if (in.V > x.size(1)) throw Refused();
         in.ld = N > 1 ? x.stride(0) : std::max(x.size(1), N ? x.stride(0) : (int64_t)0);
         in.temperature = (float)number(a[2]);
         in.tokens = (const int32_t *)vec(a[3], at::kInt, N, dev);

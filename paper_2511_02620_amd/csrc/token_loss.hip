@@ -20,6 +20,14 @@ __device__ __forceinline__ T uniform_load(const T *p, int64_t i)
     return ((constant)(uintptr_t)p)[i];
 }
 
+// A workgroup a row or a pair: grids of more threads than 32 bits count have a second dimension, and workgroups behind the last one.
+constexpr int64_t kRowsAcross = (int64_t)1 << 21;
+static dim3 row_grid(int64_t N)
+{
+    return dim3((unsigned)(N < kRowsAcross ? N : kRowsAcross), (unsigned)((N + kRowsAcross - 1) / kRowsAcross));
+}
+__device__ __forceinline__ int64_t row_of_workgroup() { return (int64_t)blockIdx.y * kRowsAcross + blockIdx.x; }
+
 // Per-row scalars.
 struct TokenRow {
     float T, c;
@@ -149,7 +157,8 @@ template <int DT, int THREADS, bool ENT>
 __global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, const uint8_t *mask, LogProbOutputs o)
 {
     __shared__ float lds[3 * THREADS / 64];
-    const int64_t row = blockIdx.x;
+    const int64_t row = row_of_workgroup();
+    if (row >= b.N) return;
     typedef typename Elem<DT>::type elem;
     const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
     if (o.zero && threadIdx.x == 0) o.zero[row] = 0.0f;
@@ -622,7 +631,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THRE
     constexpr int E = Elem<DT>::kPerVec;
     __shared__ float lds[3 * THREADS / 64];
     __shared__ RowGrad lds_grad;
-    const int64_t row = blockIdx.x;
+    const int64_t row = row_of_workgroup();
+    if (row >= b.N) return;
     typedef typename Elem<DT>::type elem;
     const elem *x = reinterpret_cast<const elem *>(b.logits) + row * b.ld;
     elem *g = reinterpret_cast<elem *>(o.grad) + row * o.ld_grad;
@@ -660,7 +670,8 @@ __global__ __launch_bounds__(kBlock) void pair_kernel(int64_t N, PreferenceParam
 {
     __shared__ double lds_sum[2][kWaves], lds_back[2];
     __shared__ int lds_count[2][kWaves];
-    const int64_t pair = blockIdx.x;
+    const int64_t pair = row_of_workgroup();
+    if (pair >= p.S / 2) return;
     const int tid = threadIdx.x;
     int64_t lo[2], hi[2];
     for (int side = 0; side < 2; ++side) {
@@ -760,7 +771,7 @@ static void run_logprob(const TokenRows &b, const uint8_t *mask, const LogProbOu
         // 256 x 151,936 24.8 / 16.8, 512 x 32,000 10.0 / 9.7, 512 x 16,384 6.2 / 7.2.
         token_logprob_kernel<DT, 1024, ENT><<<dim3((unsigned)b.N), dim3(1024), 0, stream>>>(b, mask, o);
     } else {
-        token_logprob_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, mask, o);
+        token_logprob_kernel<DT, kBlock, ENT><<<row_grid(b.N), dim3(kBlock), 0, stream>>>(b, mask, o);
     }
 }
 
@@ -834,9 +845,9 @@ static void run_policy(const TokenRows &b, const PolicyParams &p, const PolicyOu
     }
     // With the gradient one workgroup to a compute unit, so that the rows stay in the Infinity Cache until they are read again.
     if (o.grad)
-        policy_kernel<DT, 1024, ENT><<<dim3((unsigned)b.N), dim3(1024), 0, stream>>>(b, p, o);
+        policy_kernel<DT, 1024, ENT><<<row_grid(b.N), dim3(1024), 0, stream>>>(b, p, o);
     else
-        policy_kernel<DT, kBlock, ENT><<<dim3((unsigned)b.N), dim3(kBlock), 0, stream>>>(b, p, o);
+        policy_kernel<DT, kBlock, ENT><<<row_grid(b.N), dim3(kBlock), 0, stream>>>(b, p, o);
 }
 
 template <int DT, bool ENT>
@@ -875,7 +886,7 @@ int launch_preference_loss(const TokenRows &b, const PreferenceParams &p, const 
     LogProbOutputs row = o.row;
     row.zero = back ? o.grad_logp : nullptr;  // rows outside all sequences keep that
     if (b.N > 0 && launch_token_logprob(b, p.mask, row, workspace, stream)) return 1;
-    if (pairs > 0) pair_kernel<<<dim3((unsigned)pairs), dim3(kBlock), 0, stream>>>(b.N, p, o);
+    if (pairs > 0) pair_kernel<<<row_grid(pairs), dim3(kBlock), 0, stream>>>(b.N, p, o);
     const WeightedSum sum{o.pair_loss, p.pair_weights, pairs ? 1.0 / (double)pairs : 0.0, pairs, o.loss};
     if (back) return run_backward(b, o.row.stats, nullptr, o.grad_logp, nullptr, o.grad, o.ld_grad, sum, stream);
     weighted_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(sum);

@@ -505,6 +505,41 @@ def test_a_step_is_captured_and_replayed(difr, V):
             assert torch.equal(x, y), (seed, i)
 
 
+def test_more_rows_than_a_grid_of_threads_counts(difr):
+    N, V = (1 << 24) + 5, 3
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(N, V, generator=g, device=DEV)
+    tok = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    lp = torch.log_softmax(x.double(), 1)
+    want = lp.gather(1, tok.long()[:, None]).squeeze(1)
+    # three exponents, their sum, its logarithm and the result: some 10 roundings of numbers below 12
+    bound = 10 * 2.0 ** -24 * 12
+    o = difr.token_logprob(x, 1.0, tok, want_entropy=True)
+    assert (o["logp"] - want).abs().max() < bound and o["flags"].eq(0).all()
+    assert (o["entropy"] + (lp.exp() * lp).sum(1)).abs().max() < bound
+    A = torch.randn(N, generator=g, device=DEV)
+    for kw in (dict(want_grad=False), dict(out=x)):
+        p = difr.policy_loss(x, 1.0, tok, A, **kw)
+        assert (p["logp"] - want).abs().max() < bound and torch.equal(p["token_loss"], -A)
+    empty = torch.zeros(2 * N + 1, dtype=torch.int64, device=DEV)                   # as many pairs of empty replies
+    q = difr.preference_loss(x[:1], 1.0, tok[:1], empty, 0.1, want_grad=False)
+    assert q["pair_loss"].shape[0] == N and (q["pair_loss"] - math.log(2)).abs().max() < 1e-7
+    back = -(A.double() / N)[:, None] * (torch.nn.functional.one_hot(tok.long(), V) - lp.exp())
+    assert ((x - back).abs() <= 2 * bound * (A.double().abs() / N)[:, None]).all()
+
+
+def test_a_vocabulary_beyond_the_columns_is_refused(difr):
+    buf = torch.zeros(4, 64, device=DEV)
+    x, t, A = buf[:, 8:40], torch.zeros(4, dtype=torch.int32, device=DEV), torch.ones(4, device=DEV)
+    off = torch.tensor([0, 2, 4], device=DEV)
+    for call in (lambda V: difr.token_logprob(x, 1.0, t, V=V), lambda V: difr.policy_loss(x, 1.0, t, A, V=V),
+                 lambda V: difr.preference_loss(x, 1.0, t, off, 0.1, V=V),
+                 lambda V: difr.token_logprob_backward(x, 1.0, t, torch.ones(4, 2, device=DEV), A, V=V)):
+        call(32), call(7)
+        with pytest.raises(ValueError, match="V must be at most 32"):
+            call(33)
+
+
 def test_out_that_overlaps_is_refused(difr):
     buf = torch.zeros(10, 64, device=DEV)
     x, t = buf[:4], torch.zeros(4, dtype=torch.int32, device=DEV)
