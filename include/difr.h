@@ -584,7 +584,7 @@ int difr_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N, 
 /*
  * out[n][v] = sum_k a[n][k] b[v][k], fp32 accumulation on the matrix cores, rounded once to bf16 or fp32: the logits of N hidden states
  * under an LM head of V rows.  a: N rows, b: V rows of K = padded elements each (K % 128 == 0, else DIFR_ERR_SHAPE).  out [N, ld], ld >=
- * V, base aligned to its element size.  N, V <= 2^31 - 1024, K < 2^24.
+ * V, base aligned to its element size.  N, V <= 2^31 - 1024, N + V <= 2^29 - 1024 where N > 128, K < 2^24.
  * workspace  DEVICE scratch of at least difr_mx4_product_workspace_bytes(N, V, K) bytes (host only; 0: none is needed and NULL will do),
  * 16-byte aligned, contents irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small: DIFR_ERR_SHAPE.
  */

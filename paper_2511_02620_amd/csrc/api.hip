@@ -595,7 +595,8 @@ int difr_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N, 
 static bool mx4_product_shape(int64_t N, int64_t V, int64_t K)
 {
     const int64_t most = ((int64_t)1 << 31) - 1024;  // (row numbers of whole tiles stay in 32 bits)
-    return N >= 0 && V >= 0 && N <= most && V <= most && K >= difr::kMxSlab && K % difr::kMxSlab == 0 && K < (int64_t)1 << 24;
+    if (N < 0 || V < 0 || N > most || V > most || K < difr::kMxSlab || K % difr::kMxSlab || K >= (int64_t)1 << 24) return false;
+    return difr::mx4_product_grid(N, V);
 }
 
 size_t difr_mx4_product_workspace_bytes(int64_t N, int64_t V, int64_t K)

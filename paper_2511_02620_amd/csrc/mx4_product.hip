@@ -569,6 +569,9 @@ static Mx4Plan mx4_plan(int64_t N, int64_t V)
 
 constexpr int64_t kMxSmallMost = 128;  // most rows of a of the kernel that reads b once
 
+// Whether the threads that put the scales in tile order (2048 for 256 rows of either matrix) are counted in 32 bits.
+bool mx4_product_grid(int64_t N, int64_t V) { return N <= kMxSmallMost || N + V <= ((int64_t)1 << 29) - 1024; }
+
 size_t mx4_product_workspace_bytes(int64_t N, int64_t V, int64_t K)
 {
     if (N <= kMxSmallMost) return 0;

@@ -67,6 +67,7 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N
                           hipStream_t stream);
 int launch_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N, const uint8_t *b_codes, const uint8_t *b_scales,
                        int64_t V, int64_t K, void *out, int dtype, int64_t ld, void *workspace, hipStream_t stream);
+bool mx4_product_grid(int64_t N, int64_t V);
 size_t mx4_product_workspace_bytes(int64_t N, int64_t V, int64_t K);
 
 }  // namespace difr

@@ -114,7 +114,8 @@ def test_arguments_of_the_4_bit_calls():
         return lib.difr_mx4_product(a, sa, N, b, sb, V, K, out, t, ld, ws, n, None)
 
     for kw, want in ((dict(N=-1), SHAPE), (dict(V=-1), SHAPE), (dict(ld=7), SHAPE), (dict(K=0), SHAPE), (dict(K=64), SHAPE),
-                     (dict(K=200), SHAPE), (dict(K=1 << 24), SHAPE), (dict(N=1 << 31), SHAPE), (dict(V=1 << 31, ld=1 << 31), SHAPE),
+                     (dict(K=200), SHAPE), (dict(K=1 << 24), SHAPE), (dict(N=129, V=1 << 29, ld=1 << 29), SHAPE),
+                     (dict(N=1 << 29), SHAPE), (dict(N=129, V=(1 << 29) - 2048, ld=1 << 29, n=1 << 40, ws=None), NULL), (dict(N=1 << 31), SHAPE), (dict(V=1 << 31, ld=1 << 31), SHAPE),
                      (dict(t=2), DTYPE), (dict(a=None), NULL), (dict(sb=None), NULL), (dict(out=None), NULL), (dict(a=0x1008), ALIGN),
                      (dict(sb=0x1002), ALIGN), (dict(out=0x1001), ALIGN), (dict(N=0), OK), (dict(V=0), OK),
                      (dict(ws=0x1008), ALIGN)):
