@@ -301,9 +301,10 @@ def test_policy_rows_that_follow_each_other(difr, V, dtype):
     assert torch.equal(again["grad"], got["grad"]), "in place"
 
 
-def test_policy_rows_that_cannot_be_scored_are_loud(difr):
-    x, tok, g = _logits(3, 6, 900, torch.bfloat16)
-    x[1, 5], tok[2], x[3, :] = math.nan, 900, -INF
+@pytest.mark.parametrize("V", [900, 50000, 100003])
+def test_policy_rows_that_cannot_be_scored_are_loud(difr, V):
+    x, tok, g = _logits(3, 6, V, torch.bfloat16)
+    x[1, 5], tok[2], x[3, :] = math.nan, V, -INF
     A, w = torch.ones(6, device=DEV), torch.full((6,), 0.1, device=DEV)
     o = difr.policy_loss(x.to(DEV), 1.0, tok.to(DEV), A, w, want_entropy=True)
     assert torch.isnan(o["token_loss"]).tolist() == [False, True, True, True, False, False]
