@@ -523,6 +523,8 @@ int difr_token_logprob_backward(const difr_token_rows *in, const float *stats, c
  *          outputs are 0 and so is its gradient, whatever it holds.
  * old_logp [N] or NULL: old = logp (the ratio is 1, and A flows back as it is).
  * ref_logp [N] or NULL: no KL term; then kl and kl_coef have to be NULL and 0.
+ * A ratio or a kl beyond fp32's range (logp and old or ref more than 88 apart; a masked token, whose logp is -inf or near -3e38) is an
+ * infinity there: so are token_loss and loss, unless the clip or an advantage of 0 holds it, and what flows back leaves the range with them (entries of inf or NaN).
  * clip_low in [0, 1], clip_high >= 0 (infinity: no clip on that side), coefficients finite (else DIFR_ERR_ARGUMENT).
  * Outputs: loss [1]; token_loss, logp [N]; entropy, kl [N] or NULL; flags [N], with DIFR_FLAG_CLIPPED where the clip counts; grad
  * [N, V] or NULL: the gradient of loss.  N == 0 writes loss = 0.

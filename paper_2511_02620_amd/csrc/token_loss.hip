@@ -360,7 +360,8 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyParams &p, int64_t r
 {
     PolicyRow o;
     const double A = uniform_load(p.advantages, row);
-    const double ratio = p.old_logp ? exp_of(logp - (double)uniform_load(p.old_logp, row)) : (logp == logp ? 1.0 : logp);
+    double ratio = p.old_logp ? exp_of(logp - (double)uniform_load(p.old_logp, row)) : (logp == logp ? 1.0 : logp);
+    ratio = ratio > 1e300 ? 1e300 : ratio;  // a number, of which an advantage of 0 leaves nothing; any other makes it infinite in fp32
     const double lo = 1.0 - p.clip_low, hi = 1.0 + p.clip_high;
     const double inside = ratio < lo ? lo : (ratio > hi ? hi : ratio);
     const bool clipped = ratio * A > inside * A;
