@@ -545,6 +545,8 @@ int difr_policy_loss(const difr_token_rows *in, const difr_policy *p, float *los
  * (average != 0), R_s = ref_seq_logp[s]:
  *   h    = beta ((L_c - R_c) - (L_r - R_r)) - margin
  *   pair_loss = -(1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h);   loss = sum_p pair_weights[p] pair_loss[p]
+ * A side of -ln sigma whose factor is 0 is left out: a rejected reply with a token of logit -inf (h = inf) has the loss 0 without smoothing,
+ * an infinite one with it, and what flows back is a number either way.  Such a token in both replies leaves NaN.
  * mask [N] or NULL: a token whose byte is 0 (a prompt's, padding) does not count: its row is not read, its logp and gradient are 0.
  * An empty sequence, or one that is masked whole, has L = 0.  Rows outside all sequences get their logp and a gradient of 0.
  * ref_seq_logp [S] or NULL: 0.  pair_weights [S / 2] or NULL: 2 / S each.  S even (DIFR_ERR_SHAPE); beta, margin finite,

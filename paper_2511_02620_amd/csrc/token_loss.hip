@@ -711,7 +711,8 @@ __global__ __launch_bounds__(kBlock) void pair_kernel(int64_t N, PreferenceParam
         const double soft = log1p(exp(-fabs(h)));  // -ln sigma(h) = soft + max(-h, 0)
         const double up = h >= 0.0 ? 1.0 / (1.0 + exp(-h)) : exp(h) / (1.0 + exp(h));
         const double down = h >= 0.0 ? exp(-h) / (1.0 + exp(-h)) : 1.0 / (1.0 + exp(h));
-        o.pair_loss[pair] = (float)((1.0 - eps) * (soft + (h < 0.0 ? -h : 0.0)) + eps * (soft + (h > 0.0 ? h : 0.0)));
+        // (a side of factor 0 is left out: it may be infinite, where a reply holds a token without probability)
+        o.pair_loss[pair] = (float)((eps == 1.0 ? 0.0 : (1.0 - eps) * (soft + (h < 0.0 ? -h : 0.0))) + (eps == 0.0 ? 0.0 : eps * (soft + (h > 0.0 ? h : 0.0))));
         const double w = p.pair_weights ? (double)p.pair_weights[pair] : 2.0 / (double)p.S;
         const double back = w == 0.0 ? 0.0 : w * p.beta * (eps * up - (1.0 - eps) * down);
         lds_back[0] = back * share[0];
