@@ -181,21 +181,17 @@ __device__ __forceinline__ double ln_of(double S)
     const int k = S > 0.0 && S < (double)__builtin_inff() ? ilogb(S * 1.41421356) : 0;  // S 2^-k in [0.707, 1.414)
     return (double)k * 0.69314718055994530942 + (double)logf((float)ldexp(S, -k));
 }
-// (e^u from 700 on is infinite: far beyond fp32, near the end of 64 bits)
+// (without branches: e^u runs to infinity and to 0 by itself, and NaN stays what it is)
 __device__ __forceinline__ double exp_of(double u)
 {
-    if (u != u) return u;
-    if (u >= 700.0) return __builtin_inf();
-    if (u < -700.0) return 0.0;
-    const double k = rint(u * 1.44269504088896340736);
+    const double k = fmin(fmax(rint(u * 1.44269504088896340736), -3000.0), 3000.0);
     return ldexp((double)expf((float)(u - k * 0.69314718055994530942)), (int)k);
 }
 __device__ __forceinline__ double expm1_of(double u) { return fabs(u) < 0.35 ? (double)expm1f((float)u) : exp_of(u) - 1.0; }
 // e^d - d - 1, by its series where the difference would cancel (the terms left out are below 1e-8 of the sum); it goes to infinity on both sides
 __device__ __forceinline__ double exp_less_line(double d)
 {
-    if (d >= 700.0) return __builtin_inf();
-    if (fabs(d) >= 0.35) return exp_of(d) - d - 1.0;
+    if (fabs(d) >= 0.35) return exp_of(d) - (d > 1e300 ? 1e300 : d) - 1.0;
     return d * d * (0.5 + d * (1.0 / 6 + d * (1.0 / 24 + d * (1.0 / 120 + d * (1.0 / 720 + d * (1.0 / 5040 + d * (1.0 / 40320)))))));
 }
 
