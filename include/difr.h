@@ -471,14 +471,18 @@ int difr_seq_reduce(const float *scores, const uint8_t *row_flags, const int64_t
  *
  *   p = softmax(x / T) over the row;  logp = ln p_t;  H = -sum_v p_v ln p_v
  *
- * A logit of -inf or of the type's lowest value is a masked entry: no probability, no gradient (a row that holds nothing but the
+ * A logit of -inf or of the type's lowest value is a masked entry: no probability, and no gradient unless it is the logged token's own (a row that holds nothing but the
  * lowest value is uniform).  A row that holds no finite logit, a NaN or +inf, or has a temperature that is not positive and finite,
  * gets NaN and DIFR_FLAG_NONFINITE; a token outside [0, V) gets a NaN log-probability and DIFR_FLAG_INVALID_CLAIM.  Other rows are
  * not touched by either.
  *
  * Gradients are written in the logits' type, rounded once; `grad` is [N, V] with row pitch ld_grad >= V and may be the logits
  * themselves (same address and pitch): the row is read before it is overwritten.  Any other overlap gives wrong results.
- * Sums of a row are formed in fp32 per thread and in fp64 from there on, in a fixed order; everything per row is fp64.
+ * The terms of a row, 2^((x - the row's largest logit) log2(e) / T), are fp32; 16 bytes of the row are summed in fp32, the rest in fp64, in
+ * a fixed order.  The largest logit's term is exactly 1: logp <= 0 and H >= 0.  What follows for each row (logp, H, ratios, losses) is formed in
+ * fp64 with exp and ln good to 2e-7 of their value.  The coefficients of a gradient are fp32 in difr_token_logprob_backward, in the
+ * preference loss and where few long rows are shared among workgroups, which take the sum from fp32 statistics, and fp64 rounded
+ * once elsewhere.
  *
  * workspace  DEVICE scratch of at least difr_token_workspace_bytes(N, V, dtype) bytes (host only, no device needed), 8-byte aligned,
  * contents irrelevant before and after; calls that overlap in time need distinct workspaces.  Few long rows are shared among several
@@ -495,7 +499,7 @@ typedef struct {
 
 /*
  * logp     [N] fp32
- * stats    [N, 2] fp32 or NULL: (r, sum_v exp((x_v - r) / T)) with r a logit of the row, what difr_token_logprob_backward needs
+ * stats    [N, 2] fp32 or NULL: (r, sum_v exp((x_v - r) / T)) with r the row's largest logit, what difr_token_logprob_backward needs
  * entropy  [N] fp32 or NULL
  * flags    [N]
  * One pass over the logits.

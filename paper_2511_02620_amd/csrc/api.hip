@@ -134,7 +134,8 @@ int validate_token_rows(const difr_token_rows *in, difr::TokenRows *b)
         if (!in->temperatures && !(in->temperature > 0.0f && isfinite(in->temperature))) return DIFR_ERR_TEMPERATURE;
     }
     if ((uintptr_t)in->logits % (in->dtype == DIFR_BF16 ? 2u : 4u)) return DIFR_ERR_ALIGN;
-    *b = difr::TokenRows{in->logits, in->dtype, in->N, in->V, in->ld, in->temperature, in->temperatures, in->tokens};
+    *b = difr::TokenRows{in->logits, in->dtype, in->N, in->V, in->ld, in->temperature, in->temperatures, in->tokens,
+                         difr::exponent_scale(in->temperature)};
     return DIFR_OK;
 }
 

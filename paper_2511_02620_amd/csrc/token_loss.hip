@@ -30,7 +30,8 @@ __device__ __forceinline__ int64_t row_of_workgroup() { return (int64_t)blockIdx
 
 // Per-row scalars.
 struct TokenRow {
-    float T, c;
+    float T;
+    ExponentScale c;
     int32_t t;
     bool temp_ok, token_ok;
 };
@@ -41,7 +42,8 @@ __device__ __forceinline__ TokenRow load_token_row(const TokenRows &b, int64_t r
     r.temp_ok = r.T > 0.0f && r.T < __builtin_inff();
     r.t = uniform_load(b.tokens, row);
     r.token_ok = r.t >= 0 && (int64_t)r.t < b.V;
-    r.c = r.temp_ok ? kLog2e / r.T : __builtin_nanf("");
+    r.c = b.temperatures ? exponent_scale(r.T) : b.scale;
+    if (!r.temp_ok) r.c.hi = __builtin_nanf("");
     return r;
 }
 
@@ -103,19 +105,19 @@ __device__ __forceinline__ void first_vector(u32x4 q, int lead, float x[Elem<DT>
 
 // The row's sums, by all threads of the workgroup, for the first wave.
 template <int DT, int THREADS, bool ENT>
-__device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, float c, bool past, float *lds)
+__device__ __forceinline__ RowSums row_sums(const typename Elem<DT>::type *row, int64_t V, ExponentScale c, bool past, RowSums *lds)
 {
     constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64, U = 4;
+    __shared__ float lds_first[W];
     const AlignedRow<DT> a = aligned_row<DT>(row, V);
     float x[E];
     first_vector<DT>(row_vector<DT>(a.x, threadIdx.x, a.V), a.lead, x);
-    const float m = wave_max(vector_max<DT>(x));
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+    const float m = wave_top(vector_max<DT>(x));
+    if ((threadIdx.x & 63) == 0) lds_first[threadIdx.x >> 6] = m;
     __syncthreads();
-    float first = lds[0];
+    float first = lds_first[0];
 #pragma unroll
-    for (int i = 1; i < W; ++i) first = fmaxf(first, lds[i]);
-    __syncthreads();
+    for (int i = 1; i < W; ++i) first = fmaxf(first, lds_first[i]);
     SoftmaxSums<DT, ENT> s;
     s.begin(first, c);
     s.add(x);
@@ -156,7 +158,7 @@ __device__ __forceinline__ void logprob_left_out(const LogProbOutputs &o, int64_
 template <int DT, int THREADS, bool ENT>
 __global__ __launch_bounds__(THREADS) void token_logprob_kernel(TokenRows b, const uint8_t *mask, LogProbOutputs o)
 {
-    __shared__ float lds[3 * THREADS / 64];
+    __shared__ RowSums lds[THREADS / 64];
     const int64_t row = row_of_workgroup();
     if (row >= b.N) return;
     typedef typename Elem<DT>::type elem;
@@ -189,7 +191,8 @@ __global__ __launch_bounds__(kBlock) void row_part_kernel(TokenRows b, const uin
 {
     constexpr int E = Elem<DT>::kPerVec, U = 4;
     typedef typename Elem<DT>::type elem;
-    __shared__ float lds_first[kWaves], lds[3 * kWaves];
+    __shared__ float lds_first[kWaves];
+    __shared__ RowSums lds[kWaves];
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / parts;
     const int part = blockIdx.x % parts;
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(kBlock) void row_part_kernel(TokenRows b, const uin
     const elem *x = a.x + begin * E;
     const int64_t len = part + 1 == parts ? a.V - begin * E : (end - begin) * E, total = (len + E - 1) / E;
     const int lead = part == 0 ? a.lead : 0;
-    const float T = b.temperatures ? uniform_load(b.temperatures, row) : b.temperature;
+    const ExponentScale c = load_token_row(b, row).c;
     SoftmaxSums<DT, ENT> s;
     for (int64_t i = 0; i < total; i += U * kBlock) {
         u32x4 q[U];
@@ -213,10 +216,10 @@ __global__ __launch_bounds__(kBlock) void row_part_kernel(TokenRows b, const uin
         float y[E];
         first_vector<DT>(q[0], i == 0 ? lead : 0, y);
         if (i == 0) {
-            const float m = wave_max(vector_max<DT>(y));
+            const float m = wave_top(vector_max<DT>(y));
             if ((tid & 63) == 0) lds_first[tid >> 6] = m;
             __syncthreads();
-            s.begin(fmaxf(fmaxf(lds_first[0], lds_first[1]), fmaxf(lds_first[2], lds_first[3])), T > 0.0f && T < __builtin_inff() ? kLog2e / T : __builtin_nanf(""));
+            s.begin(fmaxf(fmaxf(lds_first[0], lds_first[1]), fmaxf(lds_first[2], lds_first[3])), c);
         }
         s.add(y);
 #pragma unroll
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(kBlock) void row_part_kernel(TokenRows b, const uin
 
 // The sums of a row's parts (64 or fewer), for all lanes of a wave.
 template <bool ENT>
-__device__ __forceinline__ RowSums joined(const RowSums *sums, int parts, int64_t row, float c)
+__device__ __forceinline__ RowSums joined(const RowSums *sums, int parts, int64_t row, ExponentScale c)
 {
     const int lane = threadIdx.x;
     return join_sums<64, ENT>(lane < parts ? sums[row * parts + lane] : RowSums{kNoLogit, 0.0, 0.0}, c);
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6,6))) v
         float v[E];
         unpack_vector<DT>(q[u], v);
 #pragma unroll
-        for (int j = 0; j < E; ++j) v[j] = k.operator()<ENT>(v[j]);
+        for (int j = 0; j < E; ++j) v[j] = k.operator()<DT, ENT>(v[j]);
         if (here && i == r.t / E) {
 #pragma unroll
             for (int j = 0; j < E; ++j)
@@ -463,7 +466,8 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
     constexpr int E = Elem<DT>::kPerVec, W = THREADS / 64, AHEAD = LDS || R < 24 || THREADS < 512 ? 0 : R - 8 < kAheadRounds ? R - 8 : kAheadRounds;
     __shared__ __attribute__((aligned(16))) uint8_t lds_row[LDS ? kLdsRounds * THREADS * 16 : AHEAD ? AHEAD * THREADS * 16 : 16];
     typedef typename Elem<DT>::type elem;
-    __shared__ float lds_first[W], lds[3 * W];
+    __shared__ float lds_first[W];
+    __shared__ RowSums lds[W];
     __shared__ RowGrad lds_grad;
     const int tid = threadIdx.x;
     const int64_t step = gridDim.x, V = b.V;
@@ -531,7 +535,7 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
                 unpack_vector<DT>(q[0], y);
                 m = fmaxf(m, vector_max<DT>(y));
             }
-            m = wave_max(m);
+            m = wave_top(m);
             if ((tid & 63) == 0) lds_first[tid >> 6] = m;
         }
         __syncthreads();
@@ -592,7 +596,7 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 4 : R <= 16 ? 3 : 2) void policy_
             asm volatile("" : "+v"(v));  // unpacked anew: the compiler would keep the values from the first time, twice the registers
             unpack_vector<DT>(v, y);
 #pragma unroll
-            for (int j = 0; j < E; ++j) y[j] = k.operator()<ENT>(y[j]);
+            for (int j = 0; j < E; ++j) y[j] = k.operator()<DT, ENT>(y[j]);
             return pack_vector<DT>(y);
         };
         if (LDS) {
@@ -630,7 +634,7 @@ template <int DT, int THREADS, bool ENT>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THREADS == 1024 ? 4 : 8))) void policy_kernel(TokenRows b, PolicyParams p, PolicyOutputs o)
 {
     constexpr int E = Elem<DT>::kPerVec;
-    __shared__ float lds[3 * THREADS / 64];
+    __shared__ RowSums lds[THREADS / 64];
     __shared__ RowGrad lds_grad;
     const int64_t row = row_of_workgroup();
     if (row >= b.N) return;
@@ -653,7 +657,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4, THRE
     stream_row<DT, THREADS, 4, false>(x, 0, b.V, [&](const float *v, int64_t i) {
         float d[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) d[j] = k.operator()<ENT>(v[j]);
+        for (int j = 0; j < E; ++j) d[j] = k.operator()<DT, ENT>(v[j]);
         if (r.token_ok && i == r.t / E) {
 #pragma unroll
             for (int j = 0; j < E; ++j)

@@ -6,6 +6,27 @@
 
 namespace difr {
 
+// log2(e) / T in two parts, of which the second is positive (so that a difference of -inf is one with either).
+struct ExponentScale {
+    float hi, lo;
+    __device__ __forceinline__ double whole() const { return (double)hi + (double)lo; }
+};
+__host__ __device__ inline ExponentScale exponent_scale(float T)
+{
+    constexpr float kLog2e = 1.44269504088896340736f, kLog2eRest = (float)(1.44269504088896340736 - (double)kLog2e), kLn2 = 0.693147180559945309417f;
+    ExponentScale c;
+    c.hi = kLog2e / T;
+    c.lo = (__builtin_fmaf(-c.hi, T, kLog2e) + kLog2eRest) * (c.hi * kLn2);  // what is left of log2(e), over T
+    if (!(c.lo > 0.0f)) {
+        c.hi = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, c.hi) - 1u);  // the next one below
+        c.lo = (__builtin_fmaf(-c.hi, T, kLog2e) + kLog2eRest) * (c.hi * kLn2);
+    }
+    // (a temperature at the end of fp32's range leaves 0 or no number)
+    c.lo = c.lo > 0x1p-149f ? c.lo : 0x1p-149f;
+    c.lo = c.lo < 0x1p127f ? c.lo : 0x1p127f;
+    return c;
+}
+
 struct TokenRows {
     const void *logits;
     int32_t dtype;
@@ -13,6 +34,7 @@ struct TokenRows {
     float temperature;
     const float *temperatures;  // [N] or null
     const int32_t *tokens;
+    ExponentScale scale;  // of `temperature`
 };
 
 struct LogProbOutputs {
