@@ -557,11 +557,18 @@ struct TokenRows {
 };
 constexpr int kTokenRowArgs = 5;
 
+// A tensor of the caller's has been written, if the call succeeded: its version goes up, as by torch's own operations in place, so that a
+// graph that has saved it refuses to run backward.
+void written(int rc, const at::Tensor &t)
+{
+    if (rc == 0 && t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // Where a gradient [N, V] goes: a tensor of the caller's (the logits themselves, or one that does not overlap them), or a new one.
 struct Grad {
     void *data = nullptr;
     int64_t ld = 0;
-    at::Tensor t;
+    at::Tensor t, theirs;
     Grad(const TokenRows &r, PyObject *out, Outputs &o)
     {
         if (out == Py_None) {
@@ -570,7 +577,7 @@ struct Grad {
             ld = std::max(r.in.V, (int64_t)1);
             return;
         }
-        t = tensor(out);
+        theirs = t = tensor(out);
         if (t.device() != r.dev || t.scalar_type() != r.type || t.dim() != 2 || t.size(0) != r.N || t.size(1) != r.in.V ||
             (t.stride(1) != 1 && t.size(1) > 1))
             throw Refused();
@@ -636,6 +643,7 @@ PyObject *token_logprob_backward(PyObject *const *a)
     Outputs o(r.dev);
     Grad g(r, a[4], o);
     const int rc = enter(r.dev, [&](void *s) { return lib.difr_token_logprob_backward(&r.in, stats, entropy, ga, ge, g.data, g.ld, s); });
+    written(rc, g.theirs);
     return rc ? PyLong_FromLong(rc) : g.wrap();
 }
 
@@ -657,16 +665,19 @@ PyObject *policy_loss(PyObject *const *a)
     uint8_t *flags = o.u8(key::flags, r.N);
     void *grad = nullptr;
     int64_t ld = 0;
+    at::Tensor theirs;
     if (truth(a[9])) {
         Grad g(r, a[10], o);
-        grad = g.data, ld = g.ld;
+        grad = g.data, ld = g.ld, theirs = g.theirs;
         g.into(o);
     }
     if (!r.N) grad = nullptr;
     const Scratch w(r, o);
-    return one(enter(r.dev, [&](void *s) {
-                   return lib.difr_policy_loss(&r.in, &p, loss, token_loss, logp, entropy, kl, flags, grad, ld, w.data, w.bytes, s);
-               }), o);
+    const int rc = enter(r.dev, [&](void *s) {
+        return lib.difr_policy_loss(&r.in, &p, loss, token_loss, logp, entropy, kl, flags, grad, ld, w.data, w.bytes, s);
+    });
+    written(rc, theirs);
+    return one(rc, o);
 }
 
 // token rows, seq_offsets, beta, mask, ref_seq_logp, pair_weights, label_smoothing, margin, average, want_grad, out
@@ -689,19 +700,22 @@ PyObject *preference_loss(PyObject *const *a)
     uint8_t *flags = o.u8(key::flags, r.N);
     void *grad = nullptr;
     int64_t ld = 0;
+    at::Tensor theirs;
     if (truth(a[8])) {
         stats = (float *)o.add(key::stats, at::kFloat, {r.N, 2});
         grad_logp = o.f32(key::grad_logp, r.N);
         Grad g(r, a[9], o);
-        grad = g.data, ld = g.ld;
+        grad = g.data, ld = g.ld, theirs = g.theirs;
         g.into(o);
     }
     if (!r.N) grad = nullptr;
     const Scratch w(r, o);
-    return one(enter(r.dev, [&](void *s) {
-                   return lib.difr_preference_loss(&r.in, &p, loss, pair_loss, seq_logp, logp, stats, grad_logp, flags, grad, ld, w.data,
-                                                   w.bytes, s);
-               }), o);
+    const int rc = enter(r.dev, [&](void *s) {
+        return lib.difr_preference_loss(&r.in, &p, loss, pair_loss, seq_logp, logp, stats, grad_logp, flags, grad, ld, w.data,
+                                        w.bytes, s);
+    });
+    written(rc, theirs);
+    return one(rc, o);
 }
 
 // ---- 4-bit floating point ----
@@ -793,6 +807,7 @@ PyObject *mx4_product(PyObject *const *a)
         return lib.difr_mx4_product(x.codes, x.scales, x.rows, y.codes, y.scales, y.rows, x.K, t.data_ptr(), f32 ? DIFR_F32 : DIFR_BF16,
                                     ld, wsp, need, s);
     });
+    if (a[5] != Py_None) written(rc, t);
     return wrapped(rc, t);
 }
 
