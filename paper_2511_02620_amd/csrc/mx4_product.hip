@@ -27,7 +27,7 @@ struct Mx4Plan {
     int n_tb, n_vt, splits;
 };
 
-// Eight 4-byte codes of a fragment and nothing above them: the instruction reads the lower half only for this type.
+// The 32 codes of a lane's fragment, 4 bits each, in four dwords, and nothing above them: the instruction reads the lower half only for this type.
 __device__ __forceinline__ i32x8 fp4_operand(i32x4 v) { return __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1); }
 
 // acc += a b for fragments of 32 x 64 elements; byte STEP of the two scale registers is the scale of the lane's 32.
@@ -96,15 +96,9 @@ __device__ __forceinline__ void pack_block(const f32x16 acc, u32x4 q[2])
     }
 }
 
-// When the 16 copies of a slab go out, as in the fused LM head: copy c after matrix instruction kCopySlot[c] of the 48 of the fourth k
-// step of one slab and the first two of the next.
-__host__ __device__ constexpr int copy_at_slot(int n)
-{
-    constexpr int kCopySlot[16] = {0, 2, 4, 6, 8, 10, 12, 14, 16, 18, 20, 22, 24, 26, 28, 30};
-    for (int c = 0; c < 16; ++c)
-        if (kCopySlot[c] == n) return c;
-    return -1;
-}
+// When the 16 copies of a slab go out, spaced as in the fused LM head: after every second matrix instruction of the 32 of the fourth k step of
+// one slab and the first of the next.  The copy after instruction n of them, or -1.
+static constexpr int product_copy_at_slot(int n) { return n % 2 == 0 ? n / 2 : -1; }
 
 // 256 threads = 4 waves, 2 (rows of b) x 2 (rows of a), each with a 128 x 128 sub-tile of 4 x 4 accumulator blocks.  One wave per SIMD.
 // LDS: two stages of [256 rows][128 bytes] for either operand; the eight 16-byte chunks of a row, one block of 32 elements each, are
@@ -255,17 +249,17 @@ __global__ __launch_bounds__(kBlock, 1) void mx4_product_kernel(Mx4Product m, Mx
     const std::integral_constant<int, 3> k3;
     auto cp = [&](auto PH, int buf) {
         return [&, buf](auto E) {
-            constexpr int c = copy_at_slot(16 * decltype(PH)::value + decltype(E)::value);
+            constexpr int c = product_copy_at_slot(16 * decltype(PH)::value + decltype(E)::value);
             if constexpr (c >= 0) copy_chunk(std::integral_constant<int, c>(), buf);
         };
     };
     // One slab.  The stage of slab g is last read in its third k step, so after the barrier that follows it is free, and the copies of
-    // slab g + 2 go into it during the fourth step of slab g and the first two of slab g + 1; each wave waits for its own copies before
+    // slab g + 2 go into it during the fourth step of slab g and the first of slab g + 1; each wave waits for its own copies before
     // the barrier of slab g + 1.  The first fragments of the next slab, of the next tile too, are read in the fourth step.
     auto slab = [&](int keep) {
         copy_scales(par ^ 1);
         kstep(k0, F0, F1, par, 1, cp(k1, par ^ 1));
-        kstep(k1, F1, F0, par, 2, cp(k2, par ^ 1));
+        kstep(k1, F1, F0, par, 2, [&](auto) {});
         advance_cursor();
         if (HALF) drop(F0, keep);
         kstep(k2, F0, F1, par, 3, [&](auto) {});
