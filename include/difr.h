@@ -68,7 +68,8 @@ typedef enum {
     DIFR_ERR_DTYPE = 3,       /* dtype is not a difr_dtype                           */
     DIFR_ERR_TEMPERATURE = 4, /* temperature not finite or <= 0 (greedy T = 0 is a   */
                               /* different sampling rule and is not this path)       */
-    DIFR_ERR_ALIGN = 5,       /* logits base not aligned to its element size         */
+    DIFR_ERR_ALIGN = 5,       /* logits base not aligned to its element size, or codes, */
+                              /* scales, a workspace not as the call states             */
     DIFR_ERR_LAUNCH = 6,      /* the HIP runtime refused the launch                  */
     DIFR_ERR_UNSUPPORTED = 7, /* the current device is not gfx950                    */
     DIFR_ERR_ARGUMENT = 8,    /* sigma <= 0, eps < 0, NaN where a number is needed, or */

@@ -563,8 +563,15 @@ def classify(scores, ranks, tau, rank_cutoff, V, log2_admissible=None):
     return out
 
 
+def _need_tensors(**tensors):
+    for name, t in tensors.items():
+        if not isinstance(t, torch.Tensor):
+            raise ValueError("%s must be a tensor" % name)
+
+
 def _token_rows(logits, V, tokens, temperatures):
     """Checks of the calls on logged tokens; (device, rows, vocabulary)."""
+    _need_tensors(logits=logits)
     if not logits.is_cuda:
         raise ValueError("logits must be a GPU tensor")
     if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
@@ -581,9 +588,12 @@ def _token_rows(logits, V, tokens, temperatures):
     return dev, N, logits.shape[1] if V is None else int(V)
 
 
-def _check_grad(out, logits, V):
+def _check_grad(out, logits, V, want_grad=True):
     if out is None:
         return
+    if not want_grad:
+        raise ValueError("out is for the gradient, which want_grad=False leaves out")
+    _need_tensors(out=out)
     N = logits.shape[0]
     if out.device != logits.device or out.dtype != logits.dtype or tuple(out.shape) != (N, V) or (V > 1 and out.stride(1) != 1) or (
             N > 1 and out.stride(0) < V):
@@ -611,6 +621,7 @@ def token_logprob_backward(logits, temperature, tokens, stats, grad_logp, entrop
                                                              temperatures, stats, grad_logp, entropy, grad_entropy, out)
     if got is None:
         dev, N, cols = _token_rows(logits, V, tokens, temperatures)
+        _need_tensors(stats=stats, grad_logp=grad_logp)
         if stats.device != dev or stats.dtype != torch.float32 or tuple(stats.shape) != (N, 2) or not stats.is_contiguous():
             raise ValueError("stats must be a contiguous [%d, 2] float32 tensor on %s" % (N, dev))
         for t, name in ((grad_logp, "grad_logp"), (entropy, "entropy"), (grad_entropy, "grad_entropy")):
@@ -639,7 +650,7 @@ def policy_loss(logits, temperature, tokens, advantages, weights=None, old_logp=
                 _check(t, torch.float32, N, name, dev)
             if advantages is None:
                 raise ValueError("advantages must be a contiguous 1-D float32 tensor of %d elements" % N)
-            _check_grad(out, logits, cols)
+            _check_grad(out, logits, cols, want_grad)
         _refused("difr_policy_loss", got, checks)
     return got
 
@@ -656,6 +667,7 @@ def preference_loss(logits, temperature, tokens, seq_offsets, beta, mask=None, r
     if got.__class__ is not dict:
         def checks():
             dev, N, cols = _token_rows(logits, V, tokens, temperatures)
+            _need_tensors(seq_offsets=seq_offsets)
             if (seq_offsets.device != dev or seq_offsets.dtype != torch.int64 or seq_offsets.dim() != 1 or not seq_offsets.is_contiguous()
                     or seq_offsets.shape[0] % 2 != 1):
                 raise ValueError("seq_offsets must be a contiguous 1-D int64 GPU tensor of S+1 elements, S even")
@@ -663,7 +675,7 @@ def preference_loss(logits, temperature, tokens, seq_offsets, beta, mask=None, r
             _check(mask, torch.uint8, N, "mask", dev)
             _check(ref_seq_logp, torch.float32, S, "ref_seq_logp", dev)
             _check(pair_weights, torch.float32, S // 2, "pair_weights", dev)
-            _check_grad(out, logits, cols)
+            _check_grad(out, logits, cols, want_grad)
         _refused("difr_preference_loss", got, checks)
     return got
 
@@ -679,6 +691,7 @@ def mx4_quantize(x):
     got = (_native or _load_native()).mx4_quantize(x)
     if got.__class__ is not dict:
         def checks():
+            _need_tensors(x=x)
             if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
                 raise ValueError("x must be a 2-D bfloat16 or float32 GPU tensor with unit column stride")
         _refused("difr_mx4_quantize", got, checks)
@@ -686,6 +699,7 @@ def mx4_quantize(x):
 
 
 def _check_coded(codes, scales, name):
+    _need_tensors(**{name + "codes": codes, name + "scales": scales})
     if not codes.is_cuda or codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_contiguous() or codes.shape[1] % 64:
         raise ValueError("%scodes must be a contiguous [rows, K / 2] uint8 GPU tensor, K a multiple of 128" % name)
     if (scales.device != codes.device or scales.dtype != torch.uint8 or not scales.is_contiguous()

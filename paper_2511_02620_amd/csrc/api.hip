@@ -678,7 +678,7 @@ const char *difr_status_string(int status)
         case DIFR_ERR_SHAPE: return "bad shape (N, V, S, ld or row index)";
         case DIFR_ERR_DTYPE: return "unknown logits dtype";
         case DIFR_ERR_TEMPERATURE: return "temperature must be finite and > 0";
-        case DIFR_ERR_ALIGN: return "logits pointer not aligned to its element size";
+        case DIFR_ERR_ALIGN: return "a pointer is not aligned as the call needs it (rows to their element size, others as stated at the call)";
         case DIFR_ERR_LAUNCH: return "HIP kernel launch failed";
         case DIFR_ERR_UNSUPPORTED: return "current device is not gfx950";
         case DIFR_ERR_ARGUMENT: return "bad scalar argument (sigma, eps, threshold, delta, a coefficient of a loss, or a top_k / top_p / s / M combination the call does not take)";

@@ -670,6 +670,8 @@ PyObject *policy_loss(PyObject *const *a)
         Grad g(r, a[10], o);
         grad = g.data, ld = g.ld, theirs = g.theirs;
         g.into(o);
+    } else if (a[10] != Py_None) {
+        throw Refused();
     }
     if (!r.N) grad = nullptr;
     const Scratch w(r, o);
@@ -707,6 +709,8 @@ PyObject *preference_loss(PyObject *const *a)
         Grad g(r, a[9], o);
         grad = g.data, ld = g.ld, theirs = g.theirs;
         g.into(o);
+    } else if (a[9] != Py_None) {
+        throw Refused();
     }
     if (!r.N) grad = nullptr;
     const Scratch w(r, o);
