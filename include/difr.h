@@ -587,12 +587,13 @@ int difr_preference_loss(const difr_token_rows *in, const difr_preference *p, fl
 int64_t difr_mx4_padded(int64_t d);
 /* x [N, ld] bf16 or fp32, base aligned to the element size -> codes, scales.  d >= 1. */
 int difr_mx4_quantize(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, uint8_t *codes, uint8_t *scales, void *hip_stream);
-/* The values that the first d elements of every row stand for, [N, ld] bf16 or fp32 (both hold them exactly). */
+/* The values that the first d elements of every row stand for, [N, ld] bf16 or fp32 (both hold them exactly; scale bytes of 253 and 254,
+ * which difr_mx4_quantize does not make, can stand for values beyond either, which come out as infinities). */
 int difr_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t N, int64_t d, void *x, int32_t dtype, int64_t ld,
                         void *hip_stream);
 /*
  * out[n][v] = sum_k a[n][k] b[v][k], fp32 accumulation on the matrix cores, rounded once to bf16 or fp32: the logits of N hidden states
- * under an LM head of V rows.  a: N rows, b: V rows of K = padded elements each (K % 128 == 0, else DIFR_ERR_SHAPE).  out [N, ld], ld >=
+ * under an LM head of V rows.  Sums below 2^-126, the smallest normal fp32 number, may come out as 0.  a: N rows, b: V rows of K = padded elements each (K % 128 == 0, else DIFR_ERR_SHAPE).  out [N, ld], ld >=
  * V, base aligned to its element size.  N, V <= 2^31 - 1024, N + V <= 2^29 - 1024 where N > 128, K < 2^24.
  * workspace  DEVICE scratch of at least difr_mx4_product_workspace_bytes(N, V, K) bytes (host only; 0: none is needed and NULL will do),
  * 16-byte aligned, contents irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small: DIFR_ERR_SHAPE.

@@ -8,9 +8,9 @@
 // wave and one ballot for each vector instead of a running maximum per thread.  In the end it is the row's largest, whose term is 1
 // exactly: S >= 1 and A <= 0, so no log-probability comes out above 0 and no entropy below, and where one token has nearly all of the
 // probability, S - 1 is what the others have.  (A reference up to 60 orders below the largest needs hardly a new one, but puts the error of an
-// exponent of that size on the largest term: of 256 rows with such a token 118 had a log-probability above 0.)  Rows in random order, 8192 x
-// 128,256 bf16, take the time that they take so, 310 us; rows that rise along the vocabulary, with a new maximum in every vector, 4096 x
-// 128,256 167 us instead of 153.
+// exponent of that size on the largest term: of 256 rows with such a token 118 had a log-probability above 0.)  Rows in random order
+// take no longer for it (8192 x 128,256 bf16 310 us either way), rows that rise along the vocabulary, with a new maximum in every vector, up
+// to a tenth (4096 x 128,256 167 us / 153, the policy loss 402 / 404).
 // C is held in two parts: one of 24 bits alone would move all exponents the same way.  The second is taken at a vector's largest logit, which
 // leaves 2^-23 of a term's distance from that and costs two operations for a vector.  The 16 bytes of a vector are summed in fp32, what
 // comes after that in 64 bits.  Error of the log-probabilities of 8192 x 128,256 bf16, T = 0.7, against 64 bits: 2.6e-8, as much as their rounding; with
