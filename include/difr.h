@@ -603,6 +603,93 @@ int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N,
                      int64_t V, int64_t K, void *out, int32_t dtype, int64_t ld, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * 4-bit integers with group scales, for heads that are served in them; weights only, hidden states stay as they are.
+ *   The elements of a row are in groups of `group` (32, 64 or 128), the first from element 0 on:  w = scale (code - zero), code and zero
+ *   point in 0 ... 15, scale a bf16 number.  A matrix without zero points has 8 everywhere.
+ *   codes  [rows, K / 2]: element 2 i in the lower half of byte i;  scales [rows, K / group] bf16;  zeros [rows, K / group] bytes, or
+ *   NULL;  all without gaps, codes aligned to 16 bytes, scales to 4, zeros to 2;  K is d rounded up to a multiple of 128 (difr_int4_padded), and
+ *   what codes say of elements from d on does not count.
+ * Quantisation.  Without zero points scale = (largest magnitude) / 7, else (hi - lo) / 15 with hi = max(largest, 0), lo = min(smallest, 0),
+ * and zero = -lo / scale rounded and held in 0 ... 15.  Quotients are fp32, the scale's is rounded to bf16, and code = x / scale rounded
+ * to a whole number (ties to even) + zero, held in 0 ... 15.  A group of zeros has scale 0, and zero point 0 if it has one.  A group with a NaN, an
+ * infinity or a difference beyond fp32 has the scale NaN and stands for NaN throughout.
+ */
+int64_t difr_int4_padded(int64_t d);
+/* x [N, ld] bf16 or fp32, base aligned to the element size -> codes, scales, and zeros (NULL: a matrix without).  d >= 1. */
+int difr_int4_quantize(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, int32_t group, uint8_t *codes, void *scales,
+                       uint8_t *zeros, void *hip_stream);
+/* The first d elements of every row, [N, ld] bf16 (rounded once) or fp32 (exact). */
+int difr_int4_dequantize(const uint8_t *codes, const void *scales, const uint8_t *zeros, int64_t N, int64_t d, int32_t group, void *x,
+                         int32_t dtype, int64_t ld, void *hip_stream);
+/*
+ * out[n][v] = sum_k hidden[n][k] w[v][k], k < d: the logits of N hidden states (bf16 or fp32, [N, ldh]) under a head of V rows.  Products
+ * of elements and codes are exact, accumulation and scaling are fp32, and the sum is rounded once to bf16 or fp32 ([N, ld], ld >= V).
+ * Meant for the few rows that are decoded together: the head is read once for every 64 of them (fp32: every 21).  Rows that hold a NaN, an infinity or
+ * magnitudes above 2^120 get NaN or infinities.  A row's result does not depend on the rows beside it.  V < 2^31, K < 2^24, bases aligned to the element size.
+ */
+int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64_t d, int64_t ldh, const uint8_t *codes, const void *scales,
+                      const uint8_t *zeros, int64_t V, int32_t group, void *out, int32_t dtype, int64_t ld, void *hip_stream);
+
+/*
+ * Verification of drafted tokens: a server that decodes speculatively has a cheap draft propose tokens, forms the target's logits at all
+ * of their positions at once, and keeps what the target's own distribution would give.  B sequences, D drafted tokens in all; sequence b
+ * has the tokens [offsets[b], offsets[b + 1]) and one row of logits more than tokens, rows offsets[b] + b ... offsets[b + 1] + b: row 0 is
+ * the position after the last token that is certain.  offsets [B + 1] is non-decreasing from 0 to D (what is outside is held in [0, D]).
+ * A masked logit (-inf, the type's lowest value) has no probability, and a masked token is never emitted.
+ * Weights of a row, exp((x - its largest logit) / T), and their sums are fp64, good to 2^-50; the result does not depend on the order in
+ * which workgroups run.  Random numbers are the caller's: fp32 in [0, 1); what is below (NaN too) counts as 0, what is above as the largest.
+ */
+typedef struct {
+    const void *logits;        /* [D + B, ld] the target's, base aligned to the element size */
+    int32_t dtype;
+    int64_t B, D, V, ld;
+    float temperature;
+    const float *temperatures; /* optional [D + B] */
+    const int32_t *tokens;     /* [D] the drafted tokens */
+    const int64_t *offsets;    /* [B + 1] */
+} difr_drafts;
+
+/*
+ * Chains: token i of a sequence was drawn from its draft's row i.  With p = softmax(x / T) of the target's row i, q = softmax(y / T') of the
+ * draft's (draft [D, ld_draft] in the logits' type; NULL: the draft is certain of its token, q = 1 there), token t stands if
+ *   accept_u q_t < p_t
+ * and the tokens before it stand.  Where the first one falls, the next token is drawn from max(p - q, 0) of its row; where all stand, from
+ * p of the row after the last: the first v at which the running sum, in the order of the vocabulary, exceeds sample_u times the whole.  So
+ * the emitted tokens are distributed as if drawn from p one by one.  (Where p - q leaves less than 2^-40 of the whole, p is drawn from.)
+ * A token outside [0, V) falls, DIFR_FLAG_INVALID_CLAIM, and the next one is drawn as for a token that has no probability under either.
+ * accept_u [D], sample_u [B].  draft_temperature > 0 finite, draft_temperatures [D] or NULL.
+ * Outputs: accepted [B] the number of tokens that stand; tokens [D + B]: at the sequence's rows, its accepted tokens, then the drawn one, then
+ * -1; logp [D + B] or NULL: ln p of each emitted token, 0 behind; flags [D + B]: DIFR_FLAG_MATCH on accepted tokens' rows.  A sequence that comes
+ * to a row, of the target or the draft, that holds a NaN, +inf or no finite logit, or whose temperature is not positive and finite, ends
+ * there: token -1, logp NaN, DIFR_FLAG_NONFINITE.  Rows that a sequence does not come to may hold anything.
+ * workspace  DEVICE scratch of difr_draft_workspace_bytes(B, D, V, dtype, draft != NULL) bytes (host only), 64-byte aligned, contents
+ * irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small: DIFR_ERR_SHAPE.  D + B rows of ceil(V / 2048)
+ * cells each: fewer than 2^26 cells.
+ */
+typedef struct {
+    const void *draft;
+    int64_t ld;
+    float temperature;
+    const float *temperatures;
+    const float *accept_u, *sample_u;
+} difr_draft_chain;
+
+size_t difr_draft_workspace_bytes(int64_t B, int64_t D, int64_t V, int32_t dtype, int32_t draft);
+int difr_draft_verify(const difr_drafts *in, const difr_draft_chain *chain, int32_t *accepted, int32_t *tokens, float *logp, uint8_t *flags,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Trees, whatever they were drafted by: parents [D] holds for each token the place in its sequence of the token before it, -1 for one that
+ * follows the root (the last certain token), or NULL: chains.  A token comes after its parent; one whose parent does not (or is below -1) is
+ * never reached.  The row after token j of a sequence is its row j + 1, the root's its row 0.  From the root on, a token is drawn from p of the
+ * row with the row's own sample_u [D + B], as above; if a token that follows holds it, the first of them is accepted and its row comes next, else
+ * the sequence ends.  So the emitted tokens are those that inverse-CDF sampling with these numbers gives without a draft.
+ * Outputs and workspace (draft = 0) as above, and nodes [D + B]: at the sequence's rows, the places of the accepted tokens, then -1.
+ */
+int difr_tree_verify(const difr_drafts *in, const int32_t *parents, const float *sample_u, int32_t *accepted, int32_t *tokens, int32_t *nodes,
+                     float *logp, uint8_t *flags, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Test and audit helper: difr_gumbel_score with the exact pre-filter switched off, so that
  * every vocabulary entry goes through both logarithms.  Same arguments, same outputs; the
  * two must agree bit for bit (the filter only skips entries that provably cannot reach the

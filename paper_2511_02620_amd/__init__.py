@@ -4,7 +4,8 @@ The product is ``libdifr.so`` (hand-written HIP kernels for gfx950 behind the C 
 ``include/difr.h``).  This package is only its Python binding: one function per entry
 point, with the entry point's name less the ``difr_`` prefix (``score_both``,
 ``gumbel_score``, ``ipt_score``, ``seq_reduce``, ``classify``, ``lmhead_score``,
-``token_logprob``, ``policy_loss``, ``preference_loss``, ``mx4_product``, ...).
+``token_logprob``, ``policy_loss``, ``preference_loss``, ``mx4_product``,
+``int4_product``, ``draft_verify``, ``tree_verify``, ...).
 Each marshals torch device tensors into the C call and returns torch tensors; every step
 of the computation runs in the library's kernels.  There is no CPU fallback: if the
 library is missing, ``load_library()`` - and with it every call - fails loudly.
@@ -20,8 +21,13 @@ from .binding import (  # noqa: F401
     classify,
     debug_gumbel_map,
     debug_noise,
+    draft_verify,
     gumbel_likelihood,
     gumbel_score,
+    int4_dequantize,
+    int4_padded,
+    int4_product,
+    int4_quantize,
     ipt_score,
     ipt_score_filtered,
     lib_path,
@@ -44,5 +50,6 @@ from .binding import (  # noqa: F401
     seq_reduce,
     token_logprob,
     token_logprob_backward,
+    tree_verify,
     version,
 )

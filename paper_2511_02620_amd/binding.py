@@ -101,9 +101,20 @@ class _Preference(C.Structure):
                 ("average", C.c_int32)]
 
 
+class _Drafts(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int32), ("B", C.c_int64), ("D", C.c_int64), ("V", C.c_int64), ("ld", C.c_int64),
+                ("temperature", C.c_float), ("temperatures", C.c_void_p), ("tokens", C.c_void_p), ("offsets", C.c_void_p)]
+
+
+class _DraftChain(C.Structure):
+    _fields_ = [("draft", C.c_void_p), ("ld", C.c_int64), ("temperature", C.c_float), ("temperatures", C.c_void_p),
+                ("accept_u", C.c_void_p), ("sample_u", C.c_void_p)]
+
+
 EXPORTS = ("difr_gumbel_score", "difr_debug_gumbel_score_unfiltered", "difr_ipt_score", "difr_score_both", "difr_score_both_peaked", "difr_score_both_admissible", "difr_admissible_count", "difr_gumbel_likelihood", "difr_ipt_score_filtered", "difr_score_both_filtered", "difr_lmhead_score", "difr_lmhead_score_static", "difr_lmhead_workspace_bytes", "difr_split_workspace_bytes", "difr_score_split", "difr_classify", "difr_seq_reduce",
            "difr_token_workspace_bytes", "difr_token_logprob", "difr_token_logprob_backward", "difr_policy_loss", "difr_preference_loss", "difr_mx4_padded",
-           "difr_mx4_quantize", "difr_mx4_dequantize", "difr_mx4_product_workspace_bytes", "difr_mx4_product", "difr_debug_noise", "difr_debug_gumbel_map",
+           "difr_mx4_quantize", "difr_mx4_dequantize", "difr_mx4_product_workspace_bytes", "difr_mx4_product", "difr_int4_padded", "difr_int4_quantize", "difr_int4_dequantize",
+           "difr_int4_product", "difr_draft_workspace_bytes", "difr_draft_verify", "difr_tree_verify", "difr_debug_noise", "difr_debug_gumbel_map",
            "difr_philox4x32_10", "difr_status_string", "difr_version")
 
 
@@ -170,8 +181,18 @@ def load_library():
     lib.difr_mx4_product_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int64]
     lib.difr_mx4_product_workspace_bytes.restype = C.c_size_t
     lib.difr_mx4_product.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_int64, C.c_int64, vp, C.c_int32, C.c_int64, vp, C.c_size_t, vp]
+    i32, i64 = C.c_int32, C.c_int64
+    lib.difr_int4_padded.argtypes = [i64]
+    lib.difr_int4_padded.restype = i64
+    lib.difr_int4_quantize.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp, vp, vp]
+    lib.difr_int4_dequantize.argtypes = [vp, vp, vp, i64, i64, i32, vp, i32, i64, vp]
+    lib.difr_int4_product.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i64, i32, vp, i32, i64, vp]
+    lib.difr_draft_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.difr_draft_workspace_bytes.restype = C.c_size_t
+    lib.difr_draft_verify.argtypes = [C.POINTER(_Drafts), C.POINTER(_DraftChain)] + [vp] * 5 + [C.c_size_t, vp]
+    lib.difr_tree_verify.argtypes = [C.POINTER(_Drafts)] + [vp] * 8 + [C.c_size_t, vp]
     for name in ("token_logprob", "token_logprob_backward", "policy_loss", "preference_loss", "mx4_quantize", "mx4_dequantize",
-                 "mx4_product"):
+                 "mx4_product", "int4_quantize", "int4_dequantize", "int4_product", "draft_verify", "tree_verify"):
         getattr(lib, "difr_" + name).restype = C.c_int
     lib.difr_debug_noise.argtypes = [C.POINTER(_Rows), C.c_int64, C.c_int32, vp, vp]
     lib.difr_debug_noise.restype = C.c_int
@@ -738,6 +759,146 @@ def mx4_product(a_codes, a_scales, b_codes, b_scales, dtype=torch.bfloat16, out=
             raise ValueError("out must be a [%d, %d] %s tensor with unit column stride on the device of the codes" % (
                 a_codes.shape[0], b_codes.shape[0], dtype))
         _refused("difr_mx4_product", got, checks)
+    return got
+
+
+def int4_padded(d) -> int:
+    """difr_int4_padded: elements of a row of codes for rows of d elements (whole slabs of 128)."""
+    return int(load_library().difr_int4_padded(int(d)))
+
+
+def _check_group(group):
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    return int(group)
+
+
+def int4_quantize(x, group=128, zero_points=False):
+    """difr_int4_quantize: the rows of x [N, d] (bf16/fp32 on the GPU, unit column stride) in 4-bit integers, a scale for each `group`
+    elements of a row.  Returns a dict: codes uint8 [N, K / 2], two elements a byte, scales bf16 [N, K / group], and with zero_points
+    zeros uint8 [N, K / group], K = int4_padded(d)."""
+    got = (_native or _load_native()).int4_quantize(x, _check_group(group), zero_points)
+    if got.__class__ is not dict:
+        def checks():
+            _need_tensors(x=x)
+            if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+                raise ValueError("x must be a 2-D bfloat16 or float32 GPU tensor with unit column stride")
+        _refused("difr_int4_quantize", got, checks)
+    return got
+
+
+def _check_int4(codes, scales, zeros):
+    _need_tensors(codes=codes, scales=scales)
+    if not codes.is_cuda or codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_contiguous() or codes.shape[1] % 64 or not codes.shape[1]:
+        raise ValueError("codes must be a contiguous [rows, K / 2] uint8 GPU tensor, K a multiple of 128")
+    if (scales.device != codes.device or scales.dtype != torch.bfloat16 or scales.dim() != 2 or not scales.is_contiguous()
+            or scales.shape[0] != codes.shape[0] or 2 * codes.shape[1] not in [g * scales.shape[1] for g in (32, 64, 128)]):
+        raise ValueError("scales must be a contiguous [%d, K / group] bfloat16 tensor on the device of the codes, group 32, 64 or 128" % (
+            codes.shape[0]))
+    if zeros is None:
+        return
+    _need_tensors(zeros=zeros)
+    if zeros.device != codes.device or zeros.dtype != torch.uint8 or zeros.shape != scales.shape or not zeros.is_contiguous():
+        raise ValueError("zeros must be a contiguous [%d, %d] uint8 tensor on the device of the codes" % tuple(scales.shape))
+
+
+def int4_dequantize(codes, scales, columns, zeros=None, dtype=torch.bfloat16):
+    """difr_int4_dequantize: the values [rows, columns] that codes, scales and zero points stand for (exact in fp32)."""
+    got = (_native or _load_native()).int4_dequantize(codes, scales, zeros, int(columns), _check_float_type(dtype))
+    if got is None or got.__class__ is int:
+        def checks():
+            _check_int4(codes, scales, zeros)
+            raise ValueError("columns must be a number of elements whose rows have codes for %d" % (2 * codes.shape[1]))
+        _refused("difr_int4_dequantize", got, checks)
+    return got
+
+
+def int4_product(hidden, codes, scales, zeros=None, dtype=torch.bfloat16, out=None):
+    """difr_int4_product: [N, V] products of the N rows of hidden [N, d] (bf16/fp32, unit column stride) and the V rows of a matrix as
+    :func:`int4_quantize` returns it.  out: a [N, V] tensor of that dtype (unit column stride) to write into."""
+    got = (_native or _load_native()).int4_product(hidden, codes, scales, zeros, _check_float_type(dtype), out)
+    if got is None or got.__class__ is int:
+        def checks():
+            _need_tensors(hidden=hidden)
+            _check_int4(codes, scales, zeros)
+            if (hidden.device != codes.device or hidden.dtype not in (torch.bfloat16, torch.float32) or hidden.dim() != 2
+                    or (hidden.shape[1] > 1 and hidden.stride(1) != 1) or (hidden.shape[0] > 1 and hidden.stride(0) < hidden.shape[1])
+                    or int4_padded(hidden.shape[1]) != 2 * codes.shape[1]):
+                raise ValueError("hidden must be a 2-D bfloat16 or float32 tensor with unit column stride on the device of the codes, its rows "
+                                 "of a number of elements that have codes for %d" % (2 * codes.shape[1]))
+            if out is not None:
+                _need_tensors(out=out)
+            raise ValueError("out must be a [%d, %d] %s tensor with unit column stride on the device of the codes" % (
+                hidden.shape[0], codes.shape[0], dtype))
+        _refused("difr_int4_product", got, checks)
+    return got
+
+
+def _check_drafts(logits, V, tokens, offsets, temperatures):
+    """Checks of the calls on drafted tokens; (device, sequences, drafted tokens, rows, vocabulary)."""
+    _need_tensors(logits=logits, tokens=tokens, offsets=offsets)
+    if not logits.is_cuda:
+        raise ValueError("logits must be a GPU tensor")
+    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
+        raise ValueError("logits must be 2-D with unit column stride")
+    if logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be bfloat16 or float32")
+    dev, R = logits.device, logits.shape[0]
+    if offsets.device != dev or offsets.dtype != torch.int64 or offsets.dim() != 1 or not offsets.is_contiguous() or not offsets.shape[0]:
+        raise ValueError("offsets must be a contiguous 1-D int64 GPU tensor of B+1 elements")
+    B = offsets.shape[0] - 1
+    if R < B:
+        raise ValueError("logits must have a row for each drafted token and one more for each sequence")
+    _check(tokens, torch.int32, R - B, "tokens", dev)
+    _check(temperatures, torch.float32, R, "temperatures", dev)
+    if V is not None and int(V) > logits.shape[1]:
+        raise ValueError("V must be at most %d, the columns of logits" % logits.shape[1])
+    return dev, B, R - B, R, logits.shape[1] if V is None else int(V)
+
+
+def draft_verify(logits, temperature, tokens, offsets, accept_u, sample_u, draft=None, draft_temperature=None, temperatures=None,
+                 draft_temperatures=None, V=None):
+    """difr_draft_verify: which of the drafted tokens (int32 [D], those of sequence b at offsets[b] ... offsets[b + 1], int64 [B + 1])
+    stand, and the token that follows.  logits [D + B, >=V] bf16/fp32 on the GPU: one row more than tokens for each sequence; draft
+    [D, >=V] in the same type, or None for drafts without a distribution; accept_u fp32 [D], sample_u fp32 [B] in [0, 1).
+    draft_temperature None: `temperature` (with temperatures per row the drafts need their own).  Returns a dict of device tensors:
+    accepted int32 [B], tokens int32 [D + B] (accepted tokens, the drawn one, -1), logp, flags [D + B]."""
+    if draft is not None and temperatures is not None and draft_temperature is None and draft_temperatures is None:
+        raise ValueError("rows with temperatures of their own need draft_temperatures (or draft_temperature) for the drafts")
+    got = (_native or _load_native()).draft_verify(logits, V if V is None else int(V), float(temperature), tokens, offsets, temperatures,
+                                                   accept_u, sample_u, draft,
+                                                   float(temperature if draft_temperature is None else draft_temperature),
+                                                   draft_temperatures)
+    if got.__class__ is not dict:
+        def checks():
+            dev, B, D, _, cols = _check_drafts(logits, V, tokens, offsets, temperatures)
+            _need_tensors(accept_u=accept_u, sample_u=sample_u)
+            _check(accept_u, torch.float32, D, "accept_u", dev)
+            _check(sample_u, torch.float32, B, "sample_u", dev)
+            if draft is not None:
+                _need_tensors(draft=draft)
+                if (draft.device != dev or draft.dtype != logits.dtype or draft.dim() != 2 or draft.shape[0] != D or draft.shape[1] < cols
+                        or (draft.shape[1] > 1 and draft.stride(1) != 1)):
+                    raise ValueError("draft must be a [%d, >=%d] %s tensor with unit column stride on %s" % (D, cols, logits.dtype, dev))
+            _check(draft_temperatures, torch.float32, D, "draft_temperatures", dev)
+        _refused("difr_draft_verify", got, checks)
+    return got
+
+
+def tree_verify(logits, temperature, tokens, parents, offsets, sample_u, temperatures=None, V=None):
+    """difr_tree_verify: the path that tokens drawn row by row take through each sequence's tree of drafted tokens.  parents int32 [D]:
+    the place in its sequence of the token before each, -1 for those that come first (None: chains); row 0 of a sequence's logits is the
+    root's, row j + 1 that of token j; sample_u fp32 [D + B], one for each row.  Returns a dict of device tensors: accepted int32 [B],
+    tokens int32 [D + B] (the drawn tokens, -1 behind), nodes int32 [D + B] (places of the accepted tokens, -1 behind), logp, flags."""
+    got = (_native or _load_native()).tree_verify(logits, V if V is None else int(V), float(temperature), tokens, offsets, temperatures,
+                                                  parents, sample_u)
+    if got.__class__ is not dict:
+        def checks():
+            dev, B, D, R, _ = _check_drafts(logits, V, tokens, offsets, temperatures)
+            _need_tensors(sample_u=sample_u)
+            _check(parents, torch.int32, D, "parents", dev)
+            _check(sample_u, torch.float32, R, "sample_u", dev)
+        _refused("difr_tree_verify", got, checks)
     return got
 
 

@@ -8,7 +8,9 @@
 #include "../../include/difr.h"
 #include "difr_device.hpp"
 #include "difr_host.hpp"
+#include "draft_verify.hpp"
 #include "gumbel_stream.hpp"
+#include "int4.hpp"
 #include "ipt_stream.hpp"
 #include "lmhead.hpp"
 #include "token_loss.hpp"
@@ -621,6 +623,129 @@ int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N,
     int rc = check_device();
     if (rc != DIFR_OK) return rc;
     return difr::launch_mx4_product(a_codes, a_scales, N, b_codes, b_scales, V, K, out, dtype, ld, workspace, (hipStream_t)hip_stream)
+               ? DIFR_ERR_LAUNCH
+               : DIFR_OK;
+}
+
+int64_t difr_int4_padded(int64_t d) { return d <= 0 ? 0 : (d + difr::kInt4Slab - 1) / difr::kInt4Slab * difr::kInt4Slab; }
+
+static int element_size(int32_t dtype) { return dtype == DIFR_BF16 ? 2 : 4; }
+
+// A matrix in 4-bit integers of N rows and a dense one beside it (x: its elements, quantised, dequantised or multiplied by it).
+static int validate_int4(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, int32_t group, const uint8_t *codes,
+                         const void *scales, const uint8_t *zeros, difr::Int4Matrix *m)
+{
+    if (N < 0 || d < 1 || ld < d || N >= (int64_t)1 << 31 || d >= (int64_t)1 << 24) return DIFR_ERR_SHAPE;
+    if (group != 32 && group != 64 && group != 128) return DIFR_ERR_ARGUMENT;
+    if (dtype != DIFR_BF16 && dtype != DIFR_F32) return DIFR_ERR_DTYPE;
+    if (N == 0) return DIFR_OK;
+    if (!x || !codes || !scales) return DIFR_ERR_NULL;
+    if ((uintptr_t)x % element_size(dtype) || (uintptr_t)codes % 16u || (uintptr_t)scales % 4u || (uintptr_t)zeros % 2u) return DIFR_ERR_ALIGN;
+    *m = difr::Int4Matrix{codes, (const uint16_t *)scales, zeros, N, difr_int4_padded(d), group};
+    return DIFR_OK;
+}
+
+int difr_int4_quantize(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, int32_t group, uint8_t *codes, void *scales,
+                       uint8_t *zeros, void *hip_stream)
+{
+    difr::Int4Matrix m;
+    int rc = validate_int4(x, dtype, N, d, ld, group, codes, scales, zeros, &m);
+    if (rc != DIFR_OK || N == 0) return rc;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_int4_quantize(x, dtype, N, d, ld, group, codes, (uint16_t *)scales, zeros, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH
+                                                                                                                        : DIFR_OK;
+}
+
+int difr_int4_dequantize(const uint8_t *codes, const void *scales, const uint8_t *zeros, int64_t N, int64_t d, int32_t group, void *x,
+                         int32_t dtype, int64_t ld, void *hip_stream)
+{
+    difr::Int4Matrix m;
+    int rc = validate_int4(x, dtype, N, d, ld, group, codes, scales, zeros, &m);
+    if (rc != DIFR_OK || N == 0) return rc;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_int4_dequantize(m, d, x, dtype, ld, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+}
+
+int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64_t d, int64_t ldh, const uint8_t *codes, const void *scales,
+                      const uint8_t *zeros, int64_t V, int32_t group, void *out, int32_t dtype, int64_t ld, void *hip_stream)
+{
+    if (N < 0 || N >= (int64_t)1 << 31 || V < 0 || V >= (int64_t)1 << 31 || ldh < d || ld < V) return DIFR_ERR_SHAPE;
+    if (hidden_dtype != DIFR_BF16 && hidden_dtype != DIFR_F32) return DIFR_ERR_DTYPE;
+    difr::Int4Matrix m;
+    int rc = validate_int4(out, dtype, N ? V : 0, d, d, group, codes, scales, zeros, &m);
+    if (rc != DIFR_OK || N == 0 || V == 0) return rc;
+    if (!hidden) return DIFR_ERR_NULL;
+    if ((uintptr_t)hidden % element_size(hidden_dtype)) return DIFR_ERR_ALIGN;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_int4_product(hidden, hidden_dtype, N, d, ldh, m, out, dtype, ld, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+}
+
+static int validate_drafts(const difr_drafts *in, difr::DraftBatch *b)
+{
+    if (!in) return DIFR_ERR_NULL;
+    const int64_t most = (int64_t)1 << 31;
+    if (in->B < 0 || in->D < 0 || in->V < 0 || in->ld < 0 || in->B >= most || in->D >= most || in->V >= most) return DIFR_ERR_SHAPE;
+    if (in->dtype != DIFR_BF16 && in->dtype != DIFR_F32) return DIFR_ERR_DTYPE;
+    if (in->B == 0 && in->D > 0) return DIFR_ERR_SHAPE;
+    if (in->B > 0) {
+        if (in->V == 0 || in->ld < in->V || !difr::draft_shape(in->B, in->D, in->V)) return DIFR_ERR_SHAPE;
+        if (!in->logits || !in->offsets || (in->D > 0 && !in->tokens)) return DIFR_ERR_NULL;
+        if (!in->temperatures && !(in->temperature > 0.0f && isfinite(in->temperature))) return DIFR_ERR_TEMPERATURE;
+        if ((uintptr_t)in->logits % element_size(in->dtype)) return DIFR_ERR_ALIGN;
+    }
+    *b = difr::DraftBatch{in->logits, in->dtype, in->B, in->D, in->V, in->ld, in->temperature, in->temperatures, in->tokens, in->offsets};
+    return DIFR_OK;
+}
+
+size_t difr_draft_workspace_bytes(int64_t B, int64_t D, int64_t V, int32_t dtype, int32_t draft)
+{
+    if (B < 1 || D < 0 || V < 1 || B >= (int64_t)1 << 31 || D >= (int64_t)1 << 31 || V >= (int64_t)1 << 31 ||
+        (dtype != DIFR_BF16 && dtype != DIFR_F32) || !difr::draft_shape(B, D, V))
+        return 0;
+    return difr::draft_workspace_bytes(B, D, V, draft != 0);
+}
+
+static int check_draft_workspace(const difr::DraftBatch &b, bool draft, const void *workspace, size_t workspace_bytes)
+{
+    if (workspace_bytes < difr::draft_workspace_bytes(b.B, b.D, b.V, draft)) return DIFR_ERR_SHAPE;
+    if (!workspace) return DIFR_ERR_NULL;
+    return (uintptr_t)workspace % 64u ? DIFR_ERR_ALIGN : DIFR_OK;
+}
+
+int difr_draft_verify(const difr_drafts *in, const difr_draft_chain *chain, int32_t *accepted, int32_t *tokens, float *logp, uint8_t *flags,
+                      void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    difr::DraftBatch b;
+    int rc = validate_drafts(in, &b);
+    if (rc != DIFR_OK) return rc;
+    if (!chain) return DIFR_ERR_NULL;
+    const bool draft = chain->draft && b.D > 0;
+    if (b.B == 0) return DIFR_OK;
+    if (!accepted || !tokens || !flags || !chain->sample_u || (b.D > 0 && !chain->accept_u)) return DIFR_ERR_NULL;
+    if (draft) {
+        if (chain->ld < b.V) return DIFR_ERR_SHAPE;
+        if (!chain->temperatures && !(chain->temperature > 0.0f && isfinite(chain->temperature))) return DIFR_ERR_TEMPERATURE;
+        if ((uintptr_t)chain->draft % element_size(b.dtype)) return DIFR_ERR_ALIGN;
+    }
+    if ((rc = check_draft_workspace(b, draft, workspace, workspace_bytes)) != DIFR_OK) return rc;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    const difr::DraftChain c{draft ? chain->draft : nullptr, chain->ld, chain->temperature, chain->temperatures, chain->accept_u, chain->sample_u};
+    return difr::launch_draft_verify(b, c, difr::DraftOutputs{accepted, tokens, nullptr, logp, flags}, workspace, (hipStream_t)hip_stream)
+               ? DIFR_ERR_LAUNCH
+               : DIFR_OK;
+}
+
+int difr_tree_verify(const difr_drafts *in, const int32_t *parents, const float *sample_u, int32_t *accepted, int32_t *tokens, int32_t *nodes,
+                     float *logp, uint8_t *flags, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    difr::DraftBatch b;
+    int rc = validate_drafts(in, &b);
+    if (rc != DIFR_OK || b.B == 0) return rc;
+    if (!sample_u || !accepted || !tokens || !nodes || !flags) return DIFR_ERR_NULL;
+    if ((rc = check_draft_workspace(b, false, workspace, workspace_bytes)) != DIFR_OK) return rc;
+    if ((rc = check_device()) != DIFR_OK) return rc;
+    return difr::launch_tree_verify(b, difr::DraftTree{parents, sample_u}, difr::DraftOutputs{accepted, tokens, nodes, logp, flags}, workspace,
+                                    (hipStream_t)hip_stream)
                ? DIFR_ERR_LAUNCH
                : DIFR_OK;
 }

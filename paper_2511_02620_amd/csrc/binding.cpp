@@ -51,7 +51,14 @@ namespace {
     X(difr_mx4_quantize)                                                                                                \
     X(difr_mx4_dequantize)                                                                                              \
     X(difr_mx4_product_workspace_bytes)                                                                                 \
-    X(difr_mx4_product)
+    X(difr_mx4_product)                                                                                                 \
+    X(difr_int4_padded)                                                                                                 \
+    X(difr_int4_quantize)                                                                                               \
+    X(difr_int4_dequantize)                                                                                             \
+    X(difr_int4_product)                                                                                                \
+    X(difr_draft_workspace_bytes)                                                                                       \
+    X(difr_draft_verify)                                                                                                \
+    X(difr_tree_verify)
 
 struct Entries {
 #define X(name) decltype(&::name) name = nullptr;
@@ -64,7 +71,7 @@ struct Entries {
     X(margin) X(argmax) X(max_score) X(claimed_score) X(flags) X(logit_rank) X(dist) X(cdf_lo) X(cdf_hi) X(u)           \
     X(ipt_token) X(log_mass) X(count) X(log2_count) X(kept) X(pi) X(log_pi) X(tau) X(active) X(seq_mean) X(seq_max)     \
     X(seq_mismatch) X(seq_flag) X(cls) X(bits) X(logp) X(stats) X(entropy) X(loss) X(token_loss) X(kl) X(grad)           \
-    X(grad_logp) X(pair_loss) X(seq_logp) X(codes) X(scales)
+    X(grad_logp) X(pair_loss) X(seq_logp) X(codes) X(scales) X(zeros) X(accepted) X(tokens) X(nodes)
 namespace key {
 #define X(name) PyObject *name = nullptr;
 DIFR_KEYS(X)
@@ -815,6 +822,180 @@ PyObject *mx4_product(PyObject *const *a)
     return wrapped(rc, t);
 }
 
+// ---- 4-bit integers ----
+
+// [rows, K / 2] codes, [rows, K / group] scales, and zero points or None
+struct Coded4 {
+    const uint8_t *codes, *zeros = nullptr;
+    const void *scales;
+    int64_t rows, K, group;
+    c10::Device dev;
+    Coded4(PyObject *c, PyObject *s, PyObject *z) : dev(c10::kCUDA)
+    {
+        const at::Tensor &x = tensor(c), &y = tensor(s);
+        if (!x.is_cuda() || x.scalar_type() != at::kByte || x.dim() != 2 || !x.is_contiguous()) throw Refused();
+        dev = x.device();
+        rows = x.size(0), K = 2 * x.size(1);
+        if (y.device() != dev || y.scalar_type() != at::kBFloat16 || y.dim() != 2 || !y.is_contiguous() || y.size(0) != rows || !K ||
+            K % 128 || !y.size(1) || K % y.size(1))
+            throw Refused();
+        group = K / y.size(1);
+        if (group != 32 && group != 64 && group != 128) throw Refused();
+        codes = (const uint8_t *)x.data_ptr(), scales = y.data_ptr();
+        if (z == Py_None) return;
+        const at::Tensor &t = tensor(z);
+        if (t.device() != dev || t.scalar_type() != at::kByte || t.dim() != 2 || !t.is_contiguous() || t.size(0) != rows || t.size(1) != y.size(1))
+            throw Refused();
+        zeros = (const uint8_t *)t.data_ptr();
+    }
+};
+
+// x, group, zero_points
+PyObject *int4_quantize(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[0]);
+    if (!x.is_cuda() || x.dim() != 2 || (x.stride(1) != 1 && x.size(1) > 1)) throw Refused();
+    const int32_t dtype = float_type(x.scalar_type());
+    const int64_t N = x.size(0), d = x.size(1), K = lib.difr_int4_padded(d), group = whole(a[1]);
+    if (group != 32 && group != 64 && group != 128) throw Refused();
+    const int64_t ld = N > 1 ? x.stride(0) : d;
+    Outputs o(x.device());
+    uint8_t *codes = (uint8_t *)o.add(key::codes, at::kByte, {N, K / 2});
+    void *scales = o.add(key::scales, at::kBFloat16, {N, K / group});
+    uint8_t *zeros = truth(a[2]) ? (uint8_t *)o.add(key::zeros, at::kByte, {N, K / group}) : nullptr;
+    return one(enter(x.device(), [&](void *s) { return lib.difr_int4_quantize(x.data_ptr(), dtype, N, d, ld, (int32_t)group, codes, scales, zeros, s); }), o);
+}
+
+// codes, scales, zeros, columns, fp32
+PyObject *int4_dequantize(PyObject *const *a)
+{
+    const Coded4 c(a[0], a[1], a[2]);
+    const int64_t d = whole(a[3]);
+    if (d < 1 || lib.difr_int4_padded(d) != c.K) throw Refused();
+    const bool f32 = truth(a[4]);
+    Outputs o(c.dev);
+    at::Tensor t = o.make(f32 ? at::kFloat : at::kBFloat16, {c.rows, d});
+    const int rc = enter(c.dev, [&](void *s) {
+        return lib.difr_int4_dequantize(c.codes, c.scales, c.zeros, c.rows, d, (int32_t)c.group, t.data_ptr(), f32 ? DIFR_F32 : DIFR_BF16, d, s);
+    });
+    return wrapped(rc, t);
+}
+
+// hidden, codes, scales, zeros, fp32, out
+PyObject *int4_product(PyObject *const *a)
+{
+    const at::Tensor &h = tensor(a[0]);
+    const Coded4 c(a[1], a[2], a[3]);
+    if (h.device() != c.dev || h.dim() != 2 || (h.stride(1) != 1 && h.size(1) > 1)) throw Refused();
+    const int32_t type = float_type(h.scalar_type());
+    const int64_t N = h.size(0), d = h.size(1), ldh = N > 1 ? h.stride(0) : d;
+    if (d < 1 || lib.difr_int4_padded(d) != c.K || ldh < d) throw Refused();
+    const bool f32 = truth(a[4]);
+    Outputs o(c.dev);
+    at::Tensor t;
+    int64_t ld = c.rows;
+    if (a[5] == Py_None) {
+        t = o.make(f32 ? at::kFloat : at::kBFloat16, {N, c.rows});
+    } else {
+        t = tensor(a[5]);
+        if (t.device() != c.dev || t.scalar_type() != (f32 ? at::kFloat : at::kBFloat16) || t.dim() != 2 || t.size(0) != N || t.size(1) != c.rows ||
+            (t.stride(1) != 1 && c.rows > 1) || (N > 1 && t.stride(0) < c.rows))
+            throw Refused();
+        if (N > 1) ld = t.stride(0);
+    }
+    const int rc = enter(c.dev, [&](void *s) {
+        return lib.difr_int4_product(h.data_ptr(), type, N, d, ldh, c.codes, c.scales, c.zeros, c.rows, (int32_t)c.group, t.data_ptr(),
+                                     f32 ? DIFR_F32 : DIFR_BF16, ld, s);
+    });
+    if (a[5] != Py_None) written(rc, t);
+    return wrapped(rc, t);
+}
+
+// ---- drafted tokens ----
+
+// The first six arguments of these calls: logits, V, temperature, tokens, offsets, temperatures.
+struct Drafts {
+    difr_drafts in;
+    int64_t R;
+    c10::Device dev;
+    at::ScalarType type;
+    explicit Drafts(PyObject *const *a) : dev(c10::kCUDA)
+    {
+        const at::Tensor &x = tensor(a[0]), &off = tensor(a[4]);
+        if (!x.is_cuda() || x.dim() != 2 || (x.stride(1) != 1 && x.size(1) > 1)) throw Refused();
+        type = x.scalar_type();
+        in.dtype = float_type(type);
+        dev = x.device();
+        in.offsets = (const int64_t *)vec(a[4], at::kLong, -1, dev);
+        in.B = off.size(0) - 1;
+        in.tokens = (const int32_t *)vec(a[3], at::kInt, -1, dev);
+        in.D = tensor(a[3]).size(0);
+        R = x.size(0);
+        if (in.B < 0 || R != in.D + in.B) throw Refused();
+        in.logits = x.data_ptr();
+        in.V = a[1] == Py_None ? x.size(1) : whole(a[1]);
+        if (in.V > x.size(1)) throw Refused();
+        in.ld = R > 1 ? x.stride(0) : std::max(x.size(1), R ? x.stride(0) : (int64_t)0);
+        in.temperature = (float)number(a[2]);
+        in.temperatures = (const float *)vec_or_null(a[5], at::kFloat, R, dev);
+    }
+};
+constexpr int kDraftArgs = 6;
+
+struct DraftScratch {
+    at::Tensor t;
+    void *data = nullptr;
+    size_t bytes;
+    DraftScratch(const Drafts &r, bool draft, Outputs &o) : bytes(lib.difr_draft_workspace_bytes(r.in.B, r.in.D, r.in.V, r.in.dtype, draft))
+    {
+        if (!bytes) return;
+        t = o.make(at::kByte, {(int64_t)bytes});
+        data = t.data_ptr();
+    }
+};
+
+// drafts, accept_u, sample_u, draft, draft_temperature, draft_temperatures
+PyObject *draft_verify(PyObject *const *a)
+{
+    const Drafts r(a);
+    a += kDraftArgs;
+    difr_draft_chain c;
+    c.accept_u = (const float *)vec(a[0], at::kFloat, r.in.D, r.dev);
+    c.sample_u = (const float *)vec(a[1], at::kFloat, r.in.B, r.dev);
+    c.draft = nullptr, c.ld = r.in.V;
+    if (a[2] != Py_None) {
+        const at::Tensor &y = tensor(a[2]);
+        if (y.device() != r.dev || y.scalar_type() != r.type || y.dim() != 2 || y.size(0) != r.in.D || y.size(1) < r.in.V ||
+            (y.stride(1) != 1 && y.size(1) > 1))
+            throw Refused();
+        c.draft = r.in.D ? y.data_ptr() : nullptr;
+        c.ld = r.in.D > 1 ? y.stride(0) : std::max(y.size(1), r.in.D ? y.stride(0) : (int64_t)0);
+    }
+    c.temperature = (float)number(a[3]);
+    c.temperatures = (const float *)vec_or_null(a[4], at::kFloat, r.in.D, r.dev);
+    Outputs o(r.dev);
+    int32_t *accepted = o.i32(key::accepted, r.in.B), *tokens = o.i32(key::tokens, r.R);
+    float *logp = o.f32(key::logp, r.R);
+    uint8_t *flags = o.u8(key::flags, r.R);
+    const DraftScratch w(r, c.draft != nullptr, o);
+    return one(enter(r.dev, [&](void *s) { return lib.difr_draft_verify(&r.in, &c, accepted, tokens, logp, flags, w.data, w.bytes, s); }), o);
+}
+
+// drafts, parents, sample_u
+PyObject *tree_verify(PyObject *const *a)
+{
+    const Drafts r(a);
+    a += kDraftArgs;
+    const int32_t *parents = (const int32_t *)vec_or_null(a[0], at::kInt, r.in.D, r.dev);
+    const float *u = (const float *)vec(a[1], at::kFloat, r.R, r.dev);
+    Outputs o(r.dev);
+    int32_t *accepted = o.i32(key::accepted, r.in.B), *tokens = o.i32(key::tokens, r.R), *nodes = o.i32(key::nodes, r.R);
+    float *logp = o.f32(key::logp, r.R);
+    uint8_t *flags = o.u8(key::flags, r.R);
+    const DraftScratch w(r, false, o);
+    return one(enter(r.dev, [&](void *s) { return lib.difr_tree_verify(&r.in, parents, u, accepted, tokens, nodes, logp, flags, w.data, w.bytes, s); }), o);
+}
+
 // ---- module ----
 
 template <PyObject *(*F)(PyObject *const *), int N>
@@ -877,6 +1058,11 @@ PyMethodDef methods[] = {
     method<mx4_quantize, 1>("mx4_quantize"),
     method<mx4_dequantize, 4>("mx4_dequantize"),
     method<mx4_product, 6>("mx4_product"),
+    method<int4_quantize, 3>("int4_quantize"),
+    method<int4_dequantize, 5>("int4_dequantize"),
+    method<int4_product, 6>("int4_product"),
+    method<draft_verify, kDraftArgs + 5>("draft_verify"),
+    method<tree_verify, kDraftArgs + 2>("tree_verify"),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,0 +1,161 @@
+"""4-bit integers with group scales against their definition: codes, values, and products of a few hidden states."""
+import math
+
+import pytest
+import torch
+
+import draft_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def difr():
+    import paper_2511_02620_amd as m
+    m.load_library()
+    return m
+
+
+def _same(a, b):
+    return torch.equal(a.cpu().double().nan_to_num(nan=-77.0), b.double().nan_to_num(nan=-77.0))
+
+
+def _rows(t, offset, gap, fill=math.nan):
+    """The tensor on the device as a view whose rows start anywhere; what lies between them is `fill`."""
+    N, d = t.shape
+    buf = torch.full((offset + N * (d + gap),), fill, dtype=t.dtype, device=DEV)
+    view = buf[offset:].view(N, d + gap)[:, :d]
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("N,d", [(1, 1), (3, 31), (2, 32), (5, 63), (4, 128), (2, 129), (7, 1000), (33, 4096)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group,zero_points,offset,gap", [(32, True, 0, 0), (64, False, 1, 0), (128, True, 5, 3), (128, False, 0, 0), (64, True, 2, 1)])
+def test_quantize_and_back(difr, N, d, dtype, group, zero_points, offset, gap):
+    g = torch.Generator().manual_seed(N * 100 + d)
+    x = (torch.randn(N, d, generator=g) * (2 * torch.randn(N, 1, generator=g)).exp() + 0.3).to(dtype)
+    codes, scales, zeros, values = ref.int4(x, group, zero_points)
+    q = difr.int4_quantize(_rows(x, offset, gap), group=group, zero_points=zero_points)
+    assert torch.equal(q["codes"].cpu(), codes) and torch.equal(q["scales"].cpu().view(torch.int16), scales.view(torch.int16))
+    assert ("zeros" in q) == zero_points and (not zero_points or torch.equal(q["zeros"].cpu(), zeros))
+    assert _same(difr.int4_dequantize(q["codes"], q["scales"], d, q.get("zeros"), dtype=torch.float32), values[:, :d])
+    assert _same(difr.int4_dequantize(q["codes"], q["scales"], d, q.get("zeros")), values[:, :d].to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("zero_points", [False, True])
+def test_groups_that_are_special(difr, zero_points):
+    half = torch.arange(-16, 16).float()
+    rows = [half / 2, half / 2 + 0.25, torch.zeros(32), -torch.zeros(32), half.abs(), -half.abs(), half * 2.0 ** -120, half * 2.0 ** -140,
+            half * 2.0 ** 120, torch.full((32,), 3.0), torch.full((32,), -3.0), torch.full((32,), 3e38)]
+    for bad in (math.nan, math.inf, -math.inf):
+        r = half.clone()
+        r[5] = bad
+        rows.append(r)
+    huge = torch.full((32,), 3e38)
+    huge[::2] = -3e38                                   # a difference beyond fp32
+    rows.append(huge)
+    x = torch.stack(rows)
+    x = torch.cat([x, x.flip(0), x, x], 1)
+    codes, scales, zeros, values = ref.int4(x, 32, zero_points)
+    q = difr.int4_quantize(x.to(DEV), group=32, zero_points=zero_points)
+    good = ~scales.isnan()
+    assert torch.equal(q["scales"].cpu().isnan(), ~good)
+    assert torch.equal(q["scales"].cpu()[good], scales[good])
+    back = difr.int4_dequantize(q["codes"], q["scales"], 128, q.get("zeros"), dtype=torch.float32).cpu()
+    assert _same(back, values.float().double())
+
+
+def _matrix(difr, V, d, group, zero_points, seed, scale_of=None):
+    """Random codes (padding too), scales and zero points, and the values [V, d] in 64 bits."""
+    g = torch.Generator().manual_seed(seed)
+    K = difr.int4_padded(d)
+    c = torch.randint(0, 16, (V, K), generator=g, dtype=torch.uint8)
+    s = (scale_of(g, V, K // group) if scale_of else torch.rand(V, K // group, generator=g) + 0.1).to(torch.bfloat16)
+    z = torch.randint(0, 16, (V, K // group), generator=g, dtype=torch.uint8) if zero_points else None
+    w = c.double() - (8.0 if z is None else z.double().repeat_interleave(group, 1))
+    w = w * s.double().repeat_interleave(group, 1)
+    return (c[:, 0::2] | (c[:, 1::2] << 4)).to(DEV), s.to(DEV), None if z is None else z.to(DEV), w[:, :d]
+
+
+SHAPES = [(1, 1, 1), (1, 16, 128), (2, 17, 31), (3, 64, 256), (5, 100, 129), (15, 1000, 1000), (16, 33, 4096), (17, 250, 2000), (31, 129, 512),
+          (33, 1024, 640), (48, 77, 384), (64, 500, 4096), (65, 96, 1024), (130, 40, 896)]
+
+
+@pytest.mark.parametrize("N,V,d", SHAPES)
+@pytest.mark.parametrize("group,zero_points", [(32, True), (64, False), (128, True), (128, False)])
+@pytest.mark.parametrize("hidden,out", [(torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16)])
+def test_whole_numbers_are_exact(difr, N, V, d, group, zero_points, hidden, out):
+    """Hidden states of small whole numbers and scales of 1, 2 and 4: every partial sum, with the codes' offsets of up to 32, is a whole
+    number below 2^24 (4096 elements * 32 * 4 * 8 = 2^22), so the only rounding is the last."""
+    codes, scales, zeros, w = _matrix(difr, V, d, group, zero_points, V + d, lambda g, r, c: 2.0 ** torch.randint(0, 3, (r, c), generator=g))
+    h = torch.randint(-8, 9, (N, d), generator=torch.Generator().manual_seed(N)).to(hidden)
+    want = (h.double() @ w.t()).to(out)
+    got = difr.int4_product(_rows(h, 3, 5), codes, scales, zeros, dtype=out)
+    assert got.dtype == out and torch.equal(got.cpu(), want)
+
+
+@pytest.mark.parametrize("N,V,d", [s for s in SHAPES if s[2] > 100])
+@pytest.mark.parametrize("group,zero_points", [(32, False), (64, True), (128, True)])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_product(difr, N, V, d, group, zero_points, hidden):
+    codes, scales, zeros, w = _matrix(difr, V, d, group, zero_points, V + d)
+    h = (torch.randn(N, d, generator=torch.Generator().manual_seed(N)) * 3).to(hidden)
+    want = h.double() @ w.t()
+    # a running sum of `group` products of an element by a code offset by up to 32, scaled, summed over the groups: each of at most
+    # group + d / group + 8 additions is off by 2^-23 (the matrix cores may cut) of what has been added up
+    size = h.double().abs() @ (w.abs() + 32 * scales.cpu().double().repeat_interleave(group, 1)[:, :d]).t()
+    bound = size * (group + difr.int4_padded(d) // group + 8) * 2.0 ** -23
+    got = difr.int4_product(h.to(DEV), codes, scales, zeros, dtype=torch.float32)
+    assert ((got.cpu().double() - want).abs() <= bound + want.abs() * 2.0 ** -24).all()
+    # what the bound does not see: on the whole the sums are as good as fp32 sums are
+    error = (got.cpu().double() - want).square().mean().sqrt() / want.square().mean().sqrt()
+    assert error < 2.0 ** -19, error
+    half = difr.int4_product(h.to(DEV), codes, scales, zeros)
+    assert ((half.cpu().double() - want).abs() <= bound + (want.abs() + bound) * 2.0 ** -8).all()
+
+
+def test_out_with_a_pitch_and_what_lies_beside_it(difr):
+    codes, scales, zeros, w = _matrix(difr, 333, 256, 64, True, 5)
+    h = torch.randint(-4, 5, (20, 256)).to(torch.bfloat16)
+    buf = torch.full((20, 340), 7.0, device=DEV)
+    h_dev = h.to(DEV)
+    v0 = buf._version
+    got = difr.int4_product(h_dev, codes, scales, zeros, dtype=torch.float32, out=buf[:, 3:336])
+    assert got.data_ptr() == buf[:, 3:].data_ptr() and buf._version > v0
+    assert torch.equal(buf[:, 3:336].cpu(), difr.int4_product(h_dev, codes, scales, zeros, dtype=torch.float32).cpu())
+    assert buf[:, :3].eq(7).all() and buf[:, 336:].eq(7).all()
+
+
+def test_rows_do_not_touch_each_other(difr):
+    """A row's logits are the same alone and among others, and what is no number stays in its row."""
+    codes, scales, zeros, w = _matrix(difr, 500, 1000, 128, True, 6)
+    h = torch.randn(64, 1000, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    whole = difr.int4_product(h.to(DEV), codes, scales, zeros, dtype=torch.float32)
+    for n in (1, 2, 16, 17, 40):
+        assert torch.equal(difr.int4_product(h[:n].to(DEV), codes, scales, zeros, dtype=torch.float32), whole[:n]), n
+    h[3, 7], h[20, 999], h[41, 0] = math.nan, math.inf, -math.inf
+    got = difr.int4_product(h.to(DEV), codes, scales, zeros, dtype=torch.float32)
+    bad = torch.zeros(64, dtype=torch.bool)
+    bad[[3, 20, 41]] = True
+    assert torch.equal(got[~bad], whole[~bad]) and not got[bad].isfinite().any()
+
+
+def test_empty(difr):
+    codes, scales, zeros, w = _matrix(difr, 5, 128, 128, False, 1)
+    assert difr.int4_product(torch.zeros(0, 128, dtype=torch.bfloat16, device=DEV), codes, scales).shape == (0, 5)
+    assert difr.int4_product(torch.zeros(3, 128, dtype=torch.bfloat16, device=DEV), codes[:0], scales[:0]).shape == (3, 0)
+    assert difr.int4_quantize(torch.zeros(0, 5, device=DEV))["codes"].shape == (0, 64)
+
+
+def test_a_quantised_head_gives_the_dense_products(difr):
+    g = torch.Generator().manual_seed(9)
+    w = (torch.randn(700, 2048, generator=g) / 45).to(torch.bfloat16).to(DEV)
+    h = torch.randn(6, 2048, generator=g).to(torch.bfloat16).to(DEV)
+    q = difr.int4_quantize(w, group=64, zero_points=True)
+    dense = difr.int4_dequantize(q["codes"], q["scales"], 2048, q["zeros"], dtype=torch.float32)
+    assert (dense - w.float()).abs().max() < 0.02       # half a step of a sixteenth of a group's range
+    want = h.double().cpu() @ dense.double().cpu().t()
+    got = difr.int4_product(h, q["codes"], q["scales"], q["zeros"], dtype=torch.float32)
+    assert (got.cpu().double() - want).abs().max() < 1e-4 * want.abs().max()
