@@ -607,7 +607,7 @@ int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N,
  *   The elements of a row are in groups of `group` (32, 64 or 128), the first from element 0 on:  w = scale (code - zero), code and zero
  *   point in 0 ... 15, scale a bf16 number.  A matrix without zero points has 8 everywhere.
  *   codes  [rows, K / 2]: element 2 i in the lower half of byte i;  scales [rows, K / group] bf16;  zeros [rows, K / group] bytes, or
- *   NULL;  all without gaps, codes aligned to 16 bytes, scales to 4, zeros to 2;  K is d rounded up to a multiple of 128 (difr_int4_padded), and
+ *   NULL;  all without gaps, codes aligned to 16 bytes, scales to 2;  K is d rounded up to a multiple of 128 (difr_int4_padded), and
  *   what codes say of elements from d on does not count.
  * Quantisation.  Without zero points scale = (largest magnitude) / 7, else (hi - lo) / 15 with hi = max(largest, 0), lo = min(smallest, 0),
  * and zero = -lo / scale rounded and held in 0 ... 15.  Quotients are fp32, the scale's is rounded to bf16, and code = x / scale rounded
@@ -626,9 +626,14 @@ int difr_int4_dequantize(const uint8_t *codes, const void *scales, const uint8_t
  * of elements and codes are exact, accumulation and scaling are fp32, and the sum is rounded once to bf16 or fp32 ([N, ld], ld >= V).
  * Meant for the few rows that are decoded together: the head is read once for every 64 of them (fp32: every 21).  Rows that hold a NaN, an infinity or
  * magnitudes above 2^120 get NaN or infinities.  A row's result does not depend on the rows beside it.  V < 2^31, K < 2^24, bases aligned to the element size.
+ * workspace  DEVICE scratch of at least difr_int4_product_workspace_bytes(N, d, hidden_dtype, group) bytes (host only; 0: none is needed and
+ * NULL will do), 16-byte aligned, contents irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small:
+ * DIFR_ERR_SHAPE.
  */
+size_t difr_int4_product_workspace_bytes(int64_t N, int64_t d, int32_t hidden_dtype, int32_t group);
 int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64_t d, int64_t ldh, const uint8_t *codes, const void *scales,
-                      const uint8_t *zeros, int64_t V, int32_t group, void *out, int32_t dtype, int64_t ld, void *hip_stream);
+                      const uint8_t *zeros, int64_t V, int32_t group, void *out, int32_t dtype, int64_t ld, void *workspace,
+                      size_t workspace_bytes, void *hip_stream);
 
 /*
  * Verification of drafted tokens: a server that decodes speculatively has a cheap draft propose tokens, forms the target's logits at all

@@ -114,7 +114,7 @@ class _DraftChain(C.Structure):
 EXPORTS = ("difr_gumbel_score", "difr_debug_gumbel_score_unfiltered", "difr_ipt_score", "difr_score_both", "difr_score_both_peaked", "difr_score_both_admissible", "difr_admissible_count", "difr_gumbel_likelihood", "difr_ipt_score_filtered", "difr_score_both_filtered", "difr_lmhead_score", "difr_lmhead_score_static", "difr_lmhead_workspace_bytes", "difr_split_workspace_bytes", "difr_score_split", "difr_classify", "difr_seq_reduce",
            "difr_token_workspace_bytes", "difr_token_logprob", "difr_token_logprob_backward", "difr_policy_loss", "difr_preference_loss", "difr_mx4_padded",
            "difr_mx4_quantize", "difr_mx4_dequantize", "difr_mx4_product_workspace_bytes", "difr_mx4_product", "difr_int4_padded", "difr_int4_quantize", "difr_int4_dequantize",
-           "difr_int4_product", "difr_draft_workspace_bytes", "difr_draft_verify", "difr_tree_verify", "difr_debug_noise", "difr_debug_gumbel_map",
+           "difr_int4_product_workspace_bytes", "difr_int4_product", "difr_draft_workspace_bytes", "difr_draft_verify", "difr_tree_verify", "difr_debug_noise", "difr_debug_gumbel_map",
            "difr_philox4x32_10", "difr_status_string", "difr_version")
 
 
@@ -186,7 +186,9 @@ def load_library():
     lib.difr_int4_padded.restype = i64
     lib.difr_int4_quantize.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp, vp, vp]
     lib.difr_int4_dequantize.argtypes = [vp, vp, vp, i64, i64, i32, vp, i32, i64, vp]
-    lib.difr_int4_product.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i64, i32, vp, i32, i64, vp]
+    lib.difr_int4_product_workspace_bytes.argtypes = [i64, i64, i32, i32]
+    lib.difr_int4_product_workspace_bytes.restype = C.c_size_t
+    lib.difr_int4_product.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i64, i32, vp, i32, i64, vp, C.c_size_t, vp]
     lib.difr_draft_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
     lib.difr_draft_workspace_bytes.restype = C.c_size_t
     lib.difr_draft_verify.argtypes = [C.POINTER(_Drafts), C.POINTER(_DraftChain)] + [vp] * 5 + [C.c_size_t, vp]

@@ -629,6 +629,7 @@ int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N,
 
 int64_t difr_int4_padded(int64_t d) { return d <= 0 ? 0 : (d + difr::kInt4Slab - 1) / difr::kInt4Slab * difr::kInt4Slab; }
 
+static bool int4_group(int32_t group) { return group == 32 || group == 64 || group == 128; }
 static int element_size(int32_t dtype) { return dtype == DIFR_BF16 ? 2 : 4; }
 
 // A matrix in 4-bit integers of N rows and a dense one beside it (x: its elements, quantised, dequantised or multiplied by it).
@@ -636,11 +637,11 @@ static int validate_int4(const void *x, int32_t dtype, int64_t N, int64_t d, int
                          const void *scales, const uint8_t *zeros, difr::Int4Matrix *m)
 {
     if (N < 0 || d < 1 || ld < d || N >= (int64_t)1 << 31 || d >= (int64_t)1 << 24) return DIFR_ERR_SHAPE;
-    if (group != 32 && group != 64 && group != 128) return DIFR_ERR_ARGUMENT;
+    if (!int4_group(group)) return DIFR_ERR_ARGUMENT;
     if (dtype != DIFR_BF16 && dtype != DIFR_F32) return DIFR_ERR_DTYPE;
     if (N == 0) return DIFR_OK;
     if (!x || !codes || !scales) return DIFR_ERR_NULL;
-    if ((uintptr_t)x % element_size(dtype) || (uintptr_t)codes % 16u || (uintptr_t)scales % 4u || (uintptr_t)zeros % 2u) return DIFR_ERR_ALIGN;
+    if ((uintptr_t)x % element_size(dtype) || (uintptr_t)codes % 16u || (uintptr_t)scales % 2u) return DIFR_ERR_ALIGN;
     *m = difr::Int4Matrix{codes, (const uint16_t *)scales, zeros, N, difr_int4_padded(d), group};
     return DIFR_OK;
 }
@@ -666,8 +667,16 @@ int difr_int4_dequantize(const uint8_t *codes, const void *scales, const uint8_t
     return difr::launch_int4_dequantize(m, d, x, dtype, ld, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
 }
 
+size_t difr_int4_product_workspace_bytes(int64_t N, int64_t d, int32_t hidden_dtype, int32_t group)
+{
+    if (N < 1 || N >= (int64_t)1 << 31 || d < 1 || d >= (int64_t)1 << 24 || !int4_group(group) || (hidden_dtype != DIFR_BF16 && hidden_dtype != DIFR_F32))
+        return 0;
+    return difr::int4_product_workspace_bytes(N, d, hidden_dtype, group);
+}
+
 int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64_t d, int64_t ldh, const uint8_t *codes, const void *scales,
-                      const uint8_t *zeros, int64_t V, int32_t group, void *out, int32_t dtype, int64_t ld, void *hip_stream)
+                      const uint8_t *zeros, int64_t V, int32_t group, void *out, int32_t dtype, int64_t ld, void *workspace,
+                      size_t workspace_bytes, void *hip_stream)
 {
     if (N < 0 || N >= (int64_t)1 << 31 || V < 0 || V >= (int64_t)1 << 31 || ldh < d || ld < V) return DIFR_ERR_SHAPE;
     if (hidden_dtype != DIFR_BF16 && hidden_dtype != DIFR_F32) return DIFR_ERR_DTYPE;
@@ -675,9 +684,12 @@ int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64
     int rc = validate_int4(out, dtype, N ? V : 0, d, d, group, codes, scales, zeros, &m);
     if (rc != DIFR_OK || N == 0 || V == 0) return rc;
     if (!hidden) return DIFR_ERR_NULL;
-    if ((uintptr_t)hidden % element_size(hidden_dtype)) return DIFR_ERR_ALIGN;
+    if ((uintptr_t)hidden % element_size(hidden_dtype) || (uintptr_t)workspace % 16u) return DIFR_ERR_ALIGN;
+    const size_t need = difr::int4_product_workspace_bytes(N, d, hidden_dtype, group);
+    if (workspace_bytes < need) return DIFR_ERR_SHAPE;
+    if (need && !workspace) return DIFR_ERR_NULL;
     if ((rc = check_device()) != DIFR_OK) return rc;
-    return difr::launch_int4_product(hidden, hidden_dtype, N, d, ldh, m, out, dtype, ld, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
+    return difr::launch_int4_product(hidden, hidden_dtype, N, d, ldh, m, out, dtype, ld, workspace, (hipStream_t)hip_stream) ? DIFR_ERR_LAUNCH : DIFR_OK;
 }
 
 static int validate_drafts(const difr_drafts *in, difr::DraftBatch *b)

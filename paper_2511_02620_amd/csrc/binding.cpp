@@ -55,6 +55,7 @@ namespace {
     X(difr_int4_padded)                                                                                                 \
     X(difr_int4_quantize)                                                                                               \
     X(difr_int4_dequantize)                                                                                             \
+    X(difr_int4_product_workspace_bytes)                                                                                \
     X(difr_int4_product)                                                                                                \
     X(difr_draft_workspace_bytes)                                                                                       \
     X(difr_draft_verify)                                                                                                \
@@ -903,9 +904,13 @@ PyObject *int4_product(PyObject *const *a)
             throw Refused();
         if (N > 1) ld = t.stride(0);
     }
+    const size_t need = lib.difr_int4_product_workspace_bytes(N, d, type, (int32_t)c.group);
+    at::Tensor ws;
+    if (need) ws = o.make(at::kByte, {(int64_t)need});
+    void *wsp = need ? ws.data_ptr() : nullptr;
     const int rc = enter(c.dev, [&](void *s) {
         return lib.difr_int4_product(h.data_ptr(), type, N, d, ldh, c.codes, c.scales, c.zeros, c.rows, (int32_t)c.group, t.data_ptr(),
-                                     f32 ? DIFR_F32 : DIFR_BF16, ld, s);
+                                     f32 ? DIFR_F32 : DIFR_BF16, ld, wsp, need, s);
     });
     if (a[5] != Py_None) written(rc, t);
     return wrapped(rc, t);

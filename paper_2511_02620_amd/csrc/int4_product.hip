@@ -1,55 +1,615 @@
-// out[n][v] = sum_k h[n][k] w[v][k] for a head w in 4-bit integers: few hidden states, of which one each is what a token takes.
+// out[n][v] = sum_k h[n][k] w[v][k] for a head w in 4-bit integers with group scales: the few hidden states that are decoded together.
+//
+// What bounds it is reading the codes once, so everything else has to hide behind that: a compute unit gets some 10 bytes of codes a
+// cycle.  A code goes to the matrix cores as the bf16 number 16 + code, which is two instructions for two codes (a shift, and one that masks
+// them into bits 3 ... 6 of 0x4180), and exact.  With S_g = sum_{k in g} h_k over a group,
+//   sum_{k in g} s (code - zero) h_k = s (sum_{k in g} (16 + code) h_k)  -  s (16 + zero) S_g:
+// products of whole numbers below 32 by bf16 numbers are exact in fp32, a group's sum is scaled in fp32, and the second part is a product of
+// its own on the matrix cores, four groups at once: S_g in three bf16 parts (24 bits), s (16 + zero) in two (13 bits, exact), so that nothing
+// but fp32 accumulation is rounded.  fp32 hidden states are three bf16 parts too, one matrix instruction each.
 #include "difr_host.hpp"
 #include "int4.hpp"
 #include "softmax_row.hpp"
 
 namespace difr {
 
-constexpr int kInt4Rows = 8;  // hidden states of a pass over the head
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
 
-// A wave a row of the head, eight elements a lane at a time.
-template <int HT, int DT>
-__global__ __launch_bounds__(kBlock) void int4_product_kernel(const typename Elem<HT>::type *h, int64_t N, int64_t d, int64_t ldh, Int4Matrix m,
-                                                              typename Elem<DT>::type *out, int64_t ld)
+struct Int4Product {
+    const void *h;
+    int64_t N, d, ldh;
+    Int4Matrix m;
+    void *out;
+    int64_t ld;
+    int f32_out;
+    int passes, per_pass;   // of the blocks of 16 rows of the head that a wave has, `per_pass` at a time
+    const uint8_t *image;   // hidden states as the matrix instructions want them (int4_image_kernel), or null
+};
+
+constexpr int kProductWaves = 8, kProductThreads = kProductWaves * 64;
+constexpr int kSlab = 256;                     // elements of a row that a step takes
+constexpr int kHiddenBytes = 140 * 1024;       // of LDS for hidden states that stay there
+
+// The order in which the codes of four bytes come out of two at a time: 0 4 1 5 2 6 3 7.  Hidden states are put in that order in LDS.
+__device__ __forceinline__ u32x4 code_order(u32x4 q)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t v = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6), n0 = (int64_t)blockIdx.y * kInt4Rows;
-    if (v >= m.V) return;
-    float acc[kInt4Rows] = {};
-    for (int64_t k = lane * 8; k < m.K; k += 512) {
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(m.codes + v * (m.K / 2) + k / 2);
-        const int64_t g = v * (m.K / m.group) + k / m.group;
-        const float s = __uint_as_float((uint32_t)m.scales[g] << 16), z = m.zeros ? (float)m.zeros[g] : 8.0f;
+    return u32x4{__builtin_amdgcn_perm(q.z, q.x, 0x05040100u), __builtin_amdgcn_perm(q.z, q.x, 0x07060302u),
+                 __builtin_amdgcn_perm(q.w, q.y, 0x05040100u), __builtin_amdgcn_perm(q.w, q.y, 0x07060302u)};
+}
+// Eight codes as bf16 numbers 16 + code, in that order.  (The two constants in registers: one instruction takes one of another kind.)
+struct CodeBits {
+    uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
+    __device__ __forceinline__ CodeBits() { asm("" : "+v"(mask), "+v"(sixteen)); }
+    __device__ __forceinline__ bf16x8 of(uint32_t w) const
+    {
+        return __builtin_bit_cast(bf16x8, u32x4{(w << 3 & mask) | sixteen, (w >> 1 & mask) | sixteen, (w >> 5 & mask) | sixteen, (w >> 9 & mask) | sixteen});
+    }
+};
+// An fp32 number as three bf16 numbers whose sum it is (the first two cut).
+struct Three {
+    uint32_t h, m, l;  // upper halves
+};
+__device__ __forceinline__ Three three_parts(float f)
+{
+    Three t;
+    t.h = __float_as_uint(f) & 0xFFFF0000u;
+    const float r = f - __uint_as_float(t.h);
+    t.m = __float_as_uint(r) & 0xFFFF0000u;
+    t.l = __float_as_uint(r - __uint_as_float(t.m)) & 0xFFFF0000u;
+    return t;
+}
+__device__ __forceinline__ uint32_t halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }  // of upper halves
+
+// A block of 16 rows and a slab as a wave fetches it: neighbouring lanes neighbouring bytes (the caches are asked for each run of lanes apart; a lane
+// a row of its own took four times the requests, and those were what the time went to).  Codes: lane l 16 bytes l % 8 of rows l / 8 and 8 + l / 8.
+// Scales and zero points: lanes 4 r ... 4 r + 3 those of row r.
+struct Int4Fetched {
+    u32x4 w[2];
+    uint32_t s, z;
+};
+constexpr int kCodePitch = kSlab / 2 + 16;  // bytes of a row of codes in LDS: 16 rows spread over the banks
+
+// The same as the matrix instructions take it.  Lane (kg, v), v = lane % 16, has of row v the codes of the slots 8 kg ... of each step of 32:
+// of every group the kg-th quarter.
+template <int G>
+struct Int4Slab {
+    static constexpr int kGroups = kSlab / G;
+    uint32_t w[8];                    // by steps
+    uint32_t s[G == 32 ? 4 : 2];      // of the groups of each half, as they are stored
+    uint32_t z[2];
+    template <int GS>
+    __device__ __forceinline__ float scale() const  // of group GS
+    {
+        if constexpr (G == 128)
+            return __uint_as_float((uint32_t)s[GS] << 16);
+        else
+            return __uint_as_float(GS % 2 ? s[GS / 2] & 0xFFFF0000u : s[GS / 2] << 16);
+    }
+    // of group 4 q + kg (G = 128: kg % 2)
+    __device__ __forceinline__ float scale_of(int q, int kg) const
+    {
+        if constexpr (G == 128) return __uint_as_float((uint32_t)(kg & 1 ? s[1] : s[0]) << 16);
+        const uint32_t pair = G == 64 ? (kg & 2 ? s[1] : s[0]) : q ? (kg & 2 ? s[3] : s[2]) : (kg & 2 ? s[1] : s[0]);
+        return __uint_as_float(kg & 1 ? pair & 0xFFFF0000u : pair << 16);
+    }
+    __device__ __forceinline__ uint32_t zero_of(int q, int kg) const
+    {
+        if constexpr (G == 128) return kg & 1 ? z[1] : z[0];
+        if constexpr (G == 64) return (uint32_t)(kg & 2 ? z[1] : z[0]) >> (8 * (kg & 1)) & 0xFFu;
+        return (q ? z[1] : z[0]) >> (8 * kg) & 0xFFu;
+    }
+};
+
+// Two vectors of eight elements in the order of the codes, and their sum, as the matrix instructions want them.
+template <int HT>
+struct Eight {
+    static constexpr int P = HT == 0 ? 1 : 3;
+    u32x4 part[P];
+    float sum;
+    __device__ __forceinline__ Eight(const typename Elem<HT>::type *p, int64_t at, int64_t d)  // zeros from element d on
+    {
+        float e[8];
 #pragma unroll
-        for (int i = 0; i < kInt4Rows; ++i) {
-            if (n0 + i >= N) break;
-            const typename Elem<HT>::type *row = h + (n0 + i) * ldh;
-            float part = 0.0f;
+        for (int j = 0; j < 8; ++j) e[j] = 0.0f;
+        constexpr int E = Elem<HT>::kPerVec;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (k + j < d) part = __builtin_fmaf((float)(w >> (4 * j) & 15u) - z, Elem<HT>::to_float(row[k + j]), part);
-            acc[i] = __builtin_fmaf(s, part, acc[i]);
+        for (int j = 0; j < 8; j += E) {
+            if (at + j + E <= d) {
+                unpack_vector<HT>(*reinterpret_cast<const u32x4_any *>(p + at + j), e + j);
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if (at + j + i < d) e[j + i] = Elem<HT>::to_float(p[at + j + i]);
+            }
+        }
+        sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        Three t[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = three_parts(e[j]);  // (of bf16 the first part is all)
+        part[0] = u32x4{halves(t[0].h, t[4].h), halves(t[1].h, t[5].h), halves(t[2].h, t[6].h), halves(t[3].h, t[7].h)};
+        if constexpr (P == 3) {
+            part[1] = u32x4{halves(t[0].m, t[4].m), halves(t[1].m, t[5].m), halves(t[2].m, t[6].m), halves(t[3].m, t[7].m)};
+            part[2] = u32x4{halves(t[0].l, t[4].l), halves(t[1].l, t[5].l), halves(t[2].l, t[6].l), halves(t[3].l, t[7].l)};
         }
     }
+};
+// A group's sum, by the first of the G / 8 lanes that have its elements: in three parts.
+template <int G>
+__device__ __forceinline__ u32x2 group_sum(float sum)
+{
 #pragma unroll
-    for (int i = 0; i < kInt4Rows; ++i) {
-        const float sum = wave_sum(acc[i]);
-        if (lane == 0 && n0 + i < N) store_element<DT>(out + (n0 + i) * ld + v, sum);
+    for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor(sum, o);
+    const Three t = three_parts(sum);
+    return u32x2{halves(t.h, t.m), t.l >> 16};
+}
+// A fragment of three-part sums, to be multiplied by two-part coefficients: slots h m l h m l.
+__device__ __forceinline__ u32x4 sum_slots(u32x2 m) { return u32x4{m.x, m.y | m.x << 16, m.x >> 16 | m.y << 16, 0u}; }
+
+// The step of a half slab (128 elements) in which the eight elements `piece` of it are multiplied, and the quarter of the lanes that has them.
+template <int G>
+__device__ __forceinline__ void step_of(int piece, int &j, int &kg)
+{
+    if constexpr (G == 128)
+        kg = piece >> 2, j = piece & 3;
+    else if constexpr (G == 64)
+        kg = piece >> 1 & 3, j = (piece >> 3) * 2 + (piece & 1);
+    else
+        kg = piece & 3, j = piece >> 2;
+}
+template <int G>
+__device__ __forceinline__ int piece_of(int j, int kg)
+{
+    return G == 128 ? kg * 4 + j : G == 64 ? (j >> 1) * 8 + kg * 2 + (j & 1) : j * 4 + kg;
+}
+
+// Batches of more than 16 hidden states, whose fragments are the same for every workgroup and do not fit its LDS: an image of them in
+// global memory.  For each slab, tile of 16 states and part, 8 fragments of 64 lanes of 16 bytes; then the fragments of the groups' sums.
+constexpr int kFragment = 1024;
+template <int G, int P>
+constexpr int image_fragments() { return P * 8 + (kSlab / G + 3) / 4; }  // of a slab and tile
+
+// A thread eight elements of a row of 256.
+template <int HT, int G>
+__global__ __launch_bounds__(kBlock) void int4_image_kernel(const typename Elem<HT>::type *h, int64_t N, int64_t d, int64_t ldh, int tiles, uint8_t *image)
+{
+    constexpr int P = Eight<HT>::P, F = image_fragments<G, P>();
+    const int id = blockIdx.x * kBlock + threadIdx.x, piece = id & 31, row = id >> 5, tile = row >> 4, n = row & 15;
+    const int64_t slab = blockIdx.y;
+    uint8_t *const to = image + (slab * tiles + tile) * (int64_t)(F * kFragment);
+    const Eight<HT> x(h + (row < N ? row : N - 1) * ldh, slab * kSlab + piece * 8, row < N ? d : 0);
+    int j, kg;
+    step_of<G>(piece & 15, j, kg);
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4 *>(to + (p * 8 + (piece >> 4) * 4 + j) * kFragment + (kg * 16 + n) * 16) = x.part[p];
+    const u32x2 m = group_sum<G>(x.sum);
+    const int g = piece / (G / 8);
+    if (piece % (G / 8) == 0) *reinterpret_cast<u32x4 *>(to + (P * 8 + g / 4) * kFragment + ((g & 3) * 16 + n) * 16) = sum_slots(m);
+    if (G == 128 && piece % 16 == 0)  // a slab of two groups: the other two quarters
+        *reinterpret_cast<u32x4 *>(to + P * 8 * kFragment + ((g + 2) * 16 + n) * 16) = u32x4{0u, 0u, 0u, 0u};
+}
+
+// Hidden states in P parts; NT tiles of 16 of them from the image, a step ahead (RESIDENT: up to 16, converted by each workgroup and kept in
+// LDS); KS slabs at once, each with its share of the waves (small heads, whose blocks are fewer than waves); RB blocks of 16 rows of
+// the head to a wave at a time; D steps of codes in flight, in registers.
+template <int HT, bool RESIDENT, int NT, int KS, int G, bool ZEROS, int RB, int D>
+__global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Product a)
+{
+    constexpr int P = Eight<HT>::P, kGroups = kSlab / G, kQuads = (kGroups + 3) / 4, F = image_fragments<G, P>();
+    constexpr int kSteps = G / 32;     // matrix instructions of a group
+    constexpr int kStage = KS * NT * F * kFragment, kPieces = (kStage / 16 + kProductThreads - 1) / kProductThreads;
+    constexpr int kTeams = kProductWaves / KS;
+    static_assert(!RESIDENT || NT == 1, "one tile stays");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[RESIDENT ? kHiddenBytes : 2 * kStage];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_code[kProductWaves][RB * 16 * kCodePitch];  // a wave's own
+    static_assert(KS == 1 || RB * NT * kFragment <= RB * 16 * kCodePitch, "a wave's share of the sums fits where its codes were");
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int v = lane & 15, kg = lane >> 4;
+    const int ks = wave % KS, team = wave / KS;                    // which slab of a step, which blocks
+    const int64_t n0 = (int64_t)blockIdx.y * (16 * NT);
+    const int rows_here = a.N - n0 < 16 * NT ? (int)(a.N - n0) : 16 * NT;
+    const int64_t blocks = (a.m.V + 15) / 16;
+    const int64_t block0 = blocks * blockIdx.x / gridDim.x, block1 = blocks * (blockIdx.x + 1) / gridDim.x;
+    const int mine = (int)(block1 - block0);
+    const int nslab = (int)((a.m.K + kSlab - 1) / kSlab), per = (nslab + KS - 1) / KS, total = a.passes * per;
+    const bool odd = a.m.K % kSlab != 0;                           // the last slab is half a slab
+    const int live_groups = (int)((a.d + G - 1) / G);              // what lies behind does not count
+
+    auto barrier = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    // ---- hidden states that stay: rows of K elements (and 16 bytes, to spread a fragment over the banks) of each part, then sums
+    const int hpitch = nslab * (kSlab * 2) + 16, plane = rows_here * hpitch;
+    u32x2 *const lds_sum = reinterpret_cast<u32x2 *>(lds + P * plane);  // [row][group]
+    const int spitch = nslab * kGroups + 2;
+    if constexpr (RESIDENT) {
+        const int row_pieces = nslab * 32;
+        for (int id = tid; id < rows_here * row_pieces; id += kProductThreads) {
+            const int row = id / row_pieces, piece = id - row * row_pieces;
+            const Eight<HT> x(reinterpret_cast<const typename Elem<HT>::type *>(a.h) + (n0 + row) * a.ldh, (int64_t)piece * 8, a.d);
+#pragma unroll
+            for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4 *>(lds + p * plane + row * hpitch + piece * 16) = x.part[p];
+            const u32x2 m = group_sum<G>(x.sum);  // (32 pieces of a slab go to half a wave: a group's lanes are there together)
+            if (piece % (G / 8) == 0) lds_sum[row * spitch + piece / (G / 8)] = m;
+        }
+    }
+    // ---- or come from the image, a step ahead: global memory -> registers -> LDS
+    u32x4 x[RESIDENT ? 1 : kPieces];
+    const uint8_t *const image = RESIDENT ? nullptr : a.image + (int64_t)blockIdx.y * (NT * F * kFragment);
+    const int64_t image_slab = (int64_t)gridDim.y * (NT * F * kFragment);
+    auto fetch_hidden = [&](int step) __attribute__((always_inline)) {
+        if constexpr (!RESIDENT)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int id = i * kProductThreads + tid, s = id / (NT * F * 64), at = id - s * (NT * F * 64);
+                const int sl = step * KS + s < nslab ? step * KS + s : nslab - 1;
+                if (i + 1 < kPieces || kPieces * kProductThreads * 16 == kStage)
+                    x[i] = *reinterpret_cast<const u32x4 *>(image + sl * image_slab + at * 16);
+                else  // (the last pieces are for some of the threads)
+                    x[i] = *reinterpret_cast<const u32x4 *>(image + (s < KS ? sl * image_slab + at * 16 : 0));
+            }
+    };
+    auto put_hidden = [&](int stage) __attribute__((always_inline)) {
+        if constexpr (!RESIDENT)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int at = (i * kProductThreads + tid) * 16;
+                if (at < kStage) *reinterpret_cast<u32x4 *>(lds + stage * kStage + at) = x[i];
+            }
+    };
+    // fragment of step j of a half slab, or the sums of four groups
+    auto hidden = [&](int stage, int sl, int t, int p, int seg, int j) __attribute__((always_inline)) {
+        if constexpr (RESIDENT)
+            return *reinterpret_cast<const bf16x8 *>(lds + p * plane + (v < rows_here ? v : 0) * hpitch + (sl * 32 + seg * 16 + piece_of<G>(j, kg)) * 16);
+        else
+            return *reinterpret_cast<const bf16x8 *>(lds + stage * kStage + ((ks * NT + t) * F + p * 8 + seg * 4 + j) * kFragment + lane * 16);
+    };
+    auto hidden_sums = [&](int stage, int sl, int t, int q) __attribute__((always_inline)) {
+        if constexpr (RESIDENT) {
+            const int g = q * 4 + kg;
+            u32x2 m = lds_sum[(v < rows_here ? v : 0) * spitch + sl * kGroups + (g < kGroups ? g : 0)];
+            return __builtin_bit_cast(bf16x8, sum_slots(g < kGroups ? m : u32x2{0u, 0u}));
+        } else {
+            return *reinterpret_cast<const bf16x8 *>(lds + stage * kStage + ((ks * NT + t) * F + P * 8 + q) * kFragment + lane * 16);
+        }
+    };
+
+    // ---- the head: registers, D steps ahead.  Rows of the workgroup by 32-bit offsets from its first.
+    Int4Fetched slab[D][RB];
+    const int pitch = (int)(a.m.K / 2), groups = (int)(a.m.K / G);
+    const int64_t row0 = block0 * 16;
+    const int row_end = (int)((block1 * 16 < a.m.V ? block1 * 16 : a.m.V) - row0);
+    const uint8_t *const codes = a.m.codes + row0 * pitch, *const scales = reinterpret_cast<const uint8_t *>(a.m.scales + row0 * groups);
+    const uint8_t *const zeros = ZEROS ? a.m.zeros + row0 * groups : nullptr;
+    auto first_block = [&](int pass) { return (pass * kTeams + team) * a.per_pass; };
+    int f_pass = 0, f_step = 0;
+    uint32_t at_code[RB][2], at_group[RB];
+    // (rows that are not there: the last one again, from the caches)
+    auto aim = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            const int r = (first_block(f_pass) + b) * 16;
+            at_code[b][0] = (uint32_t)min(r + (lane >> 3), row_end - 1) * (uint32_t)pitch;
+            at_code[b][1] = (uint32_t)min(r + 8 + (lane >> 3), row_end - 1) * (uint32_t)pitch;
+            at_group[b] = (uint32_t)min(r + (lane >> 2), row_end - 1) * (uint32_t)groups;
+        }
+    };
+    aim();
+    // No branches around loads: the waits for them are counted.
+    auto fetch_head = [&](Int4Fetched (&to)[RB]) __attribute__((always_inline)) {
+        const int ask = f_step * KS + ks, sl = ask < nslab ? ask : nslab - 1;
+        const bool half = odd && sl + 1 == nslab;  // the first half again in the second's place
+        const uint8_t *const c0 = codes + sl * (kSlab / 2), *const s0 = scales + sl * (kGroups * 2), *const z0 = ZEROS ? zeros + sl * kGroups : nullptr;
+        const uint32_t part = lane & (half ? 3 : 7), own = lane & (G == 32 ? (half ? 1 : 3) : (half ? 0 : 1)), zown = lane & (half ? 0 : 1);
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) to[b].w[i] = *reinterpret_cast<const u32x4 *>(c0 + (at_code[b][i] + part * 16));
+            if constexpr (G == 128) {
+                to[b].s = *reinterpret_cast<const u16_any *>(s0 + (2 * at_group[b] + own * 2));
+                if constexpr (ZEROS) to[b].z = *(z0 + (at_group[b] + zown));
+            } else {
+                to[b].s = *reinterpret_cast<const u32_any *>(s0 + (2 * at_group[b] + own * 4));
+                if constexpr (ZEROS && G == 64) to[b].z = *reinterpret_cast<const u16_any *>(z0 + (at_group[b] + zown * 2));
+                if constexpr (ZEROS && G == 32) to[b].z = *reinterpret_cast<const u32_any *>(z0 + (at_group[b] + zown * 4));
+            }
+        }
+        if (++f_step == per) {
+            f_step = 0;
+            if (f_pass + 1 < a.passes) ++f_pass;
+            aim();
+        }
+    };
+    // From the fetching lanes to the multiplying ones: codes by way of LDS (a wave's operations on it keep their order), the rest from lane 4 v.
+    uint8_t *const my_code = lds_code[wave];
+    auto deal = [&](const Int4Fetched (&from)[RB], Int4Slab<G> (&to)[RB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<u32x4 *>(my_code + (b * 16 + i * 8 + (lane >> 3)) * kCodePitch + (lane & 7) * 16) = from[b].w[i];
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        static_for<RB>([&](auto B) __attribute__((always_inline)) {
+            constexpr int b = decltype(B)::value;
+            const uint8_t *const c = my_code + (b * 16 + v) * kCodePitch;
+            static_for<2>([&](auto SEG) __attribute__((always_inline)) {
+                constexpr int seg = decltype(SEG)::value;
+                if constexpr (G == 128) {
+                    const u32x4 q = *reinterpret_cast<const u32x4 *>(c + seg * 64 + kg * 16);
+                    to[b].w[seg * 4] = q.x, to[b].w[seg * 4 + 1] = q.y, to[b].w[seg * 4 + 2] = q.z, to[b].w[seg * 4 + 3] = q.w;
+                } else if constexpr (G == 64) {
+                    static_for<2>([&](auto J) __attribute__((always_inline)) {
+                        constexpr int j = decltype(J)::value;
+                        const u32x2 q = *reinterpret_cast<const u32x2 *>(c + seg * 64 + j * 32 + kg * 8);
+                        to[b].w[seg * 4 + 2 * j] = q.x, to[b].w[seg * 4 + 2 * j + 1] = q.y;
+                    });
+                } else {
+                    static_for<4>([&](auto J) __attribute__((always_inline)) {
+                        constexpr int j = decltype(J)::value;
+                        to[b].w[seg * 4 + j] = *reinterpret_cast<const uint32_t *>(c + seg * 64 + j * 16 + kg * 4);
+                    });
+                }
+            });
+            static_for<(G == 32 ? 4 : 2)>([&](auto I) __attribute__((always_inline)) {
+                constexpr int i = decltype(I)::value;
+                to[b].s[i] = __builtin_amdgcn_ds_bpermute(v * 16 + i * 4, from[b].s);
+                if constexpr (ZEROS && i < 2) to[b].z[i] = __builtin_amdgcn_ds_bpermute(v * 16 + i * 4, from[b].z);
+            });
+        });
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    };
+
+    const CodeBits code_values;
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 acc[RB][NT];
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[b][t] = zero;
+
+    int pass = 0, step = 0;
+    auto multiply = [&](const Int4Fetched (&fetched)[RB], int stage) __attribute__((always_inline)) {
+        const int sl = step * KS + ks;
+        if (sl >= nslab || first_block(pass) >= mine) return;
+        Int4Slab<G> w[RB];
+        deal(fetched, w);
+        // groups of the slab that count (none of the second half of half a slab, whose codes are the first's again and whose states are 0)
+        const int live = sl + 1 == nslab ? live_groups - sl * kGroups : kGroups;
+        static_for<2>([&](auto SEG) __attribute__((always_inline)) {
+            constexpr int seg = decltype(SEG)::value;
+            f32x4 part[RB][NT];
+            static_for<4>([&](auto J) __attribute__((always_inline)) {
+                constexpr int j = decltype(J)::value, g = j / kSteps, js = j % kSteps, gs = seg * (128 / G) + g;  // step of the half, group, step of it
+                bf16x8 f[NT][P];
+                static_for<NT * P>([&](auto I) __attribute__((always_inline)) {
+                    constexpr int t = decltype(I)::value / P, p = decltype(I)::value % P;
+                    f[t][p] = hidden(stage, sl, t, p, seg, j);
+                });
+                static_for<RB>([&](auto B) __attribute__((always_inline)) {
+                    constexpr int b = decltype(B)::value;
+                    const bf16x8 c = code_values.of(w[b].w[seg * 4 + j]);
+                    static_for<NT * P>([&](auto I) __attribute__((always_inline)) {
+                        constexpr int t = decltype(I)::value / P, p = decltype(I)::value % P;
+                        part[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t][p], c, js == 0 && p == 0 ? zero : part[b][t], 0, 0, 0);
+                    });
+                    if constexpr (js + 1 == kSteps) {
+                        const float scale = gs < live ? w[b].template scale<gs>() : 0.0f;
+                        static_for<NT>([&](auto TT) __attribute__((always_inline)) {
+                            constexpr int t = decltype(TT)::value;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[b][t][r] = __builtin_fmaf(scale, part[b][t][r], acc[b][t][r]);
+                        });
+                    }
+                });
+            });
+        });
+        // less s (16 + zero) times the groups' sums: lane (kg, v) has the scale of group kg (and 4 + kg) of the slab, lane (kg, n) its sum
+        static_for<kQuads>([&](auto Q) __attribute__((always_inline)) {
+            constexpr int q = decltype(Q)::value;
+            const int gs = q * 4 + kg;
+            const bool there = gs < (live < kGroups ? live : kGroups);
+            bf16x8 sums[NT];
+            static_for<NT>([&](auto TT) __attribute__((always_inline)) { sums[decltype(TT)::value] = hidden_sums(stage, sl, decltype(TT)::value, q); });
+            static_for<RB>([&](auto B) __attribute__((always_inline)) {
+                constexpr int b = decltype(B)::value;
+                const float scale = w[b].scale_of(q, kg);
+                const uint32_t z = ZEROS ? w[b].zero_of(q, kg) : 8u;
+                const float c = there ? -scale * (float)(16u + z) : 0.0f;
+                const uint32_t hi = __float_as_uint(c) & 0xFFFF0000u, lo = __float_as_uint(c - __uint_as_float(hi));
+                const bf16x8 cs = __builtin_bit_cast(bf16x8, u32x4{halves(hi, hi), halves(hi, lo), halves(lo, lo), 0u});
+                static_for<NT>([&](auto TT) __attribute__((always_inline)) {
+                    constexpr int t = decltype(TT)::value;
+                    acc[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sums[t], cs, acc[b][t], 0, 0, 0);
+                });
+            });
+        });
+    };
+
+    // Lane (kg, v): rows 4 kg ... 4 kg + 3 of a tile of hidden states, row v of the block.
+    auto store = [&]() __attribute__((always_inline)) {
+        static_for<RB>([&](auto B) __attribute__((always_inline)) {
+            constexpr int b = decltype(B)::value;
+            const int r = (first_block(pass) + b) * 16 + v;
+            const bool in_pass = b < a.per_pass && first_block(pass) + b < mine;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = t * 16 + kg * 4 + i;
+                    if (in_pass && r < row_end && n < rows_here) {
+                        if (a.f32_out)
+                            reinterpret_cast<float *>(a.out)[(n0 + n) * a.ld + row0 + r] = acc[b][t][i];
+                        else
+                            store_element<0>(reinterpret_cast<uint16_t *>(a.out) + (n0 + n) * a.ld + row0 + r, acc[b][t][i]);
+                    }
+                    acc[b][t][i] = 0.0f;
+                }
+        });
+    };
+    // The shares of a team's waves are added up, in the order of their slabs.
+    auto join = [&]() __attribute__((always_inline)) {
+        auto share = [&](int w, int b, int t) { return reinterpret_cast<f32x4 *>(lds_code[w]) + (b * NT + t) * 64 + lane; };
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) *share(wave, b, t) = acc[b][t];
+        barrier();
+        if (ks == 0)
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 1; i < KS; ++i) acc[b][t] += *share(wave + i, b, t);
+        barrier();
+    };
+
+    // Loads go out in the order of the loop below, from the start on, and stay in it: waits count what has gone out since.
+    fetch_hidden(0);
+    static_for<D - 1>([&](auto U) __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_head(slab[decltype(U)::value]);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    put_hidden(0);
+    int n_put = per > 1 ? 1 : 0;  // the next step to put in LDS
+    fetch_hidden(n_put);
+    __builtin_amdgcn_sched_barrier(0);
+    fetch_head(slab[D - 1]);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (RESIDENT) barrier();
+    for (int at0 = 0; at0 < total; at0 += D) {  // (whole rounds of D: the steps past the end have no blocks)
+        static_for<D>([&](auto U) __attribute__((always_inline)) {
+            constexpr int u = decltype(U)::value;
+            const int at = at0 + u;
+            if constexpr (!RESIDENT) barrier();  // the step's hidden states are in LDS, and nobody reads those before them any more
+            multiply(slab[u], at & 1);
+            if (++step == per) {
+                if constexpr (KS > 1) join();
+                if (ks == 0) store();
+                if constexpr (KS > 1)
+#pragma unroll
+                    for (int b = 0; b < RB; ++b)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) acc[b][t] = zero;
+                step = 0;
+                ++pass;
+            }
+            put_hidden((at + 1) & 1);
+            n_put = n_put + 1 < per ? n_put + 1 : 0;
+            fetch_hidden(n_put);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch_head(slab[u]);
+            __builtin_amdgcn_sched_barrier(0);
+        });
     }
 }
 
-int launch_int4_product(const void *h, int h_dtype, int64_t N, int64_t d, int64_t ldh, const Int4Matrix &m, void *out, int dtype, int64_t ld,
-                        hipStream_t stream)
+// Heads of fewer blocks of 16 rows than the waves of the device: the slabs of a row are shared (by a rule on the head alone, so that a row's
+// sums do not depend on the rows beside it).
+static bool shared_slabs(int64_t V) { return (V + 15) / 16 < 256 * kProductWaves / 2; }
+// Whether N hidden states stay in LDS.
+static bool resident(int64_t N, int64_t K, int group, int parts)
 {
-    const dim3 grid((unsigned)((m.V + kWaves - 1) / kWaves), (unsigned)((N + kInt4Rows - 1) / kInt4Rows));
-#define RUN(HT, DT) \
-    int4_product_kernel<HT, DT><<<grid, dim3(kBlock), 0, stream>>>((const Elem<HT>::type *)h, N, d, ldh, m, (Elem<DT>::type *)out, ld)
-    if (h_dtype == 0) {
-        if (dtype == 0) RUN(0, 0); else RUN(0, 1);
-    } else {
-        if (dtype == 0) RUN(1, 0); else RUN(1, 1);
+    const int64_t slabs = (K + kSlab - 1) / kSlab;
+    return N <= 16 && N * (parts * (slabs * kSlab * 2 + 16) + (slabs * (kSlab / group) + 2) * 8) <= kHiddenBytes;
+}
+
+template <int HT, bool RESIDENT, int NT, int KS, int RB, int D>
+static void run_product(Int4Product a, hipStream_t stream)
+{
+    constexpr int kTeams = kProductWaves / KS;
+    const int64_t blocks = (a.m.V + 15) / 16, grid = blocks < 256 ? blocks : 256;
+    const int64_t most = (blocks + grid - 1) / grid, each = (most + kTeams - 1) / kTeams;  // blocks of a workgroup, of a team
+    a.passes = (int)((each + RB - 1) / RB);
+    a.per_pass = (int)((each + a.passes - 1) / a.passes);
+    const unsigned tiles = (unsigned)((a.N + 16 * NT - 1) / (16 * NT));
+    auto run = [&](auto G) {
+        constexpr int group = decltype(G)::value;
+        if constexpr (!RESIDENT)
+            int4_image_kernel<HT, group><<<dim3(tiles * NT * 2, (unsigned)((a.m.K + kSlab - 1) / kSlab)), dim3(kBlock), 0, stream>>>(
+                (const typename Elem<HT>::type *)a.h, a.N, a.d, a.ldh, (int)(tiles * NT), const_cast<uint8_t *>(a.image));
+        if (a.m.zeros)
+            int4_product_kernel<HT, RESIDENT, NT, KS, group, true, RB, D><<<dim3((unsigned)grid, tiles), dim3(kProductThreads), 0, stream>>>(a);
+        else
+            int4_product_kernel<HT, RESIDENT, NT, KS, group, false, RB, D><<<dim3((unsigned)grid, tiles), dim3(kProductThreads), 0, stream>>>(a);
+    };
+    a.m.group == 32 ? run(std::integral_constant<int, 32>()) : a.m.group == 64 ? run(std::integral_constant<int, 64>()) : run(std::integral_constant<int, 128>());
+}
+
+constexpr int kShortRows = 8;  // hidden states of a pass over the head
+
+// Rows of fewer than eight elements, whose hidden states do not fill 16 bytes: a thread a row of the head.
+template <int HT>
+__global__ __launch_bounds__(kBlock) void int4_short_kernel(Int4Product a)
+{
+    const int64_t v = (int64_t)blockIdx.x * kBlock + threadIdx.x, n0 = (int64_t)blockIdx.y * kShortRows;
+    if (v >= a.m.V) return;
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(a.m.codes + v * (a.m.K / 2));
+    const int64_t g = v * (a.m.K / a.m.group);
+    const float s = __uint_as_float((uint32_t)a.m.scales[g] << 16), z = a.m.zeros ? (float)a.m.zeros[g] : 8.0f;
+    for (int64_t n = n0; n < n0 + kShortRows && n < a.N; ++n) {
+        const typename Elem<HT>::type *row = reinterpret_cast<const typename Elem<HT>::type *>(a.h) + n * a.ldh;
+        float sum = 0.0f;
+        for (int k = 0; k < (int)a.d; ++k) sum = __builtin_fmaf((float)(w >> (4 * k) & 15u) - z, Elem<HT>::to_float(row[k]), sum);
+        if (a.f32_out)
+            reinterpret_cast<float *>(a.out)[n * a.ld + v] = s * sum;
+        else
+            store_element<0>(reinterpret_cast<uint16_t *>(a.out) + n * a.ld + v, s * sum);
     }
-#undef RUN
+}
+
+// Rows of hidden states whose image is made at once, and tiles of them that it holds.
+static int64_t image_rows(int64_t N) { return N < 1024 ? (N + 63) / 64 * 64 : 1024; }
+
+size_t int4_product_workspace_bytes(int64_t N, int64_t d, int dtype, int group)
+{
+    const int64_t K = (d + kInt4Slab - 1) / kInt4Slab * kInt4Slab;
+    const int parts = dtype == 0 ? 1 : 3;
+    if (d < 8 || resident(N, K, group, parts)) return 0;
+    return (size_t)(image_rows(N) / 16 * ((K + kSlab - 1) / kSlab) * (parts * 8 + (kSlab / group + 3) / 4) * kFragment);
+}
+
+int launch_int4_product(const void *h, int h_dtype, int64_t N, int64_t d, int64_t ldh, const Int4Matrix &m, void *out, int dtype, int64_t ld,
+                        void *workspace, hipStream_t stream)
+{
+    const int64_t most = 1024;  // rows of hidden states of a launch
+    const bool stay = resident(N, m.K, m.group, h_dtype == 0 ? 1 : 3), shared = shared_slabs(m.V);
+    for (int64_t n = 0; n < N; n += most) {
+        const Int4Product a{(const char *)h + n * ldh * (h_dtype == 0 ? 2 : 4), N - n < most ? N - n : most, d, ldh, m,
+                            (char *)out + n * ld * (dtype == 0 ? 2 : 4), ld, dtype != 0, 0, 0, (const uint8_t *)workspace};
+        if (d < 8) {
+            const dim3 grid((unsigned)((m.V + kBlock - 1) / kBlock), (unsigned)((a.N + kShortRows - 1) / kShortRows));
+            if (h_dtype == 0)
+                int4_short_kernel<0><<<grid, dim3(kBlock), 0, stream>>>(a);
+            else
+                int4_short_kernel<1><<<grid, dim3(kBlock), 0, stream>>>(a);
+        } else if (h_dtype == 0) {
+            if (stay)
+                shared ? run_product<0, true, 1, 4, 1, 4>(a, stream) : run_product<0, true, 1, 1, 1, 6>(a, stream);
+            else if (shared)
+                run_product<0, false, 1, 4, 1, 3>(a, stream);
+            else
+                a.N <= 32 ? run_product<0, false, 2, 1, 2, 3>(a, stream) : run_product<0, false, 4, 1, 2, 2>(a, stream);
+        } else {
+            if (stay)
+                shared ? run_product<1, true, 1, 2, 1, 4>(a, stream) : run_product<1, true, 1, 1, 1, 6>(a, stream);
+            else if (shared)
+                run_product<1, false, 1, 2, 1, 3>(a, stream);
+            else
+                a.N <= 16 ? run_product<1, false, 1, 1, 2, 3>(a, stream) : run_product<1, false, 2, 1, 2, 2>(a, stream);
+        }
+    }
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

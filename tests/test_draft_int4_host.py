@@ -80,18 +80,21 @@ def test_int4_arguments():
     def dequantize(x=FAKE, dt=0, N=4, d=100, ld=100, g=64, codes=FAKE, scales=FAKE, zeros=None):
         return lib.difr_int4_dequantize(codes, scales, zeros, N, d, g, x, dt, ld, None)
 
-    def product(x=FAKE, dt=0, N=4, d=100, ld=100, g=64, codes=FAKE, scales=FAKE, zeros=None, V=50, out=FAKE, odt=0, ldo=50):
-        return lib.difr_int4_product(x, dt, N, d, ld, codes, scales, zeros, V, g, out, odt, ldo, None)
+    def product(x=FAKE, dt=0, N=4, d=100, ld=100, g=64, codes=FAKE, scales=FAKE, zeros=None, V=50, out=FAKE, odt=0, ldo=50, ws=FAKE, n=1 << 40):
+        return lib.difr_int4_product(x, dt, N, d, ld, codes, scales, zeros, V, g, out, odt, ldo, ws, n, None)
 
     for call in (quantize, dequantize, product):
         for bad, want in ((dict(N=-1), SHAPE), (dict(d=0), SHAPE), (dict(ld=99), SHAPE), (dict(N=1 << 31), SHAPE), (dict(d=1 << 24, ld=1 << 24), SHAPE),
                           (dict(g=16), ARG), (dict(g=0), ARG), (dict(g=256), ARG), (dict(dt=2), DTYPE), (dict(x=None), NULL), (dict(codes=None), NULL),
-                          (dict(scales=None), NULL), (dict(x=0x1001), ALIGN), (dict(codes=0x1008), ALIGN), (dict(scales=0x1002), ALIGN)):
+                          (dict(scales=None), NULL), (dict(x=0x1001), ALIGN), (dict(codes=0x1008), ALIGN), (dict(scales=0x1001), ALIGN)):
             assert call(**bad) == want, (call.__name__, bad)
         assert call(N=0, x=None) == OK
     for bad, want in ((dict(V=-1), SHAPE), (dict(V=1 << 31, ldo=1 << 31), SHAPE), (dict(ldo=49), SHAPE), (dict(odt=3), DTYPE), (dict(out=None), NULL),
-                      (dict(out=0x1001), ALIGN), (dict(V=0), OK)):
+                      (dict(out=0x1001), ALIGN), (dict(V=0), OK), (dict(N=40, n=64), SHAPE), (dict(N=40, ws=None), NULL), (dict(N=40, ws=0x1008), ALIGN)):
         assert product(**bad) == want, bad
+    need = lib.difr_int4_product_workspace_bytes
+    assert need(0, 64, 0, 32) == 0 and need(5, 0, 0, 32) == 0 and need(5, 64, 2, 32) == 0 and need(5, 64, 0, 33) == 0 and need(1, 4096, 0, 128) == 0
+    assert 0 < need(17, 4096, 0, 128) < need(65, 4096, 0, 128) and need(17, 4096, 0, 128) < need(17, 4096, 1, 32) and need(5000, 512, 0, 64) == need(9999, 512, 0, 64)
     assert [difr.int4_padded(d) for d in (0, 1, 128, 129)] == [0, 128, 128, 256]
 
 

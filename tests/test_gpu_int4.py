@@ -79,8 +79,9 @@ def _matrix(difr, V, d, group, zero_points, seed, scale_of=None):
     return (c[:, 0::2] | (c[:, 1::2] << 4)).to(DEV), s.to(DEV), None if z is None else z.to(DEV), w[:, :d]
 
 
-SHAPES = [(1, 1, 1), (1, 16, 128), (2, 17, 31), (3, 64, 256), (5, 100, 129), (15, 1000, 1000), (16, 33, 4096), (17, 250, 2000), (31, 129, 512),
-          (33, 1024, 640), (48, 77, 384), (64, 500, 4096), (65, 96, 1024), (130, 40, 896)]
+SHAPES = [(1, 1, 1), (1, 16, 128), (2, 17, 31), (3, 64, 256), (5, 100, 129), (15, 1000, 1000), (16, 33, 4096), (17, 250, 2000), (31, 129, 512), (20, 9001, 700),
+          (33, 1024, 640), (48, 77, 384), (64, 500, 4096), (65, 96, 1024), (130, 40, 896), (16, 70000, 300), (3, 35000, 5000), (40, 40000, 260), (70, 20000, 130),
+          (1100, 33, 200)]
 
 
 @pytest.mark.parametrize("N,V,d", SHAPES)
