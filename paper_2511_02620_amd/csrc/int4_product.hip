@@ -31,9 +31,8 @@ struct Int4Product {
     const uint8_t *image;   // hidden states as the matrix instructions want them (int4_image_kernel), or null
 };
 
-constexpr int kProductWaves = 8, kProductThreads = kProductWaves * 64;
 constexpr int kSlab = 256;                     // elements of a row that a step takes
-constexpr int kHiddenBytes = 140 * 1024;       // of LDS for hidden states that stay there
+constexpr int kHiddenBytes = 122 * 1024;       // of LDS for hidden states that stay there
 
 // The order in which the codes of four bytes come out of two at a time: 0 4 1 5 2 6 3 7.  Hidden states are put in that order in LDS.
 __device__ __forceinline__ u32x4 code_order(u32x4 q)
@@ -196,9 +195,10 @@ __global__ __launch_bounds__(kBlock) void int4_image_kernel(const typename Elem<
 // Hidden states in P parts; NT tiles of 16 of them from the image, a step ahead (RESIDENT: up to 16, converted by each workgroup and kept in
 // LDS); KS slabs at once, each with its share of the waves (small heads, whose blocks are fewer than waves); RB blocks of 16 rows of
 // the head to a wave at a time; D steps of codes in flight, in registers.
-template <int HT, bool RESIDENT, int NT, int KS, int G, bool ZEROS, int RB, int D>
-__global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Product a)
+template <int HT, bool RESIDENT, int NT, int KS, int G, bool ZEROS, int RB, int D, int W, bool PAST>
+__global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
 {
+    constexpr int kProductWaves = W, kProductThreads = W * 64;
     constexpr int P = Eight<HT>::P, kGroups = kSlab / G, kQuads = (kGroups + 3) / 4, F = image_fragments<G, P>();
     constexpr int kSteps = G / 32;     // matrix instructions of a group
     constexpr int kStage = KS * NT * F * kFragment, kPieces = (kStage / 16 + kProductThreads - 1) / kProductThreads;
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Pr
     auto aim = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
-            const int r = (first_block(f_pass) + b) * 16;
+            const int r = (first_block(f_pass) + min(b, a.per_pass - 1)) * 16;
             at_code[b][0] = (uint32_t)min(r + (lane >> 3), row_end - 1) * (uint32_t)pitch;
             at_code[b][1] = (uint32_t)min(r + 8 + (lane >> 3), row_end - 1) * (uint32_t)pitch;
             at_group[b] = (uint32_t)min(r + (lane >> 2), row_end - 1) * (uint32_t)groups;
@@ -312,7 +312,13 @@ __global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Pr
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) to[b].w[i] = *reinterpret_cast<const u32x4 *>(c0 + (at_code[b][i] + part * 16));
+            for (int i = 0; i < 2; ++i) {
+                const u32x4 *const from = reinterpret_cast<const u32x4 *>(c0 + (at_code[b][i] + part * 16));
+                if constexpr (PAST)
+                    to[b].w[i] = __builtin_nontemporal_load(from);
+                else
+                    to[b].w[i] = *from;
+            }
             if constexpr (G == 128) {
                 to[b].s = *reinterpret_cast<const u16_any *>(s0 + (2 * at_group[b] + own * 2));
                 if constexpr (ZEROS) to[b].z = *(z0 + (at_group[b] + zown));
@@ -378,11 +384,9 @@ __global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Pr
         for (int t = 0; t < NT; ++t) acc[b][t] = zero;
 
     int pass = 0, step = 0;
-    auto multiply = [&](const Int4Fetched (&fetched)[RB], int stage) __attribute__((always_inline)) {
+    auto multiply = [&](const Int4Slab<G> (&w)[RB], int stage) __attribute__((always_inline)) {
         const int sl = step * KS + ks;
         if (sl >= nslab || first_block(pass) >= mine) return;
-        Int4Slab<G> w[RB];
-        deal(fetched, w);
         // groups of the slab that count (none of the second half of half a slab, whose codes are the first's again and whose states are 0)
         const int live = sl + 1 == nslab ? live_groups - sl * kGroups : kGroups;
         static_for<2>([&](auto SEG) __attribute__((always_inline)) {
@@ -476,7 +480,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Pr
 
     // Loads go out in the order of the loop below, from the start on, and stay in it: waits count what has gone out since.
     fetch_hidden(0);
-    static_for<D - 1>([&](auto U) __attribute__((always_inline)) {
+    static_for<D>([&](auto U) __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
         fetch_head(slab[decltype(U)::value]);
     });
@@ -485,15 +489,18 @@ __global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Pr
     int n_put = per > 1 ? 1 : 0;  // the next step to put in LDS
     fetch_hidden(n_put);
     __builtin_amdgcn_sched_barrier(0);
-    fetch_head(slab[D - 1]);
-    __builtin_amdgcn_sched_barrier(0);
     if constexpr (RESIDENT) barrier();
     for (int at0 = 0; at0 < total; at0 += D) {  // (whole rounds of D: the steps past the end have no blocks)
         static_for<D>([&](auto U) __attribute__((always_inline)) {
             constexpr int u = decltype(U)::value;
             const int at = at0 + u;
             if constexpr (!RESIDENT) barrier();  // the step's hidden states are in LDS, and nobody reads those before them any more
-            multiply(slab[u], at & 1);
+            Int4Slab<G> w[RB];
+            deal(slab[u], w);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch_head(slab[u]);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(w, at & 1);
             if (++step == per) {
                 if constexpr (KS > 1) join();
                 if (ks == 0) store();
@@ -509,15 +516,13 @@ __global__ __launch_bounds__(kProductThreads, 1) void int4_product_kernel(Int4Pr
             n_put = n_put + 1 < per ? n_put + 1 : 0;
             fetch_hidden(n_put);
             __builtin_amdgcn_sched_barrier(0);
-            fetch_head(slab[u]);
-            __builtin_amdgcn_sched_barrier(0);
         });
     }
 }
 
 // Heads of fewer blocks of 16 rows than the waves of the device: the slabs of a row are shared (by a rule on the head alone, so that a row's
 // sums do not depend on the rows beside it).
-static bool shared_slabs(int64_t V) { return (V + 15) / 16 < 256 * kProductWaves / 2; }
+static bool shared_slabs(int64_t V) { return (V + 15) / 16 < 1024; }
 // Whether N hidden states stay in LDS.
 static bool resident(int64_t N, int64_t K, int group, int parts)
 {
@@ -525,10 +530,10 @@ static bool resident(int64_t N, int64_t K, int group, int parts)
     return N <= 16 && N * (parts * (slabs * kSlab * 2 + 16) + (slabs * (kSlab / group) + 2) * 8) <= kHiddenBytes;
 }
 
-template <int HT, bool RESIDENT, int NT, int KS, int RB, int D>
+template <int HT, bool RESIDENT, int NT, int KS, int RB, int D, int W>
 static void run_product(Int4Product a, hipStream_t stream)
 {
-    constexpr int kTeams = kProductWaves / KS;
+    constexpr int kTeams = W / KS;
     const int64_t blocks = (a.m.V + 15) / 16, grid = blocks < 256 ? blocks : 256;
     const int64_t most = (blocks + grid - 1) / grid, each = (most + kTeams - 1) / kTeams;  // blocks of a workgroup, of a team
     a.passes = (int)((each + RB - 1) / RB);
@@ -539,10 +544,15 @@ static void run_product(Int4Product a, hipStream_t stream)
         if constexpr (!RESIDENT)
             int4_image_kernel<HT, group><<<dim3(tiles * NT * 2, (unsigned)((a.m.K + kSlab - 1) / kSlab)), dim3(kBlock), 0, stream>>>(
                 (const typename Elem<HT>::type *)a.h, a.N, a.d, a.ldh, (int)(tiles * NT), const_cast<uint8_t *>(a.image));
-        if (a.m.zeros)
-            int4_product_kernel<HT, RESIDENT, NT, KS, group, true, RB, D><<<dim3((unsigned)grid, tiles), dim3(kProductThreads), 0, stream>>>(a);
+        auto go = [&](auto ZEROS, auto PAST) {
+            int4_product_kernel<HT, RESIDENT, NT, KS, group, decltype(ZEROS)::value, RB, D, W, decltype(PAST)::value>
+                <<<dim3((unsigned)grid, tiles), dim3(W * 64), 0, stream>>>(a);
+        };
+        // a matrix larger than the 256 MB Infinity Cache is read past it
+        if (KS == 1 && a.m.V * a.m.K / 2 > (int64_t)256 << 20)
+            a.m.zeros ? go(std::true_type(), std::bool_constant<KS == 1>()) : go(std::false_type(), std::bool_constant<KS == 1>());
         else
-            int4_product_kernel<HT, RESIDENT, NT, KS, group, false, RB, D><<<dim3((unsigned)grid, tiles), dim3(kProductThreads), 0, stream>>>(a);
+            a.m.zeros ? go(std::true_type(), std::false_type()) : go(std::false_type(), std::false_type());
     };
     a.m.group == 32 ? run(std::integral_constant<int, 32>()) : a.m.group == 64 ? run(std::integral_constant<int, 64>()) : run(std::integral_constant<int, 128>());
 }
@@ -596,18 +606,18 @@ int launch_int4_product(const void *h, int h_dtype, int64_t N, int64_t d, int64_
                 int4_short_kernel<1><<<grid, dim3(kBlock), 0, stream>>>(a);
         } else if (h_dtype == 0) {
             if (stay)
-                shared ? run_product<0, true, 1, 4, 1, 4>(a, stream) : run_product<0, true, 1, 1, 1, 6>(a, stream);
+                shared ? run_product<0, true, 1, 4, 1, 3, 16>(a, stream) : run_product<0, true, 1, 1, 1, 4, 16>(a, stream);
             else if (shared)
-                run_product<0, false, 1, 4, 1, 3>(a, stream);
+                run_product<0, false, 1, 4, 1, 2, 8>(a, stream);
             else
-                a.N <= 32 ? run_product<0, false, 2, 1, 2, 3>(a, stream) : run_product<0, false, 4, 1, 2, 2>(a, stream);
+                a.N <= 32 ? run_product<0, false, 2, 1, 1, 2, 16>(a, stream) : a.N <= 48 ? run_product<0, false, 3, 1, 2, 2, 8>(a, stream) : run_product<0, false, 4, 1, 2, 1, 8>(a, stream);
         } else {
             if (stay)
-                shared ? run_product<1, true, 1, 2, 1, 4>(a, stream) : run_product<1, true, 1, 1, 1, 6>(a, stream);
+                shared ? run_product<1, true, 1, 2, 1, 3, 16>(a, stream) : run_product<1, true, 1, 1, 1, 3, 16>(a, stream);
             else if (shared)
-                run_product<1, false, 1, 2, 1, 3>(a, stream);
+                run_product<1, false, 1, 2, 1, 2, 8>(a, stream);
             else
-                a.N <= 16 ? run_product<1, false, 1, 1, 2, 3>(a, stream) : run_product<1, false, 2, 1, 2, 2>(a, stream);
+                a.N <= 16 ? run_product<1, false, 1, 1, 4, 1, 8>(a, stream) : run_product<1, false, 2, 1, 3, 1, 8>(a, stream);
         }
     }
     return hipGetLastError() == hipSuccess ? 0 : 1;
