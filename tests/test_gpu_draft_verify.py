@@ -418,3 +418,33 @@ def test_draws_near_each_border(difr):
     got = difr.tree_verify(x.repeat(R, 1).to(DEV), 1.0, torch.empty(0, dtype=torch.int32, device=DEV), None,
                            torch.zeros(R + 1, dtype=torch.int64, device=DEV), torch.tensor(u, dtype=torch.float32).to(DEV))["tokens"].tolist()
     assert [a for a, s in zip(got, sure) if s] == [a for a, s in zip(want, sure) if s]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_batches_of_chains(difr, dtype):
+    """Batches that are taken level by level: chains of one length, of many, longer than the levels that are launched, and without drafts' logits."""
+    V = 33000
+    for counts, drift, with_draft in (([3] * 140, 0.4, True), ([i % 4 for i in range(150)], 0.5, True), ([1] * 130 + [17], 0.02, True),
+                                      ([i % 3 for i in range(270)], 0.0, False)):
+        case = list(_chains(len(counts), counts, V, dtype, drift, spread=0.5 if with_draft else 6.0))
+        if not with_draft:
+            case[3] = case[2].float().argmax(1).int()                    # the likeliest token: such drafts stand now and then
+        case[1][5] = math.nan                                            # some sequences end early
+        case[3][4] = V + 7
+        got, _ = _check_chain(difr, tuple(case), 0.9, 0.8 if drift > 0.1 else 0.9, with_draft)
+        assert got["accepted"].max() >= min(2, max(counts))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_batches_of_trees(difr, dtype):
+    V = 40000
+    case = _trees(17, [12, 0, 14, 13] * 22, V, dtype, hit=0.9)
+    T = torch.rand(88 + 39 * 22, generator=torch.Generator().manual_seed(3)) + 0.5
+    case[2][3] = math.nan
+    _hit(case, T, 5)
+    assert int(_check_tree(difr, case, T)["accepted"].max()) >= 3
+    # chains deeper than the levels that are launched
+    case = _trees(18, [10] * 90, V, dtype, hit=1.0)
+    case = (case[0], None) + case[2:]
+    _hit(case, torch.ones(990), 1)
+    assert _check_tree(difr, case, 1.0)["accepted"].tolist() == [10] * 90
