@@ -641,7 +641,7 @@ int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64
  * has the tokens [offsets[b], offsets[b + 1]) and one row of logits more than tokens, rows offsets[b] + b ... offsets[b + 1] + b: row 0 is
  * the position after the last token that is certain.  offsets [B + 1] is non-decreasing from 0 to D (what is outside is held in [0, D]).
  * A masked logit (-inf, the type's lowest value) has no probability, and a masked token is never emitted.
- * Weights of a row, exp((x - its largest logit) / T), and their sums are fp64, good to 2^-50; the result does not depend on the order in
+ * Weights of a row, exp((x - its largest logit) / T), and their sums are fp64, good to 2^-45; the result does not depend on the order in
  * which workgroups run.  Random numbers are the caller's: fp32 in [0, 1); what is below (NaN too) counts as 0, what is above as the largest.
  */
 typedef struct {
@@ -668,8 +668,8 @@ typedef struct {
  * to a row, of the target or the draft, that holds a NaN, +inf or no finite logit, or whose temperature is not positive and finite, ends
  * there: token -1, logp NaN, DIFR_FLAG_NONFINITE.  Rows that a sequence does not come to may hold anything.
  * workspace  DEVICE scratch of difr_draft_workspace_bytes(B, D, V, dtype, draft != NULL) bytes (host only), 64-byte aligned, contents
- * irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small: DIFR_ERR_SHAPE.  D + B rows of ceil(V / 2048)
- * cells each: fewer than 2^26 cells.
+ * irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small: DIFR_ERR_SHAPE.  (D + B) ceil(V / 1024) < 2^25 - 32,
+ * else DIFR_ERR_SHAPE.
  */
 typedef struct {
     const void *draft;

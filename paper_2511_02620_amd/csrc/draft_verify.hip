@@ -3,7 +3,7 @@
 //
 // What is decided here are whole numbers: u q < p, and the first token whose cumulative weight passes u of the whole, among 150,000
 // weights many of which are 1e-7 and less.  Sums good to 2^-24 would choose another token in one row of some hundreds, so weights are
-// formed and summed in 64 bits throughout: 2^((x - m) log2(e) / T), good to 2^-50, relative to the largest logit m of what is summed.
+// formed and summed in 64 bits throughout: 2^((x - m) log2(e) / T), good to 2^-45, relative to the largest logit m of what is summed.
 // fp64 multiply-adds run at the rate of fp32 ones here; a weight is some 20 instructions, which is what bounds large batches (a pass over
 // a row of 151,936 logits is 0.075 us of the whole device, reading it 0.045).
 //
@@ -24,26 +24,28 @@ constexpr int kCell = 1024;
 // way, and a masked entry stays masked).
 __device__ __forceinline__ double exponent_factor(float T) { return 1.44269504088896340736 / (double)fminf(T, 0x1p100f); }
 
+// The least difference of logits that is told from what is below it: a weight of 2^-1000.
+__device__ __forceinline__ double least_of(float T) { return (double)fminf(T, 0x1p100f) * (-1000.0 / 1.44269504088896340736); }
+
 struct Weight {
-    double m, c, least;  // reference, log2(e) / T, and the least difference that is told from what is below it (a weight of 2^-1000)
-    __device__ __forceinline__ Weight(float top, double factor) : m((double)top), c(factor), least(-1000.0 / factor) {}
+    double m, c, least;  // reference, log2(e) / T, least difference
+    __device__ __forceinline__ Weight(float top, double factor, double least_) : m((double)top), c(factor), least(least_) {}
     // 2^((x - m) c): the whole part of the exponent goes into the exponent field, the rest, within 1/2 of 0, through a polynomial
-    // (Chebyshev interpolation of 2^f in degree 10: relative error 3.2e-16)
+    // (Chebyshev interpolation of 2^f in degree 9: relative error 1.9e-14)
     __device__ __forceinline__ double at(float x) const
     {
         double d = (double)x - m;
         d = __builtin_fmax(d, least);
         const double t = __builtin_fma(d, c, 0x1.8p52), n = t - 0x1.8p52, f = __builtin_fma(d, c, -n);
-        double p = 0x1.e6063f7217bc6p-28;
-        p = __builtin_fma(p, f, 0x1.b675bca4eeebbp-24);
-        p = __builtin_fma(p, f, 0x1.62bfd47773353p-20);
-        p = __builtin_fma(p, f, 0x1.ffcb54062e698p-17);
-        p = __builtin_fma(p, f, 0x1.430913096fd9fp-13);
-        p = __builtin_fma(p, f, 0x1.5d87fe9d7a584p-10);
-        p = __builtin_fma(p, f, 0x1.3b2ab6fba1ddap-7);
-        p = __builtin_fma(p, f, 0x1.c6b08d703ce49p-5);
-        p = __builtin_fma(p, f, 0x1.ebfbdff82c598p-3);
-        p = __builtin_fma(p, f, 0x1.62e42fefa3a19p-1);
+        double p = 0x1.b6571de2f2351p-24;
+        p = __builtin_fma(p, f, 0x1.63ef969a64d3cp-20);
+        p = __builtin_fma(p, f, 0x1.ffcb76789860fp-17);
+        p = __builtin_fma(p, f, 0x1.43088e257f341p-13);
+        p = __builtin_fma(p, f, 0x1.5d87fe908f88ap-10);
+        p = __builtin_fma(p, f, 0x1.3b2ab72b175eep-7);
+        p = __builtin_fma(p, f, 0x1.c6b08d7044119p-5);
+        p = __builtin_fma(p, f, 0x1.ebfbdff8149f2p-3);
+        p = __builtin_fma(p, f, 0x1.62e42fefa39f7p-1);
         p = __builtin_fma(p, f, 1.0);
         // (the low half of t is the whole part; with what is shifted out of the field it is at least -1000)
         return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
@@ -99,7 +101,7 @@ struct CellStats {
 struct Stop {
     double rho;             // S_p / S_q: weights of the draft in units of the target's
     double p_sum;           // S_p, relative to p_top
-    double p_factor, q_factor;
+    float p_T, q_T;
     float p_top, q_top;
     int32_t place;          // row of the sequence where it stops
     int32_t kind;
@@ -113,6 +115,7 @@ struct Workspace {
     int32_t *depth;           // [B]: trees: tokens accepted so far
 };
 constexpr int32_t kDone = -2;
+constexpr int kMany = 2;  // cells of a wave in large batches: what a row needs is formed once for them, and more is in flight
 
 static int64_t cells_of(int64_t V) { return (V + kCell - 1) / kCell; }
 
@@ -121,7 +124,7 @@ template <int DT>
 struct Cell {
     static constexpr int E = Elem<DT>::kPerVec, kVectors = kCell / (64 * E);
     u32x4 q[kVectors];
-    __device__ __forceinline__ Cell(const typename Elem<DT>::type *row, int64_t first, int64_t V, int lane)
+    __device__ __forceinline__ void load(const typename Elem<DT>::type *row, int64_t first, int64_t V, int lane)
     {
         if (first + kCell <= V) {
 #pragma unroll
@@ -137,42 +140,51 @@ struct Cell {
     }
 };
 
-template <int DT>
-__device__ __forceinline__ void cell_stats(const typename Elem<DT>::type *row, int64_t cell, int64_t V, float T, const CellStats &out, int64_t id, int lane)
+// Statistics of CELLS cells of a row from `cell` on, which are all read before the first is summed.  `id`: the first one's place.
+template <int DT, int CELLS>
+__device__ __forceinline__ void cell_stats(const typename Elem<DT>::type *row, uint32_t cell, uint32_t cells, int64_t V, float T, const CellStats &out,
+                                           int64_t id, int lane)
 {
     constexpr int E = Elem<DT>::kPerVec;
-    const Cell<DT> c(row, cell * kCell, V, lane);
-    float top = -INFINITY;
-    bool bad = false;
+    Cell<DT> c[CELLS];
 #pragma unroll
-    for (int i = 0; i < Cell<DT>::kVectors; ++i) {
-        float x[E];
-        unpack_vector<DT>(c.q[i], x);
+    for (int k = 0; k < CELLS; ++k) c[k].load(row, (int64_t)(cell + k < cells ? cell + k : cells - 1) * kCell, V, lane);
+    const double factor = exponent_factor(T), least = least_of(T);
 #pragma unroll
-        for (int j = 0; j < E; j += 2) {
-            top = fmaxf(top, fmaxf(x[j], x[j + 1]));
-            bad |= __builtin_isunordered(x[j], x[j + 1]);
-        }
-    }
-    top = wave_top(top);
-    double sum = 0.0;
-    if (__any(bad) || top == INFINITY) {
-        top = NAN;
-    } else if (top > -INFINITY) {
-        const Weight w(top, exponent_factor(T));
-        double part[2] = {0.0, 0.0};
+    for (int k = 0; k < CELLS; ++k) {
+        if (cell + k >= cells) break;
+        float top = -INFINITY;
+        bool bad = false;
 #pragma unroll
         for (int i = 0; i < Cell<DT>::kVectors; ++i) {
             float x[E];
-            unpack_vector<DT>(c.q[i], x);
+            unpack_vector<DT>(c[k].q[i], x);
 #pragma unroll
-            for (int j = 0; j < E; ++j) part[j & 1] += w.at(x[j]);
+            for (int j = 0; j < E; j += 2) {
+                top = fmaxf(top, fmaxf(x[j], x[j + 1]));
+                bad |= __builtin_isunordered(x[j], x[j + 1]);
+            }
         }
-        sum = wave_sum64(part[0] + part[1]);
-    }
-    if (lane == 0) {
-        out.sum[id] = sum;
-        out.top[id] = top;
+        top = wave_top(top);
+        double sum = 0.0;
+        if (__any(bad) || top == INFINITY) {
+            top = NAN;
+        } else if (top > -INFINITY) {
+            const Weight w(top, factor, least);
+            double part[2] = {0.0, 0.0};
+#pragma unroll
+            for (int i = 0; i < Cell<DT>::kVectors; ++i) {
+                float x[E];
+                unpack_vector<DT>(c[k].q[i], x);
+#pragma unroll
+                for (int j = 0; j < E; ++j) part[j & 1] += w.at(x[j]);
+            }
+            sum = wave_sum64(part[0] + part[1]);
+        }
+        if (lane == 0) {
+            out.sum[id + k] = sum;
+            out.top[id + k] = top;
+        }
     }
 }
 
@@ -191,71 +203,75 @@ struct Span {
     }
 };
 
-// Statistics of all cells: of the target's rows, then of the draft's.  A wave a cell.
-template <int DT>
-__global__ __launch_bounds__(kBlock) void all_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, uint32_t cells, uint32_t total)
+// Statistics of all cells: of the target's rows, then of the draft's.  A wave CELLS cells of a row, of which there are `groups`.
+template <int DT, int CELLS>
+__global__ __launch_bounds__(kBlock) void all_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, uint32_t cells, uint32_t groups, uint32_t total)
 {
     typedef typename Elem<DT>::type elem;
     const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (id >= total) return;
-    const uint32_t row = id / cells, cell = id - row * cells, R = (uint32_t)(b.D + b.B);
-    const int lane = threadIdx.x & 63;
-    if (row < R)
-        cell_stats<DT>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell, b.V, row_temperature(b, row), ws.target, id, lane);
-    else
-        cell_stats<DT>(reinterpret_cast<const elem *>(c.draft) + (row - R) * c.ld, cell, b.V, draft_temperature(c, row - R), ws.draft,
-                       id - (int64_t)R * cells, lane);
+    const uint32_t row = id / groups, cell = (id - row * groups) * CELLS, R = (uint32_t)(b.D + b.B);
+    const bool of_draft = row >= R;
+    const int64_t at = of_draft ? row - R : row;
+    const elem *const p = of_draft ? reinterpret_cast<const elem *>(c.draft) + at * c.ld : reinterpret_cast<const elem *>(b.logits) + at * b.ld;
+    cell_stats<DT, CELLS>(p, cell, cells, b.V, of_draft ? draft_temperature(c, at) : row_temperature(b, at), of_draft ? ws.draft : ws.target,
+                          at * cells + cell, threadIdx.x & 63);
 }
 
 // Statistics of the rows that the sequences have come to, the target's and the draft's; LAST: of all rows from there on.
 template <int DT, bool LAST>
-__global__ __launch_bounds__(kBlock) void level_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, int level, uint32_t cells, uint32_t total)
+__global__ __launch_bounds__(kBlock) void level_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, int level, uint32_t cells, uint32_t groups, uint32_t total)
 {
     typedef typename Elem<DT>::type elem;
     const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (id >= total) return;
-    const uint32_t both = c.draft ? 2 : 1, s = id / (cells * both), of_draft = (id - s * cells * both) / cells, cell = id % cells;
+    const uint32_t both = c.draft ? 2 : 1, r = id / groups, s = r / both, cell = (id - r * groups) * kMany;
+    const bool of_draft = r - s * both != 0;
     if (level && ws.at[s] != level) return;
     const Span span(b, s);
-    const int lane = threadIdx.x & 63;
     for (int64_t i = level; i <= (LAST ? span.drafts : level); ++i) {
-        const int64_t k = span.first_draft + i, row = k + s;
-        if (!of_draft)
-            cell_stats<DT>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell, b.V, row_temperature(b, row), ws.target, row * cells + cell, lane);
-        else if (i < span.drafts)
-            cell_stats<DT>(reinterpret_cast<const elem *>(c.draft) + k * c.ld, cell, b.V, draft_temperature(c, k), ws.draft, k * cells + cell, lane);
+        if (of_draft && i >= span.drafts) break;
+        const int64_t k = span.first_draft + i, at = of_draft ? k : k + s;
+        const elem *const p = of_draft ? reinterpret_cast<const elem *>(c.draft) + at * c.ld : reinterpret_cast<const elem *>(b.logits) + at * b.ld;
+        cell_stats<DT, kMany>(p, cell, cells, b.V, of_draft ? draft_temperature(c, at) : row_temperature(b, at), of_draft ? ws.draft : ws.target,
+                              at * cells + cell, threadIdx.x & 63);
     }
 }
-template <int DT>
-__global__ __launch_bounds__(kBlock) void node_stats_kernel(DraftBatch b, Workspace ws, bool first, uint32_t cells, uint32_t total)
+// The same for trees; LAST: of all rows that may still come.
+template <int DT, bool LAST>
+__global__ __launch_bounds__(kBlock) void node_stats_kernel(DraftBatch b, Workspace ws, bool first, uint32_t cells, uint32_t groups, uint32_t total)
 {
     typedef typename Elem<DT>::type elem;
     const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (id >= total) return;
-    const uint32_t s = id / cells, cell = id - s * cells;
+    const uint32_t s = id / groups, cell = (id - s * groups) * kMany;
     const int32_t node = first ? -1 : ws.at[s];
     if (node == kDone) return;
-    const int64_t row = Span(b, s).first_draft + s + node + 1;
-    cell_stats<DT>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell, b.V, row_temperature(b, row), ws.target, row * cells + cell, threadIdx.x & 63);
+    const Span span(b, s);
+    for (int64_t j = node; j < (LAST ? span.drafts : node + 1); ++j) {  // (only nodes behind this one can follow it)
+        const int64_t row = span.first_draft + s + j + 1;
+        cell_stats<DT, kMany>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell, cells, b.V, row_temperature(b, row), ws.target,
+                              row * cells + cell, threadIdx.x & 63);
+    }
 }
 
-// A whole row from its cells, by 16 lanes: sum 0 where it cannot be scored.
+// A whole row from its cells, by a wave: sum 0 where it cannot be scored.
 struct RowStats {
     float top;
     double sum, factor;
 };
-__device__ __forceinline__ RowStats row_stats(const CellStats &s, int64_t row, int64_t cells, float T, int lane16)
+__device__ __forceinline__ RowStats row_stats(const CellStats &s, int64_t row, int64_t cells, float T, int lane)
 {
     float top = -INFINITY;
     bool bad = !(T > 0.0f && T < INFINITY);
     const float *tops = s.top + row * cells;
     const double *sums = s.sum + row * cells;
-    constexpr int kHeld = 10;  // of the first cells are loaded at once: 160 of them
+    constexpr int kHeld = 3;  // of the first cells are loaded at once: 192 of them
     float t[kHeld];
     double v[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-        const int64_t c = lane16 + 16 * i;
+        const int64_t c = lane + 64 * i;
         t[i] = c < cells ? tops[c] : -INFINITY;
         v[i] = c < cells ? sums[c] : 0.0;
     }
@@ -264,30 +280,23 @@ __device__ __forceinline__ RowStats row_stats(const CellStats &s, int64_t row, i
         bad |= t[i] != t[i];
         top = fmaxf(top, t[i]);
     }
-    for (int64_t c = lane16 + 16 * kHeld; c < cells; c += 16) {
+    for (int64_t c = lane + 64 * kHeld; c < cells; c += 64) {
         bad |= tops[c] != tops[c];
         top = fmaxf(top, tops[c]);
     }
-    int any = bad;
-#pragma unroll
-    for (int o = 8; o; o >>= 1) {
-        top = fmaxf(top, __shfl_xor(top, o));
-        any |= __shfl_xor(any, o);
-    }
+    top = wave_top(top);
     RowStats r{NAN, 0.0, 1.0};
-    if (any || top == -INFINITY) return r;
+    if (__any(bad) || top == -INFINITY) return r;
     r.top = top;
     r.factor = exponent_factor(T);
-    const Weight w(top, r.factor);
+    const Weight w(top, r.factor, least_of(T));
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
         if (t[i] > -INFINITY) sum += v[i] * w.at(t[i]);
-    for (int64_t c = lane16 + 16 * kHeld; c < cells; c += 16)
+    for (int64_t c = lane + 64 * kHeld; c < cells; c += 64)
         if (tops[c] > -INFINITY) sum += sums[c] * w.at(tops[c]);
-#pragma unroll
-    for (int o = 8; o; o >>= 1) sum += __shfl_xor(sum, o);
-    r.sum = sum;
+    r.sum = wave_sum64(sum);
     return r;
 }
 
@@ -297,103 +306,107 @@ __device__ __forceinline__ float logit_at(const void *logits, int64_t row, int64
     return Elem<DT>::to_float(reinterpret_cast<const typename Elem<DT>::type *>(logits)[row * ld + v]);
 }
 
-// Which drafts of a sequence stand, by a workgroup: from row `from` on, whose statistics are there up to row `to` (or the last).  The first
-// eight groups of 16 lanes have a row of the target each, the others the draft's of the same number.  False where rows behind `to` are needed;
-// else `stop` says where the sequence stops.  `write`: outputs too.
+// Which drafts of a sequence stand, by a workgroup of WAVES waves: from row `from` on, whose statistics are there up to row `to` (or the last).
+// A wave has a row of the target, another the draft's of the same number; then lanes 0, 1, ... of the first wave a row each.  False where
+// rows behind `to` are needed; else `stop` says where the sequence stops.  `write`: outputs too.
+template <int WAVES>
 struct DecideLds {
-    float top[16];
-    double sum[16], factor[16], weight[16];  // weight: the drafted token's
+    float top[WAVES], T[WAVES], u[WAVES];
+    double sum[WAVES], weight[WAVES];  // weight: the drafted token's
+    int32_t token[WAVES];
     Stop stop;
     int go;
 };
-template <int DT>
-__device__ bool decide_drafts(const DraftBatch &b, const DraftChain &c, const DraftOutputs &o, const Workspace &ws, int64_t s, const Span &span, int64_t cells,
-                       int64_t from, int64_t to, bool write, DecideLds &lds, Stop &stop, int64_t &reached)
+template <int DT, int WAVES>
+__device__ __forceinline__ bool decide_drafts(const DraftBatch &b, const DraftChain &c, const DraftOutputs &o, const Workspace &ws, int64_t s,
+                                              const Span &span, int64_t cells, int64_t from, int64_t to, bool write, DecideLds<WAVES> &lds,
+                                              Stop &stop, int64_t &reached)
 {
-    const int tid = threadIdx.x, group = tid >> 4, lane16 = tid & 15;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rows = c.draft ? WAVES / 2 : WAVES;  // of a round
     const int64_t row0 = span.first_draft + s, last = to < span.drafts ? to : span.drafts;
-    for (int64_t base = from;; base += 8) {
-        const int64_t i = base + (group & 7), k = span.first_draft + i;
-        const bool of_draft = group >= 8;
-        if (i <= last && (!of_draft || (c.draft && i < span.drafts))) {
+    const bool of_draft = wave >= rows;
+    const CellStats &mine = of_draft ? ws.draft : ws.target;
+    for (int64_t base = from;; base += rows) {
+        const int64_t i = base + (of_draft ? wave - rows : wave), k = span.first_draft + i, row = of_draft ? k : row0 + i;
+        if (i <= last && (!of_draft || i < span.drafts)) {
             const int32_t t = i < span.drafts ? b.tokens[k] : -1;
+            const float u = i < span.drafts ? c.accept_u[k] : 0.0f;
             const bool inside = t >= 0 && t < b.V;
-            const float x = !inside ? -INFINITY : of_draft ? logit_at<DT>(c.draft, k, c.ld, t) : logit_at<DT>(b.logits, row0 + i, b.ld, t);
-            const RowStats r = of_draft ? row_stats(ws.draft, k, cells, draft_temperature(c, k), lane16)
-                                        : row_stats(ws.target, row0 + i, cells, row_temperature(b, row0 + i), lane16);
-            if (lane16 == 0) {
-                lds.top[group] = r.top, lds.sum[group] = r.sum, lds.factor[group] = r.factor;
-                lds.weight[group] = inside && r.sum > 0.0 ? Weight(r.top, r.factor).at(x) : 0.0;
+            const float x = inside ? logit_at<DT>(of_draft ? c.draft : b.logits, row, of_draft ? c.ld : b.ld, t) : -INFINITY;
+            const float T = of_draft ? draft_temperature(c, k) : row_temperature(b, row);
+            const RowStats r = row_stats(mine, row, cells, T, lane);
+            if (lane == 0) {
+                lds.top[wave] = r.top, lds.sum[wave] = r.sum, lds.T[wave] = T;
+                lds.weight[wave] = inside && r.sum > 0.0 ? Weight(r.top, r.factor, least_of(T)).at(x) : 0.0;
+                lds.token[wave] = inside ? t : -1, lds.u[wave] = u;
             }
         }
         __syncthreads();
-        if (tid == 0) {
-            lds.go = -1;
-            for (int g = 0; g < 8 && base + g <= last && lds.go < 0; ++g) {
-                const int64_t at = base + g, kk = span.first_draft + at;
+        if (wave == 0) {
+            const int g = lane < rows ? lane : 0, d = c.draft ? rows + g : g;
+            const int64_t at = base + g;
+            const bool own = lane < rows && at <= last;
+            const int32_t t = lds.token[g];
+            const double ps = lds.sum[g], qs = lds.sum[d], p = lds.weight[g] / ps;
+            const bool scored = ps > 0.0 && (at >= span.drafts || !c.draft || qs > 0.0);
+            const double q = c.draft ? lds.weight[d] / qs : t >= 0 ? 1.0 : 0.0;
+            const bool stands = own && scored && at < span.drafts && lds.weight[g] > kNothing && (double)lds.u[g] * q < p;
+            const uint64_t stops = __ballot(own && !stands);
+            const int first = stops ? __builtin_ctzll(stops) : 64;
+            if (lane == 0) lds.go = first < 64 ? 1 : 0;
+            if (stands && lane < first && write) {
+                o.tokens[row0 + at] = t;
+                if (o.logp) o.logp[row0 + at] = (float)log(p);
+                o.flags[row0 + at] = (uint8_t)kFlagMatch;
+            }
+            if (lane == first) {
                 Stop &st = lds.stop;
                 st.place = (int32_t)at;
-                st.p_top = lds.top[g], st.p_sum = lds.sum[g], st.p_factor = lds.factor[g];
-                st.q_top = 0.0f, st.q_factor = 1.0, st.rho = 0.0;
-                if (!(lds.sum[g] > 0.0) || (at < span.drafts && c.draft && !(lds.sum[8 + g] > 0.0))) {
-                    st.kind = kNoToken;
-                    lds.go = 0;
-                } else if (at == span.drafts) {
-                    st.kind = kFromTarget;
-                    lds.go = 0;
-                } else {
-                    const int32_t t = b.tokens[kk];
-                    const bool inside = t >= 0 && t < b.V;
-                    const double q = c.draft ? lds.weight[8 + g] / lds.sum[8 + g] : inside ? 1.0 : 0.0, e = lds.weight[g];
-                    if (e > kNothing && (double)c.accept_u[kk] * q < e / lds.sum[g]) {
-                        if (write) {
-                            o.tokens[row0 + at] = t;
-                            if (o.logp) o.logp[row0 + at] = (float)log(e / lds.sum[g]);
-                            o.flags[row0 + at] = (uint8_t)kFlagMatch;
-                        }
-                    } else {
-                        st.kind = c.draft ? kFromRest : inside ? kWithoutDraft : kFromTarget;
-                        if (c.draft) st.rho = lds.sum[g] / lds.sum[8 + g], st.q_top = lds.top[8 + g], st.q_factor = lds.factor[8 + g];
-                        lds.go = inside ? 0 : 1;
+                st.p_top = lds.top[g], st.p_sum = ps, st.p_T = lds.T[g];
+                st.kind = !scored ? kNoToken : at == span.drafts ? kFromTarget : c.draft ? kFromRest : t >= 0 ? kWithoutDraft : kFromTarget;
+                const bool rest = st.kind == kFromRest;
+                st.rho = rest ? ps / qs : 0.0, st.q_top = rest ? lds.top[d] : 0.0f, st.q_T = rest ? lds.T[d] : 1.0f;
+                if (write) {
+                    o.accepted[s] = (int32_t)at;
+                    o.flags[row0 + at] = !scored ? (uint8_t)kFlagNonfinite : at < span.drafts && t < 0 ? (uint8_t)kFlagInvalidClaim : 0;
+                    if (!scored) {  // (else the drawn token is written when it is drawn)
+                        o.tokens[row0 + at] = -1;
+                        if (o.logp) o.logp[row0 + at] = NAN;
                     }
                 }
             }
         }
         __syncthreads();
-        const int go = lds.go;
-        if (go >= 0) {
+        if (lds.go) {
             stop = lds.stop;
-            if (write) {
-                if (tid == 0) o.accepted[s] = stop.place;
-                for (int64_t j = stop.place + tid; j <= span.drafts; j += kBlock) {
-                    const bool here = j == stop.place;
-                    if (!here || stop.kind == kNoToken) {  // (the drawn token is written when it is drawn)
-                        o.tokens[row0 + j] = -1;
-                        if (o.logp) o.logp[row0 + j] = here ? NAN : 0.0f;
-                    }
-                    o.flags[row0 + j] = !here ? 0 : stop.kind == kNoToken ? (uint8_t)kFlagNonfinite : go == 1 ? (uint8_t)kFlagInvalidClaim : 0;
+            if (write)
+                for (int64_t j = stop.place + 1 + tid; j <= span.drafts; j += WAVES * 64) {
+                    o.tokens[row0 + j] = -1;
+                    if (o.logp) o.logp[row0 + j] = 0.0f;
+                    o.flags[row0 + j] = 0;
                 }
-            }
             return true;
         }
-        if (base + 8 > last) {
+        if (base + rows > last) {
             reached = last + 1;
             return false;
         }
+        __syncthreads();
     }
 }
 
-// Large batches: after level `level` (LAST: after all), a workgroup a sequence.
+// Large batches: after level `level`, by two waves a sequence; LAST: after all.
 template <int DT, bool LAST>
-__global__ __launch_bounds__(kBlock) void draft_decide_kernel(DraftBatch b, DraftChain c, DraftOutputs o, Workspace ws, int level, int64_t cells)
+__global__ __launch_bounds__(128) void draft_decide_kernel(DraftBatch b, DraftChain c, DraftOutputs o, Workspace ws, int level, int64_t cells)
 {
-    __shared__ DecideLds lds;
+    __shared__ DecideLds<2> lds;
     const int64_t s = blockIdx.x;
     if (level && ws.at[s] != level) return;
     const Span span(b, s);
     Stop stop;
     int64_t reached = 0;
-    const bool stops = decide_drafts<DT>(b, c, o, ws, s, span, cells, level, LAST ? span.drafts : level, true, lds, stop, reached);
+    const bool stops = decide_drafts<DT, 2>(b, c, o, ws, s, span, cells, level, LAST ? span.drafts : level, true, lds, stop, reached);
     if (threadIdx.x == 0) {
         ws.at[s] = stops ? kDone : (int32_t)reached;
         if (stops) ws.stop[s] = stop;
@@ -403,28 +416,30 @@ __global__ __launch_bounds__(kBlock) void draft_decide_kernel(DraftBatch b, Draf
 // Sums of max(p - q, 0) over the cells of the rows where a draft fell, in units of p's weights.  DECIDE (small batches): the workgroup finds out by
 // itself where that is; `spread` workgroups share the cells of a sequence.
 template <int DT, bool DECIDE>
-__global__ __launch_bounds__(kBlock) void draft_rest_kernel(DraftBatch b, DraftChain c, DraftOutputs o, Workspace ws, int64_t cells, int spread)
+__global__ __launch_bounds__(DECIDE ? 1024 : kBlock) void draft_rest_kernel(DraftBatch b, DraftChain c, DraftOutputs o, Workspace ws, int64_t cells, int spread)
 {
     typedef typename Elem<DT>::type elem;
     constexpr int E = Elem<DT>::kPerVec;
-    __shared__ DecideLds lds;
+    constexpr int WAVES = DECIDE ? 16 : kWaves;
+    __shared__ DecideLds<16> lds;
     const int64_t s = blockIdx.x / (unsigned)spread;
     const int share = (int)(blockIdx.x - s * spread), lane = threadIdx.x & 63;
     const Span span(b, s);
     Stop stop;
     if constexpr (DECIDE) {
         int64_t unused;
-        decide_drafts<DT>(b, c, o, ws, s, span, cells, 0, span.drafts, share == 0, lds, stop, unused);
+        decide_drafts<DT, 16>(b, c, o, ws, s, span, cells, 0, span.drafts, share == 0, lds, stop, unused);
         if (share == 0 && threadIdx.x == 0) ws.stop[s] = stop;
     } else {
         stop = ws.stop[s];
     }
     if (stop.kind != kFromRest) return;
     const int64_t k = span.first_draft + stop.place, row = k + s;
-    const Weight wp(stop.p_top, stop.p_factor), wq(stop.q_top, stop.q_factor);
-    for (int64_t cell = share * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); cell < cells; cell += spread * kWaves) {
-        const Cell<DT> x(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell * kCell, b.V, lane);
-        const Cell<DT> y(reinterpret_cast<const elem *>(c.draft) + k * c.ld, cell * kCell, b.V, lane);
+    const Weight wp(stop.p_top, exponent_factor(stop.p_T), least_of(stop.p_T)), wq(stop.q_top, exponent_factor(stop.q_T), least_of(stop.q_T));
+    for (int64_t cell = share * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); cell < cells; cell += spread * WAVES) {
+        Cell<DT> x, y;
+        x.load(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell * kCell, b.V, lane);
+        y.load(reinterpret_cast<const elem *>(c.draft) + k * c.ld, cell * kCell, b.V, lane);
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < Cell<DT>::kVectors; ++i) {
@@ -440,13 +455,13 @@ __global__ __launch_bounds__(kBlock) void draft_rest_kernel(DraftBatch b, DraftC
 }
 
 // Of numbers that the threads of a workgroup have, PER each in order, none negative: the first at which their running sum, begun at `base`,
-// exceeds `level`, else the last above kNothing, else -1; the sum before it, and the sum of all.
+// exceeds `share` of `total` (negative: of their own sum), else the last above kNothing, else -1; the sum before it, and the sum of all.
 struct PickLds {
     double wave[kWaves], before;
     int first, last;
 };
 template <int PER>
-__device__ __forceinline__ int pick(const double (&v)[PER], double base, double level, PickLds &lds, double &before, double &end)
+__device__ __forceinline__ int pick(const double (&v)[PER], double base, double share, double total, PickLds &lds, double &before, double &end)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     double own = 0.0;
@@ -463,6 +478,7 @@ __device__ __forceinline__ int pick(const double (&v)[PER], double base, double 
     end = base;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) end += lds.wave[w];
+    const double level = share * (total < 0.0 ? end : total);
     double c = start + (prefix - own);
     int mine = 1 << 30, some = -1;
     double mine_before = 0.0, some_before = 0.0;
@@ -492,34 +508,34 @@ __device__ __forceinline__ int pick(const double (&v)[PER], double base, double 
 // The token whose cumulative weight is the first above u of the whole, by a workgroup.  cell_sum(c): sum of the weights of cell c; weight(v):
 // weight of entry v.  -1 where the whole is not above `nothing`.
 template <class C, class W>
-__device__ int64_t draw_token(int64_t V, int64_t cells, float u, double nothing, PickLds &lds, C &&cell_sum, W &&weight)
+__device__ __forceinline__ int64_t draw_token(int64_t V, int64_t cells, float u, double nothing, PickLds &lds, C &&cell_sum, W &&weight)
 {
     const int tid = threadIdx.x;
-    double total = 0.0, before, end;
-    double v[1] = {0.0};
-    for (int64_t c0 = 0; c0 < cells; c0 += kBlock) {
-        v[0] = c0 + tid < cells ? cell_sum(c0 + tid) : 0.0;
-        pick(v, total, INFINITY, lds, before, end);
-        total = end;
+    const double share = (double)(u > 0.0f ? u : 0.0f);
+    double total = -1.0, before, end;  // (of up to 256 cells the sum is known when they are searched)
+    if (cells > kBlock) {
+        double sum = 0.0;
+        for (int64_t c = tid; c < cells; c += kBlock) sum += cell_sum(c);
+        const double v[1] = {sum};
+        pick(v, 0.0, 1.0, 0.0, lds, before, total);
     }
-    if (!(total > nothing)) return -1;
-    const double level = (double)(u > 0.0f ? u : 0.0f) * total;
-    double base = 0.0, found_before = 0.0;
+    double base = 0.0, found_before = 0.0, level = 0.0;
     int64_t cell = -1;
     for (int64_t c0 = 0; c0 < cells; c0 += kBlock) {
-        if (cells > kBlock) v[0] = c0 + tid < cells ? cell_sum(c0 + tid) : 0.0;
-        const int at = pick(v, base, level, lds, before, end);
+        const double v[1] = {c0 + tid < cells ? cell_sum(c0 + tid) : 0.0};
+        const int at = pick(v, base, share, total, lds, before, end);
+        level = share * (total < 0.0 ? end : total);
         if (at >= 0) cell = c0 + at, found_before = before;
-        if (end > level) break;
         base = end;
+        if (end > level && at >= 0) break;
     }
-    if (cell < 0) return -1;
+    if (cell < 0 || !((total < 0.0 ? base : total) > nothing)) return -1;
     constexpr int PER = kCell / kBlock;
     const int64_t first = cell * kCell + tid * PER;
     double w[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) w[j] = first + j < V ? weight(first + j) : 0.0;
-    const int at = pick(w, 0.0, level - found_before, lds, before, end);
+    const int at = pick(w, 0.0, 1.0, level - found_before, lds, before, end);
     return at < 0 ? -1 : cell * kCell + at;
 }
 
@@ -528,46 +544,54 @@ template <int DT, bool DECIDE>
 __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftChain c, DraftOutputs o, Workspace ws, int64_t cells)
 {
     __shared__ PickLds lds;
-    __shared__ DecideLds decision;
+    __shared__ DecideLds<kWaves> decision;
     const int64_t s = blockIdx.x;
     const Span span(b, s);
     Stop stop;
     if constexpr (DECIDE) {
         int64_t unused;
-        decide_drafts<DT>(b, c, o, ws, s, span, cells, 0, span.drafts, true, decision, stop, unused);
+        decide_drafts<DT, kWaves>(b, c, o, ws, s, span, cells, 0, span.drafts, true, decision, stop, unused);
     } else {
         stop = ws.stop[s];
     }
     if (stop.kind == kNoToken) return;
     const int64_t k = span.first_draft + stop.place, row = k + s;
-    const Weight wp(stop.p_top, stop.p_factor);
+    const Weight wp(stop.p_top, exponent_factor(stop.p_T), least_of(stop.p_T)), wq(stop.q_top, exponent_factor(stop.q_T), least_of(stop.q_T));
     auto p = [&](int64_t v) { return wp.at(logit_at<DT>(b.logits, row, b.ld, v)); };
-    auto p_cell = [&](int64_t cell) {
-        const float top = ws.target.top[row * cells + cell];
-        return top > -INFINITY ? ws.target.sum[row * cells + cell] * wp.at(top) : 0.0;
-    };
-    const float u = c.sample_u[s];
-    int64_t t = -1;
-    if (stop.kind == kFromRest) {
-        const Weight wq(stop.q_top, stop.q_factor);
-        t = draw_token(b.V, cells, u, 0x1p-40 * stop.p_sum, lds, [&](int64_t cell) { return ws.rest[s * cells + cell]; },
-                       [&](int64_t v) { return __builtin_fmax(__builtin_fma(-stop.rho, wq.at(logit_at<DT>(c.draft, k, c.ld, v)), p(v)), 0.0); });
-    } else if (stop.kind == kWithoutDraft) {
-        // the cell of the drafted token is summed without it
-        const int32_t out = b.tokens[k];
-        const int64_t its = out / kCell;
+    // the cell of a draft without a distribution is summed without it
+    int64_t out = -1, its = -1;
+    double rest = 0.0;
+    if (stop.kind == kWithoutDraft) {
+        out = b.tokens[k];
+        its = out / kCell;
         constexpr int PER = kCell / kBlock;
-        double w[PER], before, rest;
+        double w[PER], before;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int64_t v = its * kCell + threadIdx.x * PER + j;
             w[j] = v < b.V && v != out ? p(v) : 0.0;
         }
-        pick(w, 0.0, INFINITY, lds, before, rest);
-        t = draw_token(b.V, cells, u, 0.0, lds, [&](int64_t cell) { return cell == its ? rest : p_cell(cell); },
-                       [&](int64_t v) { return v == out ? 0.0 : p(v); });
+        pick(w, 0.0, 1.0, 0.0, lds, before, rest);
     }
-    if (t < 0) t = draw_token(b.V, cells, u, 0.0, lds, p_cell, p);  // (also where nothing is left of p - q)
+    const float u = c.sample_u[s];
+    int64_t t = -1;
+    for (bool from_rest = stop.kind == kFromRest;; from_rest = false) {
+        t = draw_token(b.V, cells, u, from_rest ? 0x1p-40 * stop.p_sum : 0.0, lds,
+                       [&](int64_t cell) {
+                           if (from_rest) return ws.rest[s * cells + cell];
+                           if (cell == its) return rest;
+                           const float top = ws.target.top[row * cells + cell];
+                           return top > -INFINITY ? ws.target.sum[row * cells + cell] * wp.at(top) : 0.0;
+                       },
+                       [&](int64_t v) {
+                           const double e = p(v);
+                           if (from_rest) return __builtin_fmax(__builtin_fma(-stop.rho, wq.at(logit_at<DT>(c.draft, k, c.ld, v)), e), 0.0);
+                           return v == out ? 0.0 : e;
+                       });
+        // where nothing is left: p, and the drafted token with it
+        if (t >= 0 || (!from_rest && its < 0)) break;
+        its = out = -1;
+    }
     if (threadIdx.x == 0) {
         o.tokens[row] = (int32_t)t;
         if (o.logp) o.logp[row] = (float)log(p(t) / stop.p_sum);
@@ -594,12 +618,12 @@ __global__ __launch_bounds__(kBlock) void tree_walk_kernel(DraftBatch b, DraftTr
     bool drawn = true;
     for (;; ++n) {
         const int64_t row = row0 + node + 1;
-        const RowStats p = row_stats(ws.target, row, cells, row_temperature(b, row), tid & 15);  // (by each 16 lanes)
+        const RowStats p = row_stats(ws.target, row, cells, row_temperature(b, row), tid & 63);  // (by each wave)
         if (!(p.sum > 0.0)) {
             drawn = false;
             break;
         }
-        const Weight w(p.top, p.factor);
+        const Weight w(p.top, p.factor, least_of(row_temperature(b, row)));
         auto weight = [&](int64_t v) { return w.at(logit_at<DT>(b.logits, row, b.ld, v)); };
         const int64_t t = draw_token(b.V, cells, tree.sample_u[row], 0.0, lds,
                                      [&](int64_t cell) {
@@ -645,23 +669,6 @@ __global__ __launch_bounds__(kBlock) void tree_walk_kernel(DraftBatch b, DraftTr
     }
 }
 
-// Trees that have not ended after the levels that were launched: statistics of all rows that may still come.
-template <int DT>
-__global__ __launch_bounds__(kBlock) void tree_tail_stats_kernel(DraftBatch b, Workspace ws, uint32_t cells, uint32_t total)
-{
-    typedef typename Elem<DT>::type elem;
-    const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (id >= total) return;
-    const uint32_t s = id / cells, cell = id - s * cells;
-    const int32_t node = ws.at[s];
-    if (node == kDone) return;
-    const Span span(b, s);
-    for (int64_t j = node; j < span.drafts; ++j) {  // (only nodes behind this one can follow it)
-        const int64_t row = span.first_draft + s + j + 1;
-        cell_stats<DT>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell, b.V, row_temperature(b, row), ws.target, row * cells + cell, threadIdx.x & 63);
-    }
-}
-
 bool draft_shape(int64_t B, int64_t D, int64_t V)
 {
     const int64_t most = ((int64_t)1 << 26) - 64;  // cells: a wave each, and their threads are counted in 32 bits
@@ -693,42 +700,53 @@ size_t draft_workspace_bytes(int64_t B, int64_t D, int64_t V, bool draft) { retu
 static dim3 by_waves(int64_t waves) { return dim3((unsigned)((waves + kWaves - 1) / kWaves)); }
 static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 
-// Entries of a level from which on a batch is taken level by level: a level is 8 us then, and its two launches 5.
-constexpr int64_t kLevelEntries = 8 << 20;
+// Entries of a level, target's and draft's, from which on a batch is taken level by level: a level is some 20 us then, and its launches cost 8
+// more than those of all rows at once.
+constexpr int64_t kLevelEntries = 40 << 20;
 constexpr int64_t kLevels = 12;
 // Entries of all rows from which on trees are taken level by level, and levels: what goes deeper has the rows behind formed at once.
 constexpr int64_t kTreeEntries = 32 << 20;
 constexpr int kTreeLevels = 6;
+constexpr int64_t kManyCells = 16384;  // from which on waves take kMany
+
+template <int DT>
+static void run_all_stats(const DraftBatch &b, const DraftChain &c, const Workspace &ws, int64_t cells, hipStream_t stream)
+{
+    const int64_t rows = b.D + b.B + (c.draft ? b.D : 0), pairs = (cells + kMany - 1) / kMany;
+    if (rows * cells >= kManyCells)
+        all_stats_kernel<DT, kMany><<<by_waves(rows * pairs), dim3(kBlock), 0, stream>>>(b, c, ws, (uint32_t)cells, (uint32_t)pairs, (uint32_t)(rows * pairs));
+    else
+        all_stats_kernel<DT, 1><<<by_waves(rows * cells), dim3(kBlock), 0, stream>>>(b, c, ws, (uint32_t)cells, (uint32_t)cells, (uint32_t)(rows * cells));
+}
 
 template <int DT>
 static void run_chain(const DraftBatch &b, const DraftChain &c, const DraftOutputs &o, const Workspace &ws, hipStream_t stream)
 {
-    const int64_t cells = cells_of(b.V), R = b.D + b.B, both = c.draft ? 2 : 1;
+    const int64_t cells = cells_of(b.V), both = c.draft ? 2 : 1, pairs = (cells + kMany - 1) / kMany;
     const dim3 each((unsigned)b.B), block(kBlock);
     const int64_t levels = (b.D + b.B - 1) / b.B;  // rows with drafts of the longest sequence, if they are alike
     if (b.B * b.V * both >= kLevelEntries && levels > 1) {
-        const int64_t total = b.B * cells * both;
+        const int64_t total = b.B * pairs * both;
         int level = 0;
         for (; level < levels && level < kLevels; ++level) {
-            level_stats_kernel<DT, false><<<by_waves(total), block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)total);
-            draft_decide_kernel<DT, false><<<each, block, 0, stream>>>(b, c, o, ws, level, cells);
+            level_stats_kernel<DT, false><<<by_waves(total), block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
+            draft_decide_kernel<DT, false><<<each, dim3(128), 0, stream>>>(b, c, o, ws, level, cells);
         }
-        level_stats_kernel<DT, true><<<by_waves(total), block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)total);
-        draft_decide_kernel<DT, true><<<each, block, 0, stream>>>(b, c, o, ws, level, cells);
-        const int64_t spread = (cells + kWaves - 1) / kWaves;
+        level_stats_kernel<DT, true><<<by_waves(total), block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
+        draft_decide_kernel<DT, true><<<each, dim3(128), 0, stream>>>(b, c, o, ws, level, cells);
+        const int64_t spread = (pairs + kWaves - 1) / kWaves;
         if (c.draft) draft_rest_kernel<DT, false><<<dim3((unsigned)(b.B * spread)), block, 0, stream>>>(b, c, o, ws, cells, (int)spread);
         draft_draw_kernel<DT, false><<<each, block, 0, stream>>>(b, c, o, ws, cells);
         return;
     }
-    const int64_t total = (R + (c.draft ? b.D : 0)) * cells;
-    all_stats_kernel<DT><<<by_waves(total), block, 0, stream>>>(b, c, ws, (uint32_t)cells, (uint32_t)total);
+    run_all_stats<DT>(b, c, ws, cells, stream);
     if (!c.draft) {
         draft_draw_kernel<DT, true><<<each, block, 0, stream>>>(b, c, o, ws, cells);
         return;
     }
     // as many workgroups to a sequence as fill the device, a cell at least to each wave
-    const int64_t most = (cells + kWaves - 1) / kWaves, fill = (1024 + b.B - 1) / b.B, spread = most < fill ? most : fill;
-    draft_rest_kernel<DT, true><<<dim3((unsigned)(b.B * spread)), block, 0, stream>>>(b, c, o, ws, cells, (int)spread);
+    const int64_t most = (cells + 15) / 16, fill = (256 + b.B - 1) / b.B, spread = most < fill ? most : fill;
+    draft_rest_kernel<DT, true><<<dim3((unsigned)(b.B * spread)), dim3(1024), 0, stream>>>(b, c, o, ws, cells, (int)spread);
     draft_draw_kernel<DT, false><<<each, block, 0, stream>>>(b, c, o, ws, cells);
 }
 
@@ -743,22 +761,21 @@ int launch_draft_verify(const DraftBatch &b, const DraftChain &c, const DraftOut
 template <int DT>
 static void run_tree(const DraftBatch &b, const DraftTree &t, const DraftOutputs &o, const Workspace &ws, hipStream_t stream)
 {
-    const int64_t cells = cells_of(b.V), R = b.D + b.B, total = b.B * cells;
+    const int64_t cells = cells_of(b.V), pairs = (cells + kMany - 1) / kMany, total = b.B * pairs;
     const dim3 each((unsigned)b.B), block(kBlock);
     // few rows are all formed at once; of many only those on the paths, level by level
-    if (R * b.V < kTreeEntries) {
-        const DraftChain none{};
-        all_stats_kernel<DT><<<by_waves(R * cells), block, 0, stream>>>(b, none, ws, (uint32_t)cells, (uint32_t)(R * cells));
+    if ((b.D + b.B) * b.V < kTreeEntries) {
+        run_all_stats<DT>(b, DraftChain{}, ws, cells, stream);
         tree_walk_kernel<DT, false><<<each, block, 0, stream>>>(b, t, o, ws, true, cells);
         return;
     }
     const int64_t nodes = (b.D + b.B - 1) / b.B;
     const int levels = (int)(nodes < kTreeLevels ? nodes + 1 : kTreeLevels);
     for (int level = 0; level < levels; ++level) {
-        node_stats_kernel<DT><<<by_waves(total), block, 0, stream>>>(b, ws, level == 0, (uint32_t)cells, (uint32_t)total);
+        node_stats_kernel<DT, false><<<by_waves(total), block, 0, stream>>>(b, ws, level == 0, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
         tree_walk_kernel<DT, true><<<each, block, 0, stream>>>(b, t, o, ws, level == 0, cells);
     }
-    tree_tail_stats_kernel<DT><<<by_waves(total), block, 0, stream>>>(b, ws, (uint32_t)cells, (uint32_t)total);
+    node_stats_kernel<DT, true><<<by_waves(total), block, 0, stream>>>(b, ws, false, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
     tree_walk_kernel<DT, false><<<each, block, 0, stream>>>(b, t, o, ws, false, cells);
 }
 

@@ -420,19 +420,19 @@ def test_draws_near_each_border(difr):
     assert [a for a, s in zip(got, sure) if s] == [a for a, s in zip(want, sure) if s]
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_large_batches_of_chains(difr, dtype):
+@pytest.mark.parametrize("counts,drift,with_draft,dtype", [([3] * 140, 0.4, True, torch.bfloat16), ([i % 4 for i in range(150)], 0.5, True, torch.float32),
+                                                           ([1] * 130 + [17], 0.02, True, torch.bfloat16),
+                                                           ([i % 3 for i in range(270)], 0.0, False, torch.bfloat16)])
+def test_large_batches_of_chains(difr, counts, drift, with_draft, dtype):
     """Batches that are taken level by level: chains of one length, of many, longer than the levels that are launched, and without drafts' logits."""
-    V = 33000
-    for counts, drift, with_draft in (([3] * 140, 0.4, True), ([i % 4 for i in range(150)], 0.5, True), ([1] * 130 + [17], 0.02, True),
-                                      ([i % 3 for i in range(270)], 0.0, False)):
-        case = list(_chains(len(counts), counts, V, dtype, drift, spread=0.5 if with_draft else 6.0))
-        if not with_draft:
-            case[3] = case[2].float().argmax(1).int()                    # the likeliest token: such drafts stand now and then
-        case[1][5] = math.nan                                            # some sequences end early
-        case[3][4] = V + 7
-        got, _ = _check_chain(difr, tuple(case), 0.9, 0.8 if drift > 0.1 else 0.9, with_draft)
-        assert got["accepted"].max() >= min(2, max(counts))
+    V = 170000
+    case = list(_chains(len(counts), counts, V, dtype, drift, spread=0.5 if with_draft else 6.0))
+    if not with_draft:
+        case[3] = case[2].float().argmax(1).int()                        # the likeliest token: such drafts stand now and then
+    case[1][5] = math.nan                                                # some sequences end early
+    case[3][4] = V + 7
+    got, _ = _check_chain(difr, tuple(case), 0.9, 0.8 if drift > 0.1 else 0.9, with_draft)
+    assert got["accepted"].max() >= min(2, max(counts))
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
