@@ -667,8 +667,8 @@ typedef struct {
  * -1; logp [D + B] or NULL: ln p of each emitted token, 0 behind; flags [D + B]: DIFR_FLAG_MATCH on accepted tokens' rows.  A sequence that comes
  * to a row, of the target or the draft, that holds a NaN, +inf or no finite logit, or whose temperature is not positive and finite, ends
  * there: token -1, logp NaN, DIFR_FLAG_NONFINITE.  Rows that a sequence does not come to may hold anything.
- * workspace  DEVICE scratch of difr_draft_workspace_bytes(B, D, V, dtype, draft != NULL) bytes (host only), 64-byte aligned, contents
- * irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small: DIFR_ERR_SHAPE.  (D + B) ceil(V / 1024) < 2^25 - 32,
+ * workspace  DEVICE scratch of difr_draft_workspace_bytes(B, D, V, dtype, draft != NULL) bytes (host only), 128-byte aligned, contents
+ * irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small: DIFR_ERR_SHAPE.  (D + B) ceil(V / 16384) < 2^21 - 2,
  * else DIFR_ERR_SHAPE.
  */
 typedef struct {

@@ -721,7 +721,7 @@ static int check_draft_workspace(const difr::DraftBatch &b, bool draft, const vo
 {
     if (workspace_bytes < difr::draft_workspace_bytes(b.B, b.D, b.V, draft)) return DIFR_ERR_SHAPE;
     if (!workspace) return DIFR_ERR_NULL;
-    return (uintptr_t)workspace % 64u ? DIFR_ERR_ALIGN : DIFR_OK;
+    return (uintptr_t)workspace % 128u ? DIFR_ERR_ALIGN : DIFR_OK;
 }
 
 int difr_draft_verify(const difr_drafts *in, const difr_draft_chain *chain, int32_t *accepted, int32_t *tokens, float *logp, uint8_t *flags,

@@ -32,10 +32,9 @@ struct Weight {
     __device__ __forceinline__ Weight(float top, double factor, double least_) : m((double)top), c(factor), least(least_) {}
     // 2^((x - m) c): the whole part of the exponent goes into the exponent field, the rest, within 1/2 of 0, through a polynomial
     // (Chebyshev interpolation of 2^f in degree 9: relative error 1.9e-14)
-    __device__ __forceinline__ double at(float x) const
+    __device__ __forceinline__ double at(float x) const { return power(__builtin_fmax((double)x - m, least), c); }
+    static __device__ __forceinline__ double power(double d, double c)  // 2^(d c), |d c| <= 1000
     {
-        double d = (double)x - m;
-        d = __builtin_fmax(d, least);
         const double t = __builtin_fma(d, c, 0x1.8p52), n = t - 0x1.8p52, f = __builtin_fma(d, c, -n);
         double p = 0x1.b6571de2f2351p-24;
         p = __builtin_fma(p, f, 0x1.63ef969a64d3cp-20);
@@ -51,6 +50,12 @@ struct Weight {
         return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
     }
 };
+// A sum relative to reference `from`, made relative to this one: by the root of the factor, twice, which reaches 2^-2000 (sums are below 2^600).
+__device__ __forceinline__ double moved_to(double sum, float from, float to, double factor, double least)
+{
+    const double d = 0.5 * ((double)from - (double)to), r = Weight::power(__builtin_fmax(d, least), factor);
+    return sum * r * r;
+}
 constexpr double kNothing = 0x1p-900;  // a weight below this is a masked entry's
 
 // Sums and maxima over a wave (lane 63 has them; the caller's value is lane 63's, for all lanes) by moves between lanes of the vector unit.
@@ -92,10 +97,11 @@ __device__ __forceinline__ float wave_top(float v)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// Of a cell: its largest logit (NaN: it holds a NaN or +inf; -inf: no finite logit) and the sum of its weights relative to that.
-struct CellStats {
-    double *sum;
-    float *top;
+// Of a cell: the sum of its weights relative to a reference logit (its largest, or 0), which is NaN where it holds a NaN or +inf, -inf where
+// it has no finite logit.  The cells of a row are padded to whole lines, and a workgroup writes whole halves of them.
+struct __attribute__((aligned(16))) CellStats {
+    double sum;
+    float top, unused;
 };
 // Where a sequence stops.
 struct Stop {
@@ -108,7 +114,8 @@ struct Stop {
 };
 enum { kFromTarget, kFromRest, kWithoutDraft, kNoToken };
 struct Workspace {
-    CellStats target, draft;  // by row and cell
+    CellStats *target, *draft;  // by row and cell, `cells` of each row and what pads them
+    float *p_logit, *q_logit; // [D + B], [D]: the drafted token's, where rows are taken level by level
     double *rest;             // [B][cells]: sums of max(p - q, 0) where a draft fell
     Stop *stop;               // [B]
     int32_t *at;              // [B]: the row that a sequence has come to (of a tree: the node, and -1 is the root), kDone where it has stopped
@@ -117,6 +124,8 @@ struct Workspace {
 constexpr int32_t kDone = -2;
 constexpr int kMany = 2;  // cells of a wave in large batches: what a row needs is formed once for them, and more is in flight
 
+constexpr int kCellLine = 16;  // cells of a row are padded to a multiple of this
+__host__ __device__ inline int64_t padded_cells(int64_t cells) { return (cells + kCellLine - 1) / kCellLine * kCellLine; }
 static int64_t cells_of(int64_t V) { return (V + kCell - 1) / kCell; }
 
 // Entries of a cell that a lane has: vectors of 16 bytes, 64 lanes apart.
@@ -140,20 +149,27 @@ struct Cell {
     }
 };
 
-// Statistics of CELLS cells of a row from `cell` on, which are all read before the first is summed.  `id`: the first one's place.
+// Entries whose exponent (x log2(e) / T) is within 400 of 0 need no reference: their powers and sums are far from the ends of fp64.
+constexpr double kPlain = 400.0;
+
+// Statistics of 4 CELLS cells of a row from `cell0` on, CELLS of them a wave's, which are all read before the first is summed.  `out`: the row's.
+// Where all entries are plain the reference is 0, which saves the search for the largest one and three instructions an entry; a cell with masked entries,
+// infinities, NaN or large exponents is taken relative to its largest logit.
 template <int DT, int CELLS>
-__device__ __forceinline__ void cell_stats(const typename Elem<DT>::type *row, uint32_t cell, uint32_t cells, int64_t V, float T, const CellStats &out,
-                                           int64_t id, int lane)
+__device__ __forceinline__ void cell_stats(const typename Elem<DT>::type *row, uint32_t cell0, uint32_t cells, int64_t V, float T, CellStats *out,
+                                           CellStats *lds)
 {
     constexpr int E = Elem<DT>::kPerVec;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t cell = cell0 + wave * CELLS;
     Cell<DT> c[CELLS];
 #pragma unroll
     for (int k = 0; k < CELLS; ++k) c[k].load(row, (int64_t)(cell + k < cells ? cell + k : cells - 1) * kCell, V, lane);
-    const double factor = exponent_factor(T), least = least_of(T);
+    const double factor = exponent_factor(T);
+    const float plain = (float)(kPlain / factor);  // (a temperature that is none: nothing is below it, or the row is not scored)
 #pragma unroll
     for (int k = 0; k < CELLS; ++k) {
-        if (cell + k >= cells) break;
-        float top = -INFINITY;
+        float most = 0.0f;
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < Cell<DT>::kVectors; ++i) {
@@ -161,35 +177,60 @@ __device__ __forceinline__ void cell_stats(const typename Elem<DT>::type *row, u
             unpack_vector<DT>(c[k].q[i], x);
 #pragma unroll
             for (int j = 0; j < E; j += 2) {
-                top = fmaxf(top, fmaxf(x[j], x[j + 1]));
+                most = fmaxf(most, fmaxf(fabsf(x[j]), fabsf(x[j + 1])));
                 bad |= __builtin_isunordered(x[j], x[j + 1]);
             }
         }
-        top = wave_top(top);
+        float top = 0.0f;
         double sum = 0.0;
-        if (__any(bad) || top == INFINITY) {
-            top = NAN;
-        } else if (top > -INFINITY) {
-            const Weight w(top, factor, least);
+        if (!__any(bad || !(most < plain))) {
             double part[2] = {0.0, 0.0};
 #pragma unroll
             for (int i = 0; i < Cell<DT>::kVectors; ++i) {
                 float x[E];
                 unpack_vector<DT>(c[k].q[i], x);
 #pragma unroll
-                for (int j = 0; j < E; ++j) part[j & 1] += w.at(x[j]);
+                for (int j = 0; j < E; ++j) part[j & 1] += Weight::power((double)x[j], factor);
             }
             sum = wave_sum64(part[0] + part[1]);
+        } else {
+            top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < Cell<DT>::kVectors; ++i) {
+                float x[E];
+                unpack_vector<DT>(c[k].q[i], x);
+#pragma unroll
+                for (int j = 0; j < E; ++j) top = fmaxf(top, x[j]);
+            }
+            top = wave_top(top);
+            if (__any(bad) || top == INFINITY) {
+                top = NAN;
+            } else if (top > -INFINITY) {
+                const Weight w(top, factor, least_of(T));
+#pragma unroll
+                for (int i = 0; i < Cell<DT>::kVectors; ++i) {
+                    float x[E];
+                    unpack_vector<DT>(c[k].q[i], x);
+#pragma unroll 1
+                    for (int j = 0; j < E; ++j) sum += w.at(x[j]);
+                }
+                sum = wave_sum64(sum);
+            }
         }
-        if (lane == 0) {
-            out.sum[id + k] = sum;
-            out.top[id + k] = top;
-        }
+        if (lane == 0) lds[wave * CELLS + k] = CellStats{sum, top, 0.0f};
     }
+    __syncthreads();
+    if (threadIdx.x < kWaves * CELLS && cell0 + threadIdx.x < padded_cells(cells)) out[cell0 + threadIdx.x] = lds[threadIdx.x];
+    __syncthreads();
 }
 
-__device__ __forceinline__ float row_temperature(const DraftBatch &b, int64_t row) { return b.temperatures ? b.temperatures[row] : b.temperature; }
-__device__ __forceinline__ float draft_temperature(const DraftChain &c, int64_t k) { return c.temperatures ? c.temperatures[k] : c.temperature; }
+// (The value itself in a register: left to itself the compiler puts it in memory of the thread's, to choose between two addresses.)
+__device__ __forceinline__ float temperature_of(const float *Ts, float T, int64_t row)
+{
+    asm("" : "+v"(T));
+    return Ts ? Ts[row] : T;
+}
+__device__ __forceinline__ float row_temperature(const DraftBatch &b, int64_t row) { return temperature_of(b.temperatures, b.temperature, row); }
 
 // The rows of a sequence: the first, and the number of drafted tokens.  Offsets that run backwards or past D are held inside.
 struct Span {
@@ -203,29 +244,27 @@ struct Span {
     }
 };
 
-// Statistics of all cells: of the target's rows, then of the draft's.  A wave CELLS cells of a row, of which there are `groups`.
+// Statistics of all cells: of the target's rows, then of the draft's.  A workgroup 4 CELLS cells of a row, of which there are `groups` such.
 template <int DT, int CELLS>
-__global__ __launch_bounds__(kBlock) void all_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, uint32_t cells, uint32_t groups, uint32_t total)
+__global__ __launch_bounds__(kBlock) void all_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, uint32_t cells, uint32_t groups)
 {
     typedef typename Elem<DT>::type elem;
-    const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (id >= total) return;
-    const uint32_t row = id / groups, cell = (id - row * groups) * CELLS, R = (uint32_t)(b.D + b.B);
+    __shared__ CellStats lds[kWaves * CELLS];
+    const uint32_t row = blockIdx.x / groups, cell = (blockIdx.x - row * groups) * (kWaves * CELLS), R = (uint32_t)(b.D + b.B);
     const bool of_draft = row >= R;
     const int64_t at = of_draft ? row - R : row;
     const elem *const p = of_draft ? reinterpret_cast<const elem *>(c.draft) + at * c.ld : reinterpret_cast<const elem *>(b.logits) + at * b.ld;
-    cell_stats<DT, CELLS>(p, cell, cells, b.V, of_draft ? draft_temperature(c, at) : row_temperature(b, at), of_draft ? ws.draft : ws.target,
-                          at * cells + cell, threadIdx.x & 63);
+    const float T = temperature_of(of_draft ? c.temperatures : b.temperatures, of_draft ? c.temperature : b.temperature, at);
+    cell_stats<DT, CELLS>(p, cell, cells, b.V, T, (of_draft ? ws.draft : ws.target) + at * padded_cells(cells), lds);
 }
 
 // Statistics of the rows that the sequences have come to, the target's and the draft's; LAST: of all rows from there on.
 template <int DT, bool LAST>
-__global__ __launch_bounds__(kBlock) void level_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, int level, uint32_t cells, uint32_t groups, uint32_t total)
+__global__ __launch_bounds__(kBlock) void level_stats_kernel(DraftBatch b, DraftChain c, Workspace ws, int level, uint32_t cells, uint32_t groups)
 {
     typedef typename Elem<DT>::type elem;
-    const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (id >= total) return;
-    const uint32_t both = c.draft ? 2 : 1, r = id / groups, s = r / both, cell = (id - r * groups) * kMany;
+    __shared__ CellStats lds[kWaves * kMany];
+    const uint32_t both = c.draft ? 2 : 1, r = blockIdx.x / groups, s = r / both, cell = (blockIdx.x - r * groups) * (kWaves * kMany);
     const bool of_draft = r - s * both != 0;
     if (level && ws.at[s] != level) return;
     const Span span(b, s);
@@ -233,25 +272,28 @@ __global__ __launch_bounds__(kBlock) void level_stats_kernel(DraftBatch b, Draft
         if (of_draft && i >= span.drafts) break;
         const int64_t k = span.first_draft + i, at = of_draft ? k : k + s;
         const elem *const p = of_draft ? reinterpret_cast<const elem *>(c.draft) + at * c.ld : reinterpret_cast<const elem *>(b.logits) + at * b.ld;
-        cell_stats<DT, kMany>(p, cell, cells, b.V, of_draft ? draft_temperature(c, at) : row_temperature(b, at), of_draft ? ws.draft : ws.target,
-                              at * cells + cell, threadIdx.x & 63);
+        const float T = temperature_of(of_draft ? c.temperatures : b.temperatures, of_draft ? c.temperature : b.temperature, at);
+        cell_stats<DT, kMany>(p, cell, cells, b.V, T, (of_draft ? ws.draft : ws.target) + at * padded_cells(cells), lds);
+        // the drafted token's logit, while its page is at hand
+        const int32_t t = i < span.drafts ? b.tokens[k] : -1;
+        if (t >= 0 && t < b.V && (uint32_t)t / kCell - cell < kWaves * kMany && threadIdx.x == 0)
+            (of_draft ? ws.q_logit : ws.p_logit)[at] = Elem<DT>::to_float(p[t]);
     }
 }
 // The same for trees; LAST: of all rows that may still come.
 template <int DT, bool LAST>
-__global__ __launch_bounds__(kBlock) void node_stats_kernel(DraftBatch b, Workspace ws, bool first, uint32_t cells, uint32_t groups, uint32_t total)
+__global__ __launch_bounds__(kBlock) void node_stats_kernel(DraftBatch b, Workspace ws, bool first, uint32_t cells, uint32_t groups)
 {
     typedef typename Elem<DT>::type elem;
-    const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (id >= total) return;
-    const uint32_t s = id / groups, cell = (id - s * groups) * kMany;
+    __shared__ CellStats lds[kWaves * kMany];
+    const uint32_t s = blockIdx.x / groups, cell = (blockIdx.x - s * groups) * (kWaves * kMany);
     const int32_t node = first ? -1 : ws.at[s];
     if (node == kDone) return;
     const Span span(b, s);
     for (int64_t j = node; j < (LAST ? span.drafts : node + 1); ++j) {  // (only nodes behind this one can follow it)
         const int64_t row = span.first_draft + s + j + 1;
-        cell_stats<DT, kMany>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell, cells, b.V, row_temperature(b, row), ws.target,
-                              row * cells + cell, threadIdx.x & 63);
+        cell_stats<DT, kMany>(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell, cells, b.V, row_temperature(b, row),
+                              ws.target + row * padded_cells(cells), lds);
     }
 }
 
@@ -260,42 +302,40 @@ struct RowStats {
     float top;
     double sum, factor;
 };
-__device__ __forceinline__ RowStats row_stats(const CellStats &s, int64_t row, int64_t cells, float T, int lane)
+__device__ __forceinline__ RowStats row_stats(const CellStats *stats, int64_t row, int64_t cells, float T, int lane)
 {
     float top = -INFINITY;
     bool bad = !(T > 0.0f && T < INFINITY);
-    const float *tops = s.top + row * cells;
-    const double *sums = s.sum + row * cells;
+    const CellStats *const of = stats + row * padded_cells(cells);
     constexpr int kHeld = 3;  // of the first cells are loaded at once: 192 of them
-    float t[kHeld];
-    double v[kHeld];
+    CellStats held[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
         const int64_t c = lane + 64 * i;
-        t[i] = c < cells ? tops[c] : -INFINITY;
-        v[i] = c < cells ? sums[c] : 0.0;
+        held[i] = CellStats{0.0, -INFINITY, 0.0f};
+        if (c < cells) held[i] = of[c];
     }
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-        bad |= t[i] != t[i];
-        top = fmaxf(top, t[i]);
+        bad |= held[i].top != held[i].top;
+        top = fmaxf(top, held[i].top);
     }
     for (int64_t c = lane + 64 * kHeld; c < cells; c += 64) {
-        bad |= tops[c] != tops[c];
-        top = fmaxf(top, tops[c]);
+        bad |= of[c].top != of[c].top;
+        top = fmaxf(top, of[c].top);
     }
     top = wave_top(top);
     RowStats r{NAN, 0.0, 1.0};
     if (__any(bad) || top == -INFINITY) return r;
     r.top = top;
     r.factor = exponent_factor(T);
-    const Weight w(top, r.factor, least_of(T));
+    const double least = least_of(T);
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
-        if (t[i] > -INFINITY) sum += v[i] * w.at(t[i]);
+        if (held[i].top > -INFINITY) sum += moved_to(held[i].sum, held[i].top, top, r.factor, least);
     for (int64_t c = lane + 64 * kHeld; c < cells; c += 64)
-        if (tops[c] > -INFINITY) sum += sums[c] * w.at(tops[c]);
+        if (of[c].top > -INFINITY) sum += moved_to(of[c].sum, of[c].top, top, r.factor, least);
     r.sum = wave_sum64(sum);
     return r;
 }
@@ -308,7 +348,7 @@ __device__ __forceinline__ float logit_at(const void *logits, int64_t row, int64
 
 // Which drafts of a sequence stand, by a workgroup of WAVES waves: from row `from` on, whose statistics are there up to row `to` (or the last).
 // A wave has a row of the target, another the draft's of the same number; then lanes 0, 1, ... of the first wave a row each.  False where
-// rows behind `to` are needed; else `stop` says where the sequence stops.  `write`: outputs too.
+// rows behind `to` are needed; else lds.stop says where the sequence stops.  `write`: outputs too.
 template <int WAVES>
 struct DecideLds {
     float top[WAVES], T[WAVES], u[WAVES];
@@ -317,24 +357,25 @@ struct DecideLds {
     Stop stop;
     int go;
 };
-template <int DT, int WAVES>
+template <int DT, int WAVES, bool LEVELS>
 __device__ __forceinline__ bool decide_drafts(const DraftBatch &b, const DraftChain &c, const DraftOutputs &o, const Workspace &ws, int64_t s,
-                                              const Span &span, int64_t cells, int64_t from, int64_t to, bool write, DecideLds<WAVES> &lds,
-                                              Stop &stop, int64_t &reached)
+                                              const Span &span, int64_t cells, int64_t from, int64_t to, bool write, DecideLds<WAVES> &lds, int64_t &reached)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rows = c.draft ? WAVES / 2 : WAVES;  // of a round
     const int64_t row0 = span.first_draft + s, last = to < span.drafts ? to : span.drafts;
     const bool of_draft = wave >= rows;
-    const CellStats &mine = of_draft ? ws.draft : ws.target;
+    const CellStats *const mine = of_draft ? ws.draft : ws.target;
     for (int64_t base = from;; base += rows) {
         const int64_t i = base + (of_draft ? wave - rows : wave), k = span.first_draft + i, row = of_draft ? k : row0 + i;
         if (i <= last && (!of_draft || i < span.drafts)) {
             const int32_t t = i < span.drafts ? b.tokens[k] : -1;
             const float u = i < span.drafts ? c.accept_u[k] : 0.0f;
             const bool inside = t >= 0 && t < b.V;
-            const float x = inside ? logit_at<DT>(of_draft ? c.draft : b.logits, row, of_draft ? c.ld : b.ld, t) : -INFINITY;
-            const float T = of_draft ? draft_temperature(c, k) : row_temperature(b, row);
+            const float x = !inside  ? -INFINITY
+                            : LEVELS ? (of_draft ? ws.q_logit : ws.p_logit)[row]
+                                     : logit_at<DT>(of_draft ? c.draft : b.logits, row, of_draft ? c.ld : b.ld, t);
+            const float T = temperature_of(of_draft ? c.temperatures : b.temperatures, of_draft ? c.temperature : b.temperature, row);
             const RowStats r = row_stats(mine, row, cells, T, lane);
             if (lane == 0) {
                 lds.top[wave] = r.top, lds.sum[wave] = r.sum, lds.T[wave] = T;
@@ -379,9 +420,8 @@ __device__ __forceinline__ bool decide_drafts(const DraftBatch &b, const DraftCh
         }
         __syncthreads();
         if (lds.go) {
-            stop = lds.stop;
             if (write)
-                for (int64_t j = stop.place + 1 + tid; j <= span.drafts; j += WAVES * 64) {
+                for (int64_t j = lds.stop.place + 1 + tid; j <= span.drafts; j += WAVES * 64) {
                     o.tokens[row0 + j] = -1;
                     if (o.logp) o.logp[row0 + j] = 0.0f;
                     o.flags[row0 + j] = 0;
@@ -404,12 +444,11 @@ __global__ __launch_bounds__(128) void draft_decide_kernel(DraftBatch b, DraftCh
     const int64_t s = blockIdx.x;
     if (level && ws.at[s] != level) return;
     const Span span(b, s);
-    Stop stop;
     int64_t reached = 0;
-    const bool stops = decide_drafts<DT, 2>(b, c, o, ws, s, span, cells, level, LAST ? span.drafts : level, true, lds, stop, reached);
+    const bool stops = decide_drafts<DT, 2, true>(b, c, o, ws, s, span, cells, level, LAST ? span.drafts : level, true, lds, reached);
     if (threadIdx.x == 0) {
         ws.at[s] = stops ? kDone : (int32_t)reached;
-        if (stops) ws.stop[s] = stop;
+        if (stops) ws.stop[s] = lds.stop;
     }
 }
 
@@ -420,37 +459,43 @@ __global__ __launch_bounds__(DECIDE ? 1024 : kBlock) void draft_rest_kernel(Draf
 {
     typedef typename Elem<DT>::type elem;
     constexpr int E = Elem<DT>::kPerVec;
-    constexpr int WAVES = DECIDE ? 16 : kWaves;
+    constexpr int WAVES = DECIDE ? 16 : kWaves, CELLS = DECIDE ? 1 : kMany;
     __shared__ DecideLds<16> lds;
+    __shared__ double lds_sum[WAVES * CELLS];
     const int64_t s = blockIdx.x / (unsigned)spread;
     const int share = (int)(blockIdx.x - s * spread), lane = threadIdx.x & 63;
     const Span span(b, s);
-    Stop stop;
-    if constexpr (DECIDE) {
-        int64_t unused;
-        decide_drafts<DT, 16>(b, c, o, ws, s, span, cells, 0, span.drafts, share == 0, lds, stop, unused);
-        if (share == 0 && threadIdx.x == 0) ws.stop[s] = stop;
-    } else {
-        stop = ws.stop[s];
-    }
+    int64_t unused;
+    if (DECIDE) decide_drafts<DT, 16, false>(b, c, o, ws, s, span, cells, 0, span.drafts, share == 0, lds, unused);
+    if (DECIDE && share == 0 && threadIdx.x == 0) ws.stop[s] = lds.stop;
+    const Stop stop = DECIDE ? lds.stop : ws.stop[s];
     if (stop.kind != kFromRest) return;
     const int64_t k = span.first_draft + stop.place, row = k + s;
     const Weight wp(stop.p_top, exponent_factor(stop.p_T), least_of(stop.p_T)), wq(stop.q_top, exponent_factor(stop.q_T), least_of(stop.q_T));
-    for (int64_t cell = share * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); cell < cells; cell += spread * WAVES) {
-        Cell<DT> x, y;
-        x.load(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell * kCell, b.V, lane);
-        y.load(reinterpret_cast<const elem *>(c.draft) + k * c.ld, cell * kCell, b.V, lane);
-        double sum = 0.0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t cell0 = (int64_t)share * (WAVES * CELLS); cell0 < cells; cell0 += (int64_t)spread * (WAVES * CELLS)) {
+        for (int n = 0; n < CELLS; ++n) {
+            const int64_t cell = cell0 + wave * CELLS + n;
+            double sum = 0.0;
+            if (cell < cells) {
+                Cell<DT> x, y;
+                x.load(reinterpret_cast<const elem *>(b.logits) + row * b.ld, cell * kCell, b.V, lane);
+                y.load(reinterpret_cast<const elem *>(c.draft) + k * c.ld, cell * kCell, b.V, lane);
 #pragma unroll
-        for (int i = 0; i < Cell<DT>::kVectors; ++i) {
-            float xs[E], ys[E];
-            unpack_vector<DT>(x.q[i], xs);
-            unpack_vector<DT>(y.q[i], ys);
+                for (int i = 0; i < Cell<DT>::kVectors; ++i) {
+                    float xs[E], ys[E];
+                    unpack_vector<DT>(x.q[i], xs);
+                    unpack_vector<DT>(y.q[i], ys);
 #pragma unroll
-            for (int j = 0; j < E; ++j) sum += __builtin_fmax(__builtin_fma(-stop.rho, wq.at(ys[j]), wp.at(xs[j])), 0.0);
+                    for (int j = 0; j < E; ++j) sum += __builtin_fmax(__builtin_fma(-stop.rho, wq.at(ys[j]), wp.at(xs[j])), 0.0);
+                }
+                sum = wave_sum64(sum);
+            }
+            if (lane == 0) lds_sum[wave * CELLS + n] = sum;
         }
-        sum = wave_sum64(sum);
-        if (lane == 0) ws.rest[s * cells + cell] = sum;
+        __syncthreads();
+        if (threadIdx.x < WAVES * CELLS && cell0 + threadIdx.x < padded_cells(cells)) ws.rest[s * padded_cells(cells) + cell0 + threadIdx.x] = lds_sum[threadIdx.x];
+        __syncthreads();
     }
 }
 
@@ -547,13 +592,9 @@ __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftC
     __shared__ DecideLds<kWaves> decision;
     const int64_t s = blockIdx.x;
     const Span span(b, s);
-    Stop stop;
-    if constexpr (DECIDE) {
-        int64_t unused;
-        decide_drafts<DT, kWaves>(b, c, o, ws, s, span, cells, 0, span.drafts, true, decision, stop, unused);
-    } else {
-        stop = ws.stop[s];
-    }
+    int64_t unused;
+    if (DECIDE) decide_drafts<DT, kWaves, false>(b, c, o, ws, s, span, cells, 0, span.drafts, true, decision, unused);
+    const Stop stop = DECIDE ? decision.stop : ws.stop[s];
     if (stop.kind == kNoToken) return;
     const int64_t k = span.first_draft + stop.place, row = k + s;
     const Weight wp(stop.p_top, exponent_factor(stop.p_T), least_of(stop.p_T)), wq(stop.q_top, exponent_factor(stop.q_T), least_of(stop.q_T));
@@ -578,10 +619,10 @@ __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftC
     for (bool from_rest = stop.kind == kFromRest;; from_rest = false) {
         t = draw_token(b.V, cells, u, from_rest ? 0x1p-40 * stop.p_sum : 0.0, lds,
                        [&](int64_t cell) {
-                           if (from_rest) return ws.rest[s * cells + cell];
+                           if (from_rest) return ws.rest[s * padded_cells(cells) + cell];
                            if (cell == its) return rest;
-                           const float top = ws.target.top[row * cells + cell];
-                           return top > -INFINITY ? ws.target.sum[row * cells + cell] * wp.at(top) : 0.0;
+                           const CellStats of = ws.target[row * padded_cells(cells) + cell];
+                           return of.top > -INFINITY ? moved_to(of.sum, of.top, stop.p_top, wp.c, wp.least) : 0.0;
                        },
                        [&](int64_t v) {
                            const double e = p(v);
@@ -627,8 +668,8 @@ __global__ __launch_bounds__(kBlock) void tree_walk_kernel(DraftBatch b, DraftTr
         auto weight = [&](int64_t v) { return w.at(logit_at<DT>(b.logits, row, b.ld, v)); };
         const int64_t t = draw_token(b.V, cells, tree.sample_u[row], 0.0, lds,
                                      [&](int64_t cell) {
-                                         const float top = ws.target.top[row * cells + cell];
-                                         return top > -INFINITY ? ws.target.sum[row * cells + cell] * w.at(top) : 0.0;
+                                         const CellStats of = ws.target[row * padded_cells(cells) + cell];
+                                         return of.top > -INFINITY ? moved_to(of.sum, of.top, p.top, w.c, w.least) : 0.0;
                                      },
                                      weight);
         // the first child that holds it
@@ -672,21 +713,23 @@ __global__ __launch_bounds__(kBlock) void tree_walk_kernel(DraftBatch b, DraftTr
 bool draft_shape(int64_t B, int64_t D, int64_t V)
 {
     const int64_t most = ((int64_t)1 << 26) - 64;  // cells: a wave each, and their threads are counted in 32 bits
-    return 2 * (D + B) <= most / cells_of(V > 0 ? V : 1);
+    return 2 * (D + B) <= most / padded_cells(cells_of(V > 0 ? V : 1));
 }
 
 static size_t carve(Workspace *w, void *base, int64_t B, int64_t D, int64_t V, bool draft)
 {
-    const int64_t cells = cells_of(V), R = D + B;
+    const int64_t cells = padded_cells(cells_of(V)), R = D + B;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         void *p = base ? (char *)base + at : nullptr;
-        at += (bytes + 63) / 64 * 64;
+        at += (bytes + 127) / 128 * 128;
         return p;
     };
     Workspace ws{};
-    ws.target = CellStats{(double *)take(R * cells * 8), (float *)take(R * cells * 4)};
-    if (draft) ws.draft = CellStats{(double *)take(D * cells * 8), (float *)take(D * cells * 4)};
+    ws.target = (CellStats *)take(R * cells * sizeof(CellStats));
+    if (draft) ws.draft = (CellStats *)take(D * cells * sizeof(CellStats));
+    ws.p_logit = (float *)take(R * 4);
+    if (draft) ws.q_logit = (float *)take(D * 4);
     if (draft) ws.rest = (double *)take(B * cells * 8);
     ws.stop = (Stop *)take(B * sizeof(Stop));
     ws.at = (int32_t *)take(B * 4);
@@ -697,7 +740,6 @@ static size_t carve(Workspace *w, void *base, int64_t B, int64_t D, int64_t V, b
 
 size_t draft_workspace_bytes(int64_t B, int64_t D, int64_t V, bool draft) { return carve(nullptr, nullptr, B, D, V, draft); }
 
-static dim3 by_waves(int64_t waves) { return dim3((unsigned)((waves + kWaves - 1) / kWaves)); }
 static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 
 // Entries of a level, target's and draft's, from which on a batch is taken level by level: a level is some 20 us then, and its launches cost 8
@@ -712,30 +754,29 @@ constexpr int64_t kManyCells = 16384;  // from which on waves take kMany
 template <int DT>
 static void run_all_stats(const DraftBatch &b, const DraftChain &c, const Workspace &ws, int64_t cells, hipStream_t stream)
 {
-    const int64_t rows = b.D + b.B + (c.draft ? b.D : 0), pairs = (cells + kMany - 1) / kMany;
+    const int64_t rows = b.D + b.B + (c.draft ? b.D : 0), many = (cells + kWaves * kMany - 1) / (kWaves * kMany), one = (cells + kWaves - 1) / kWaves;
     if (rows * cells >= kManyCells)
-        all_stats_kernel<DT, kMany><<<by_waves(rows * pairs), dim3(kBlock), 0, stream>>>(b, c, ws, (uint32_t)cells, (uint32_t)pairs, (uint32_t)(rows * pairs));
+        all_stats_kernel<DT, kMany><<<dim3((unsigned)(rows * many)), dim3(kBlock), 0, stream>>>(b, c, ws, (uint32_t)cells, (uint32_t)many);
     else
-        all_stats_kernel<DT, 1><<<by_waves(rows * cells), dim3(kBlock), 0, stream>>>(b, c, ws, (uint32_t)cells, (uint32_t)cells, (uint32_t)(rows * cells));
+        all_stats_kernel<DT, 1><<<dim3((unsigned)(rows * one)), dim3(kBlock), 0, stream>>>(b, c, ws, (uint32_t)cells, (uint32_t)one);
 }
 
 template <int DT>
 static void run_chain(const DraftBatch &b, const DraftChain &c, const DraftOutputs &o, const Workspace &ws, hipStream_t stream)
 {
-    const int64_t cells = cells_of(b.V), both = c.draft ? 2 : 1, pairs = (cells + kMany - 1) / kMany;
+    const int64_t cells = cells_of(b.V), both = c.draft ? 2 : 1, groups = (cells + kWaves * kMany - 1) / (kWaves * kMany);
     const dim3 each((unsigned)b.B), block(kBlock);
     const int64_t levels = (b.D + b.B - 1) / b.B;  // rows with drafts of the longest sequence, if they are alike
     if (b.B * b.V * both >= kLevelEntries && levels > 1) {
-        const int64_t total = b.B * pairs * both;
+        const dim3 rows((unsigned)(b.B * both * groups));
         int level = 0;
         for (; level < levels && level < kLevels; ++level) {
-            level_stats_kernel<DT, false><<<by_waves(total), block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
+            level_stats_kernel<DT, false><<<rows, block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)groups);
             draft_decide_kernel<DT, false><<<each, dim3(128), 0, stream>>>(b, c, o, ws, level, cells);
         }
-        level_stats_kernel<DT, true><<<by_waves(total), block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
+        level_stats_kernel<DT, true><<<rows, block, 0, stream>>>(b, c, ws, level, (uint32_t)cells, (uint32_t)groups);
         draft_decide_kernel<DT, true><<<each, dim3(128), 0, stream>>>(b, c, o, ws, level, cells);
-        const int64_t spread = (pairs + kWaves - 1) / kWaves;
-        if (c.draft) draft_rest_kernel<DT, false><<<dim3((unsigned)(b.B * spread)), block, 0, stream>>>(b, c, o, ws, cells, (int)spread);
+        if (c.draft) draft_rest_kernel<DT, false><<<dim3((unsigned)(b.B * groups)), block, 0, stream>>>(b, c, o, ws, cells, (int)groups);
         draft_draw_kernel<DT, false><<<each, block, 0, stream>>>(b, c, o, ws, cells);
         return;
     }
@@ -761,7 +802,8 @@ int launch_draft_verify(const DraftBatch &b, const DraftChain &c, const DraftOut
 template <int DT>
 static void run_tree(const DraftBatch &b, const DraftTree &t, const DraftOutputs &o, const Workspace &ws, hipStream_t stream)
 {
-    const int64_t cells = cells_of(b.V), pairs = (cells + kMany - 1) / kMany, total = b.B * pairs;
+    const int64_t cells = cells_of(b.V), groups = (cells + kWaves * kMany - 1) / (kWaves * kMany);
+    const dim3 rows((unsigned)(b.B * groups));
     const dim3 each((unsigned)b.B), block(kBlock);
     // few rows are all formed at once; of many only those on the paths, level by level
     if ((b.D + b.B) * b.V < kTreeEntries) {
@@ -772,10 +814,10 @@ static void run_tree(const DraftBatch &b, const DraftTree &t, const DraftOutputs
     const int64_t nodes = (b.D + b.B - 1) / b.B;
     const int levels = (int)(nodes < kTreeLevels ? nodes + 1 : kTreeLevels);
     for (int level = 0; level < levels; ++level) {
-        node_stats_kernel<DT, false><<<by_waves(total), block, 0, stream>>>(b, ws, level == 0, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
+        node_stats_kernel<DT, false><<<rows, block, 0, stream>>>(b, ws, level == 0, (uint32_t)cells, (uint32_t)groups);
         tree_walk_kernel<DT, true><<<each, block, 0, stream>>>(b, t, o, ws, level == 0, cells);
     }
-    node_stats_kernel<DT, true><<<by_waves(total), block, 0, stream>>>(b, ws, false, (uint32_t)cells, (uint32_t)pairs, (uint32_t)total);
+    node_stats_kernel<DT, true><<<rows, block, 0, stream>>>(b, ws, false, (uint32_t)cells, (uint32_t)groups);
     tree_walk_kernel<DT, false><<<each, block, 0, stream>>>(b, t, o, ws, false, cells);
 }
 
