@@ -615,7 +615,7 @@ int difr_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t N,
  * infinity or a difference beyond fp32 has the scale NaN and stands for NaN throughout.
  */
 int64_t difr_int4_padded(int64_t d);
-/* x [N, ld] bf16 or fp32, base aligned to the element size -> codes, scales, and zeros (NULL: a matrix without).  d >= 1. */
+/* x [N, ld] bf16 or fp32, base aligned to the element size -> codes, scales, and zeros (NULL: a matrix without).  1 <= d < 2^23. */
 int difr_int4_quantize(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, int32_t group, uint8_t *codes, void *scales,
                        uint8_t *zeros, void *hip_stream);
 /* The first d elements of every row, [N, ld] bf16 (rounded once) or fp32 (exact). */
@@ -624,8 +624,8 @@ int difr_int4_dequantize(const uint8_t *codes, const void *scales, const uint8_t
 /*
  * out[n][v] = sum_k hidden[n][k] w[v][k], k < d: the logits of N hidden states (bf16 or fp32, [N, ldh]) under a head of V rows.  Products
  * of elements and codes are exact, accumulation and scaling are fp32, and the sum is rounded once to bf16 or fp32 ([N, ld], ld >= V).
- * Meant for the few rows that are decoded together: the head is read once for every 64 of them (fp32: every 21).  Rows that hold a NaN, an infinity or
- * magnitudes above 2^120 get NaN or infinities.  A row's result does not depend on the rows beside it.  V < 2^31, K < 2^24, bases aligned to the element size.
+ * Meant for the few rows that are decoded together: the head is read once for every 64 of them (fp32 states: every 32; heads of fewer than 16,369 rows: every 16).  Rows that hold a NaN, an infinity or
+ * magnitudes above 2^120 get NaN or infinities.  A row's result does not depend on the rows beside it.  V < 2^31, bases aligned to the element size; out overlaps nothing.
  * workspace  DEVICE scratch of at least difr_int4_product_workspace_bytes(N, d, hidden_dtype, group) bytes (host only; 0: none is needed and
  * NULL will do), 16-byte aligned, contents irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small:
  * DIFR_ERR_SHAPE.

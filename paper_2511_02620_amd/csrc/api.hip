@@ -636,7 +636,7 @@ static int element_size(int32_t dtype) { return dtype == DIFR_BF16 ? 2 : 4; }
 static int validate_int4(const void *x, int32_t dtype, int64_t N, int64_t d, int64_t ld, int32_t group, const uint8_t *codes,
                          const void *scales, const uint8_t *zeros, difr::Int4Matrix *m)
 {
-    if (N < 0 || d < 1 || ld < d || N >= (int64_t)1 << 31 || d >= (int64_t)1 << 24) return DIFR_ERR_SHAPE;
+    if (N < 0 || d < 1 || ld < d || N >= (int64_t)1 << 31 || d >= (int64_t)1 << 23) return DIFR_ERR_SHAPE;
     if (!int4_group(group)) return DIFR_ERR_ARGUMENT;
     if (dtype != DIFR_BF16 && dtype != DIFR_F32) return DIFR_ERR_DTYPE;
     if (N == 0) return DIFR_OK;
@@ -669,7 +669,7 @@ int difr_int4_dequantize(const uint8_t *codes, const void *scales, const uint8_t
 
 size_t difr_int4_product_workspace_bytes(int64_t N, int64_t d, int32_t hidden_dtype, int32_t group)
 {
-    if (N < 1 || N >= (int64_t)1 << 31 || d < 1 || d >= (int64_t)1 << 24 || !int4_group(group) || (hidden_dtype != DIFR_BF16 && hidden_dtype != DIFR_F32))
+    if (N < 1 || N >= (int64_t)1 << 31 || d < 1 || d >= (int64_t)1 << 23 || !int4_group(group) || (hidden_dtype != DIFR_BF16 && hidden_dtype != DIFR_F32))
         return 0;
     return difr::int4_product_workspace_bytes(N, d, hidden_dtype, group);
 }

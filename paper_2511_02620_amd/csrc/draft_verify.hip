@@ -166,7 +166,7 @@ __device__ __forceinline__ void cell_stats(const typename Elem<DT>::type *row, u
 #pragma unroll
     for (int k = 0; k < CELLS; ++k) c[k].load(row, (int64_t)(cell + k < cells ? cell + k : cells - 1) * kCell, V, lane);
     const double factor = exponent_factor(T);
-    const float plain = (float)(kPlain / factor);  // (a temperature that is none: nothing is below it, or the row is not scored)
+    const float plain = (float)(least_of(T) * (-kPlain / 1000.0));  // (a temperature that is none: the row is not scored)
 #pragma unroll
     for (int k = 0; k < CELLS; ++k) {
         float most = 0.0f;

@@ -143,6 +143,22 @@ def test_rows_do_not_touch_each_other(difr):
     assert torch.equal(got[~bad], whole[~bad]) and not got[bad].isfinite().any()
 
 
+@pytest.mark.parametrize("V,d,group", [(17000, 640, 64), (20011, 2100, 128), (16500, 300, 32)])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_a_row_alone_and_among_others(difr, V, d, group, hidden):
+    """Large heads: the same bits however many rows there are, from whatever stream and into whatever tensor."""
+    codes, scales, zeros, _ = _matrix(difr, V, d, group, True, 7)
+    h = torch.randn(100, d, generator=torch.Generator().manual_seed(2)).to(hidden).to(DEV)
+    whole = difr.int4_product(h, codes, scales, zeros, dtype=torch.float32)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    for n in (1, 5, 16, 17, 33, 49, 65):
+        with torch.cuda.stream(stream):
+            got = difr.int4_product(h[100 - n:], codes, scales, zeros, dtype=torch.float32)
+        torch.cuda.synchronize()
+        assert torch.equal(got, whole[100 - n:]), n
+
+
 def test_empty(difr):
     codes, scales, zeros, w = _matrix(difr, 5, 128, 128, False, 1)
     assert difr.int4_product(torch.zeros(0, 128, dtype=torch.bfloat16, device=DEV), codes, scales).shape == (0, 5)
