@@ -194,7 +194,10 @@ __global__ __launch_bounds__(kBlock) void int4_image_kernel(const typename Elem<
 
 // Hidden states in P parts; NT tiles of 16 of them from the image, a step ahead (RESIDENT: up to 16, converted by each workgroup and kept in
 // LDS); KS slabs at once, each with its share of the waves (small heads, whose blocks are fewer than waves); RB blocks of 16 rows of
-// the head to a wave at a time; D steps of codes in flight, in registers.
+// the head to a wave at a time; D steps of codes in flight, in registers.  What bounds it, and steps of its making, us: one bf16 row by
+// 151,936 x 4096, 58 to 60 (5.4 TB/s; SIMDs issue in 81 % of the cycles): a lane fetching a row of its own 81, whole lines dealt by LDS 67,
+// 16 waves instead of 8 64.  40 rows by 128,256 x 4096, 103: fragments of the states are read from LDS for every two blocks; RB = 1 with 16
+// waves 112 (spills), 4 and 3 blocks spill too.  17 rows by 50,257 x 2000, 25: RB = 1 with 16 waves, against 29 with RB = 2 and 8.
 template <int HT, bool RESIDENT, int NT, int KS, int G, bool ZEROS, int RB, int D, int W, bool PAST>
 __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
 {
@@ -548,7 +551,8 @@ static void run_product(Int4Product a, hipStream_t stream)
             int4_product_kernel<HT, RESIDENT, NT, KS, group, decltype(ZEROS)::value, RB, D, W, decltype(PAST)::value>
                 <<<dim3((unsigned)grid, tiles), dim3(W * 64), 0, stream>>>(a);
         };
-        // a matrix larger than the 256 MB Infinity Cache is read past it
+        // a matrix larger than the 256 MB Infinity Cache is read past it (with D = 4 for 3, 151,936 x 4096 64 -> 58 us; 50,257 x 2000, which fits,
+        // lost: 29 -> 32)
         if (KS == 1 && a.m.V * a.m.K / 2 > (int64_t)256 << 20)
             a.m.zeros ? go(std::true_type(), std::bool_constant<KS == 1>()) : go(std::false_type(), std::bool_constant<KS == 1>());
         else
