@@ -742,9 +742,9 @@ size_t draft_workspace_bytes(int64_t B, int64_t D, int64_t V, bool draft) { retu
 
 static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 
-// Entries of a level, target's and draft's, from which on a batch is taken level by level: a level is some 30 us then, its second launch 5.
-// A row of 151,936 bf16 is 0.118 us: 256 sequences of 7 drafts would be some 450 us of statistics all at once, 239 level by level (where
-// they stop as they do among random logits), with decisions 277.  Where exactly the two meet was not measured.
+// Entries of a level, target's and draft's, from which on a batch is taken level by level.  All rows at once / level by level, us a call:
+// 48, 96, 128, 160, 256 sequences of 5 drafts, 128,256 bf16 (12, 24, 31, 39, 63 << 20 entries a level): 86 / 117, 142 / 154, 167 / 171,
+// 222 / 199, 314 / 267; 128 and 256 of 7, 151,936 (37, 74 << 20): 232 / 219, 449 / 329; 128 of 3 (37 << 20): 127 / 137.
 constexpr int64_t kLevelEntries = 40 << 20;
 constexpr int64_t kLevels = 12;
 // Entries of all rows from which on trees are taken level by level, and levels: what goes deeper has the rows behind formed at once.
