@@ -748,7 +748,9 @@ static int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 constexpr int64_t kLevelEntries = 40 << 20;
 constexpr int64_t kLevels = 12;
 // Entries of all rows from which on trees are taken level by level, and levels: what goes deeper has the rows behind formed at once.
-constexpr int64_t kTreeEntries = 32 << 20;
+// All rows at once / level by level, us a call, bf16: 64 trees of widths 2, 1, 128,251 (39 << 20 entries) 50 / 64; 8 of widths 4, 2, 2, 1,
+// 151,936 (52 << 20) 65 / 74; 8, 16, 64 of widths 4, 3, 2, 1, 128,251 (64, 127, 509 << 20) 77 / 74, 125 / 75, 421 / 90.
+constexpr int64_t kTreeEntries = 60 << 20;
 constexpr int kTreeLevels = 6;
 constexpr int64_t kManyCells = 16384;  // from which on waves take kMany
 

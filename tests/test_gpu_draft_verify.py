@@ -435,9 +435,10 @@ def test_large_batches_of_chains(difr, counts, drift, with_draft, dtype):
     assert got["accepted"].max() >= min(2, max(counts))
 
 
+@pytest.mark.parametrize("V", [40000, 70000])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_large_batches_of_trees(difr, dtype):
-    V = 40000
+def test_large_batches_of_trees(difr, dtype, V):
+    """All rows at once, and level by level."""
     case = _trees(17, [12, 0, 14, 13] * 22, V, dtype, hit=0.9)
     T = torch.rand(88 + 39 * 22, generator=torch.Generator().manual_seed(3)) + 0.5
     case[2][3] = math.nan
