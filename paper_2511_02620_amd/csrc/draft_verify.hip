@@ -500,13 +500,13 @@ __global__ __launch_bounds__(DECIDE ? 1024 : kBlock) void draft_rest_kernel(Draf
 }
 
 // Of numbers that the threads of a workgroup have, PER each in order, none negative: the first at which their running sum, begun at `base`,
-// exceeds `share` of `total` (negative: of their own sum), else the last above kNothing, else -1; the sum before it, and the sum of all.
+// exceeds level(end), else the last above kNothing, else -1; the sum before it, and `end`, the sum of all.
 struct PickLds {
     double wave[kWaves], before;
     int first, last;
 };
-template <int PER>
-__device__ __forceinline__ int pick(const double (&v)[PER], double base, double share, double total, PickLds &lds, double &before, double &end)
+template <int PER, class L>
+__device__ __forceinline__ int pick(const double (&v)[PER], double base, L &&level_of, PickLds &lds, double &before, double &end)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     double own = 0.0;
@@ -523,7 +523,7 @@ __device__ __forceinline__ int pick(const double (&v)[PER], double base, double 
     end = base;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) end += lds.wave[w];
-    const double level = share * (total < 0.0 ? end : total);
+    const double level = level_of(end);
     double c = start + (prefix - own);
     int mine = 1 << 30, some = -1;
     double mine_before = 0.0, some_before = 0.0;
@@ -557,30 +557,34 @@ __device__ __forceinline__ int64_t draw_token(int64_t V, int64_t cells, float u,
 {
     const int tid = threadIdx.x;
     const double share = (double)(u > 0.0f ? u : 0.0f);
-    double total = -1.0, before, end;  // (of up to 256 cells the sum is known when they are searched)
-    if (cells > kBlock) {
+    const bool at_once = cells <= kBlock;  // (their sum is known when they are searched)
+    double total = 0.0, before, end;
+    if (!at_once) {
         double sum = 0.0;
         for (int64_t c = tid; c < cells; c += kBlock) sum += cell_sum(c);
         const double v[1] = {sum};
-        pick(v, 0.0, 1.0, 0.0, lds, before, total);
+        pick(v, 0.0, [](double) { return 0.0; }, lds, before, total);
     }
     double base = 0.0, found_before = 0.0, level = 0.0;
     int64_t cell = -1;
     for (int64_t c0 = 0; c0 < cells; c0 += kBlock) {
         const double v[1] = {c0 + tid < cells ? cell_sum(c0 + tid) : 0.0};
-        const int at = pick(v, base, share, total, lds, before, end);
-        level = share * (total < 0.0 ? end : total);
+        const int at = pick(v, base, [&](double sum) { return share * (at_once ? sum : total); }, lds, before, end);
+        if (at_once) total = end;
+        level = share * total;
         if (at >= 0) cell = c0 + at, found_before = before;
         base = end;
         if (end > level && at >= 0) break;
     }
-    if (cell < 0 || !((total < 0.0 ? base : total) > nothing)) return -1;
+    if (cell < 0 || !(total > nothing)) return -1;
     constexpr int PER = kCell / kBlock;
     const int64_t first = cell * kCell + tid * PER;
     double w[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) w[j] = first + j < V ? weight(first + j) : 0.0;
-    const int at = pick(w, 0.0, 1.0, level - found_before, lds, before, end);
+    // (found_before is rounded and may lie above the level by that: then the first entry it is)
+    const double rest = __builtin_fmax(level - found_before, 0.0);
+    const int at = pick(w, 0.0, [&](double) { return rest; }, lds, before, end);
     return at < 0 ? -1 : cell * kCell + at;
 }
 
@@ -612,7 +616,7 @@ __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftC
             const int64_t v = its * kCell + threadIdx.x * PER + j;
             w[j] = v < b.V && v != out ? p(v) : 0.0;
         }
-        pick(w, 0.0, 1.0, 0.0, lds, before, rest);
+        pick(w, 0.0, [](double) { return 0.0; }, lds, before, rest);
     }
     const float u = c.sample_u[s];
     int64_t t = -1;

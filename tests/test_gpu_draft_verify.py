@@ -449,3 +449,34 @@ def test_large_batches_of_trees(difr, dtype, V):
     case = (case[0], None) + case[2:]
     _hit(case, torch.ones(990), 1)
     assert _check_tree(difr, case, 1.0)["accepted"].tolist() == [10] * 90
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("value", [0.0625, 1.2890625, -3.0, 40.0])
+def test_constant_rows_with_u_on_the_borders_of_cells(difr, dtype, value):
+    """n tokens of one weight and u = k / 32: the definition is token k n / 32; a sum that is off in its last bit may stop at the one before,
+    but nowhere else."""
+    n, borders = 32 * 1024, torch.arange(32)
+    u = (borders / 32).to(torch.float32).to(DEV)
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    x = torch.full((32, n), value, dtype=dtype, device=DEV)
+    off = torch.zeros(33, dtype=torch.int64, device=DEV)
+    fits = [{k * 1024, max(k * 1024 - 1, 0)} for k in range(32)]
+
+    def check(tokens):
+        assert all(t in f for t, f in zip(tokens.tolist(), fits)), tokens.tolist()
+
+    check(difr.tree_verify(x, 1.0, none, None, off, u)["tokens"])
+    check(difr.draft_verify(x, 1.0, none, off, u[:0], u)["tokens"])
+    # the rest of max(p - q, 0): the draft has only the tokens of a cell behind, one of which it proposes and which fall
+    x = torch.full((64, n + 1024), value, dtype=dtype, device=DEV)
+    y = torch.full((32, n + 1024), -math.inf, dtype=dtype, device=DEV)
+    y[:, n:] = 1.0
+    one = torch.arange(33, device=DEV)
+    got = difr.draft_verify(x, 1.0, torch.full((32,), n + 5, dtype=torch.int32, device=DEV), one, torch.full((32,), 0.999, device=DEV), u, draft=y)
+    assert got["accepted"].eq(0).all()
+    check(got["tokens"][::2])
+    # a draft without a distribution, in the last place
+    got = difr.draft_verify(x[:, :n + 1], 1.0, torch.full((32,), n, dtype=torch.int32, device=DEV), one, torch.full((32,), 0.999, device=DEV), u)
+    assert got["accepted"].eq(0).all()
+    check(got["tokens"][::2])
