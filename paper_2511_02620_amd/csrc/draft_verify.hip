@@ -33,6 +33,7 @@ struct Weight {
     // 2^((x - m) c): the whole part of the exponent goes into the exponent field, the rest, within 1/2 of 0, through a polynomial
     // (Chebyshev interpolation of 2^f in degree 9: relative error 1.9e-14)
     __device__ __forceinline__ double at(float x) const { return power(__builtin_fmax((double)x - m, least), c); }
+    __device__ __forceinline__ double drawable(float x) const;  // 0 for a masked entry
     static __device__ __forceinline__ double power(double d, double c)  // 2^(d c), |d c| <= 1000
     {
         const double t = __builtin_fma(d, c, 0x1.8p52), n = t - 0x1.8p52, f = __builtin_fma(d, c, -n);
@@ -56,7 +57,18 @@ __device__ __forceinline__ double moved_to(double sum, float from, float to, dou
     const double d = 0.5 * ((double)from - (double)to), r = Weight::power(__builtin_fmax(d, least), factor);
     return sum * r * r;
 }
-constexpr double kNothing = 0x1p-900;  // a weight below this is a masked entry's
+constexpr double kNothing = 0x1p-998;  // a weight up to this is a masked entry's, which is 2^-1000
+
+__device__ __forceinline__ double Weight::drawable(float x) const
+{
+    const double w = at(x);
+    return w > kNothing ? w : 0.0;
+}
+// ln of the probability of logit x, of a row whose weights have this sum.
+__device__ __forceinline__ double log_probability(float x, const Weight &of, double sum)
+{
+    return ((double)x - of.m) * of.c * 0.693147180559945309417 - log(sum);
+}
 
 // Sums and maxima over a wave (lane 63 has them; the caller's value is lane 63's, for all lanes) by moves between lanes of the vector unit.
 template <int CTRL, int ROWS>
@@ -499,14 +511,20 @@ __global__ __launch_bounds__(DECIDE ? 1024 : kBlock) void draft_rest_kernel(Draf
     }
 }
 
-// Of numbers that the threads of a workgroup have, PER each in order, none negative: the first at which their running sum, begun at `base`,
-// exceeds level(end), else the last above kNothing, else -1; the sum before it, and `end`, the sum of all.
+// Of numbers that the threads of a workgroup have, PER each in order, none negative: the first above 0 at which their running sum, begun at
+// `base`, exceeds level(end), else the last above 0, else -1; `end` is the sum of all.  Of the number: the sum before it, it, its thread's tag.
+struct Picked {
+    int at;
+    double before, value, end;
+    float tag;
+};
 struct PickLds {
-    double wave[kWaves], before;
+    double wave[kWaves];
+    Picked found;
     int first, last;
 };
 template <int PER, class L>
-__device__ __forceinline__ int pick(const double (&v)[PER], double base, L &&level_of, PickLds &lds, double &before, double &end)
+__device__ __forceinline__ Picked pick(const double (&v)[PER], float tag, double base, L &&level_of, PickLds &lds)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     double own = 0.0;
@@ -520,21 +538,21 @@ __device__ __forceinline__ int pick(const double (&v)[PER], double base, L &&lev
     double start = base;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) start += w < wave ? lds.wave[w] : 0.0;
-    end = base;
+    double end = base;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) end += lds.wave[w];
     const double level = level_of(end);
     double c = start + (prefix - own);
     int mine = 1 << 30, some = -1;
-    double mine_before = 0.0, some_before = 0.0;
+    double mine_before = 0.0, some_before = 0.0, mine_value = 0.0, some_value = 0.0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        if (v[j] > kNothing) {
+        if (v[j] > 0.0) {
             some = tid * PER + j;
-            some_before = c;
+            some_before = c, some_value = v[j];
             if (c + v[j] > level && mine == 1 << 30) {
                 mine = some;
-                mine_before = c;
+                mine_before = c, mine_value = v[j];
             }
         }
         c += v[j];
@@ -544,48 +562,55 @@ __device__ __forceinline__ int pick(const double (&v)[PER], double base, L &&lev
     if (any && lane == 63 - __builtin_clzll(any)) atomicMax(&lds.last, some);
     __syncthreads();
     const int at = lds.first < 1 << 30 ? lds.first : lds.last;
-    if (at >= 0 && at / PER == tid) lds.before = mine == at ? mine_before : some_before;
+    if (at >= 0 && at / PER == tid) {
+        const bool crosses = mine == at;
+        lds.found.before = crosses ? mine_before : some_before, lds.found.value = crosses ? mine_value : some_value, lds.found.tag = tag;
+    }
     __syncthreads();
-    before = lds.before;
-    return at;
+    return Picked{at, lds.found.before, lds.found.value, end, lds.found.tag};
 }
 
-// The token whose cumulative weight is the first above u of the whole, by a workgroup.  cell_sum(c): sum of the weights of cell c; weight(v):
-// weight of entry v.  -1 where the whole is not above `nothing`.
+// The token whose cumulative weight is the first above u of the whole, by a workgroup.  cell_sum(c, reference): the sum of the weights of cell c, 0 where
+// it holds none that can be drawn, and what they are relative to; weight(v, reference): that of entry v, in a unit of the cell's own, 0 where it cannot
+// be drawn.  A cell whose sum is not 0 holds an entry whose weight is not, so a token is found (u is below 1, so some sum exceeds the level)
+// unless the whole is not above `nothing`: then -1.
 template <class C, class W>
 __device__ __forceinline__ int64_t draw_token(int64_t V, int64_t cells, float u, double nothing, PickLds &lds, C &&cell_sum, W &&weight)
 {
     const int tid = threadIdx.x;
     const double share = (double)(u > 0.0f ? u : 0.0f);
     const bool at_once = cells <= kBlock;  // (their sum is known when they are searched)
-    double total = 0.0, before, end;
+    double total = 0.0;
     if (!at_once) {
         double sum = 0.0;
-        for (int64_t c = tid; c < cells; c += kBlock) sum += cell_sum(c);
+        float unused;
+        for (int64_t c = tid; c < cells; c += kBlock) sum += cell_sum(c, unused);
         const double v[1] = {sum};
-        pick(v, 0.0, [](double) { return 0.0; }, lds, before, total);
+        total = pick(v, 0.0f, 0.0, [](double) { return 0.0; }, lds).end;
     }
-    double base = 0.0, found_before = 0.0, level = 0.0;
+    double base = 0.0, level = 0.0;
+    Picked in{-1, 0.0, 1.0, 0.0, 0.0f};
     int64_t cell = -1;
     for (int64_t c0 = 0; c0 < cells; c0 += kBlock) {
-        const double v[1] = {c0 + tid < cells ? cell_sum(c0 + tid) : 0.0};
-        const int at = pick(v, base, [&](double sum) { return share * (at_once ? sum : total); }, lds, before, end);
-        if (at_once) total = end;
+        float reference = 0.0f;
+        const double v[1] = {c0 + tid < cells ? cell_sum(c0 + tid, reference) : 0.0};
+        const Picked got = pick(v, reference, base, [&](double sum) { return share * (at_once ? sum : total); }, lds);
+        if (at_once) total = got.end;
         level = share * total;
-        if (at >= 0) cell = c0 + at, found_before = before;
-        base = end;
-        if (end > level && at >= 0) break;
+        base = got.end;
+        if (got.at < 0) continue;
+        cell = c0 + got.at, in = got;
+        if (base > level) break;
     }
     if (cell < 0 || !(total > nothing)) return -1;
     constexpr int PER = kCell / kBlock;
     const int64_t first = cell * kCell + tid * PER;
     double w[PER];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) w[j] = first + j < V ? weight(first + j) : 0.0;
-    // (found_before is rounded and may lie above the level by that: then the first entry it is)
-    const double rest = __builtin_fmax(level - found_before, 0.0);
-    const int at = pick(w, 0.0, [&](double) { return rest; }, lds, before, end);
-    return at < 0 ? -1 : cell * kCell + at;
+    for (int j = 0; j < PER; ++j) w[j] = first + j < V ? weight(first + j, in.tag) : 0.0;
+    // (the sum before the cell is rounded and may lie above the level by that: then the first entry it is)
+    const double rest = __builtin_fmax(level - in.before, 0.0) / in.value;
+    return cell * kCell + pick(w, 0.0f, 0.0, [&](double sum) { return rest * sum; }, lds).at;
 }
 
 // A workgroup a sequence: the token that follows the drafts that stand.  DECIDE: finds out by itself where that is (drafts without a distribution).
@@ -602,7 +627,8 @@ __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftC
     if (stop.kind == kNoToken) return;
     const int64_t k = span.first_draft + stop.place, row = k + s;
     const Weight wp(stop.p_top, exponent_factor(stop.p_T), least_of(stop.p_T)), wq(stop.q_top, exponent_factor(stop.q_T), least_of(stop.q_T));
-    auto p = [&](int64_t v) { return wp.at(logit_at<DT>(b.logits, row, b.ld, v)); };
+    auto x = [&](int64_t v) { return logit_at<DT>(b.logits, row, b.ld, v); };
+    const CellStats *const stats = ws.target + row * padded_cells(cells);
     // the cell of a draft without a distribution is summed without it
     int64_t out = -1, its = -1;
     double rest = 0.0;
@@ -610,28 +636,35 @@ __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftC
         out = b.tokens[k];
         its = out / kCell;
         constexpr int PER = kCell / kBlock;
-        double w[PER], before;
+        const Weight of_cell(stats[its].top, wp.c, wp.least);
+        double w[PER];
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int64_t v = its * kCell + threadIdx.x * PER + j;
-            w[j] = v < b.V && v != out ? p(v) : 0.0;
+            w[j] = v < b.V && v != out ? of_cell.drawable(x(v)) : 0.0;
         }
-        pick(w, 0.0, [](double) { return 0.0; }, lds, before, rest);
+        rest = pick(w, 0.0f, 0.0, [](double) { return 0.0; }, lds).end;
     }
     const float u = c.sample_u[s];
     int64_t t = -1;
     for (bool from_rest = stop.kind == kFromRest;; from_rest = false) {
         t = draw_token(b.V, cells, u, from_rest ? 0x1p-40 * stop.p_sum : 0.0, lds,
-                       [&](int64_t cell) {
-                           if (from_rest) return ws.rest[s * padded_cells(cells) + cell];
-                           if (cell == its) return rest;
-                           const CellStats of = ws.target[row * padded_cells(cells) + cell];
-                           return of.top > -INFINITY ? moved_to(of.sum, of.top, stop.p_top, wp.c, wp.least) : 0.0;
+                       [&](int64_t cell, float &reference) {
+                           if (from_rest) {
+                               // (1024 weights of more than 2^-980 in all are not all up to kNothing)
+                               const double sum = ws.rest[s * padded_cells(cells) + cell];
+                               return sum > 0x1p-980 ? sum : 0.0;
+                           }
+                           const CellStats of = stats[cell];
+                           reference = of.top;
+                           return of.top > -INFINITY ? moved_to(cell == its ? rest : of.sum, of.top, stop.p_top, wp.c, wp.least) : 0.0;
                        },
-                       [&](int64_t v) {
-                           const double e = p(v);
-                           if (from_rest) return __builtin_fmax(__builtin_fma(-stop.rho, wq.at(logit_at<DT>(c.draft, k, c.ld, v)), e), 0.0);
-                           return v == out ? 0.0 : e;
+                       [&](int64_t v, float reference) {
+                           if (from_rest) {
+                               const double r = __builtin_fma(-stop.rho, wq.at(logit_at<DT>(c.draft, k, c.ld, v)), wp.at(x(v)));
+                               return r > kNothing ? r : 0.0;
+                           }
+                           return v == out ? 0.0 : Weight(reference, wp.c, wp.least).drawable(x(v));
                        });
         // where nothing is left: p, and the drafted token with it
         if (t >= 0 || (!from_rest && its < 0)) break;
@@ -639,7 +672,7 @@ __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftC
     }
     if (threadIdx.x == 0) {
         o.tokens[row] = (int32_t)t;
-        if (o.logp) o.logp[row] = (float)log(p(t) / stop.p_sum);
+        if (o.logp) o.logp[row] = (float)log_probability(x(t), wp, stop.p_sum);
     }
 }
 
@@ -669,13 +702,14 @@ __global__ __launch_bounds__(kBlock) void tree_walk_kernel(DraftBatch b, DraftTr
             break;
         }
         const Weight w(p.top, p.factor, least_of(row_temperature(b, row)));
-        auto weight = [&](int64_t v) { return w.at(logit_at<DT>(b.logits, row, b.ld, v)); };
+        auto x = [&](int64_t v) { return logit_at<DT>(b.logits, row, b.ld, v); };
         const int64_t t = draw_token(b.V, cells, tree.sample_u[row], 0.0, lds,
-                                     [&](int64_t cell) {
+                                     [&](int64_t cell, float &reference) {
                                          const CellStats of = ws.target[row * padded_cells(cells) + cell];
+                                         reference = of.top;
                                          return of.top > -INFINITY ? moved_to(of.sum, of.top, p.top, w.c, w.least) : 0.0;
                                      },
-                                     weight);
+                                     [&](int64_t v, float reference) { return Weight(reference, w.c, w.least).drawable(x(v)); });
         // the first child that holds it
         if (tid == 0) lds_child = 1 << 30;
         __syncthreads();
@@ -691,7 +725,7 @@ __global__ __launch_bounds__(kBlock) void tree_walk_kernel(DraftBatch b, DraftTr
         if (tid == 0) {
             o.tokens[row0 + n] = (int32_t)t;
             o.nodes[row0 + n] = fits ? child : -1;
-            if (o.logp) o.logp[row0 + n] = (float)log(weight(t) / p.sum);
+            if (o.logp) o.logp[row0 + n] = (float)log_probability(x(t), w, p.sum);
             o.flags[row0 + n] = fits ? (uint8_t)kFlagMatch : 0;
         }
         if (!fits) break;

@@ -480,3 +480,54 @@ def test_constant_rows_with_u_on_the_borders_of_cells(difr, dtype, value):
     got = difr.draft_verify(x[:, :n + 1], 1.0, torch.full((32,), n, dtype=torch.int32, device=DEV), one, torch.full((32,), 0.999, device=DEV), u)
     assert got["accepted"].eq(0).all()
     check(got["tokens"][::2])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("u", [0.0, -1.0, math.nan, 2.0 ** -24])
+def test_tokens_of_hardly_any_probability(difr, dtype, u):
+    """A running sum that exceeds 0 at entries of e^-624 and less, whole cells of which come first: they are drawn, masked ones never."""
+    V, faint = 4 * 1024 + 9, -624.0
+    x = torch.zeros(7, V)
+    x[0, :1024] = faint
+    x[1, :2048] = -680.0
+    x[2, :1024], x[2, 1024:2048], x[2, 2048:2050], x[2, 2050:3072] = -math.inf, torch.finfo(dtype).min, -1e9, -680.0
+    x[3, :5], x[3, 5:1024] = -1e9, faint
+    x[4, :1500], x[4, 1500:] = faint, -math.inf
+    x[4, 4104] = 0.0                                      # a single likely token, in the last cell
+    x[5] = x[0] / 100.0
+    x[6, :] = -math.inf
+    x[6, 1024:2048], x[6, 3000], x[6, 4000] = -300.0, -950.0, -301.0
+    x = x.to(dtype)
+    T = torch.tensor([1.0, 1.0, 1.0, 1.0, 1.0, 0.01, 1.0])
+    R = x.shape[0]
+    us = torch.full((R,), u)
+    none = torch.empty(0, dtype=torch.int32)
+    off = [0] * (R + 1)
+    names = ("accepted", "tokens", "logp", "flags")
+    want = ref.tree_verify(x, T.tolist(), [], [], off, us.tolist(), _flags(difr))
+    assert all(t >= 0 for t in want[1])
+    d = lambda t: t.to(DEV)
+    got = difr.tree_verify(d(x), 1.0, d(none), None, d(torch.tensor(off)), d(us), temperatures=d(T))
+    _agree(difr, got, want, ("accepted", "tokens", "nodes", "logp", "flags"))
+    want = ref.draft_verify(x, T.tolist(), [], off, [], us.tolist(), None, [], _flags(difr))
+    _agree(difr, difr.draft_verify(d(x), 1.0, d(none), d(torch.tensor(off)), d(us[:0]), d(us), temperatures=d(T)), want, names)
+    # a draft at every row: it falls, and what is left is drawn from
+    off = list(range(R + 1))
+    both = x.repeat_interleave(2, 0)
+    T2 = T.repeat_interleave(2)
+    y = both[::2].clone()
+    y[:, V - 5:] = 0.0
+    au = torch.full((R,), 0.99)
+    for token in (V - 1, 0, 4104):
+        tokens = torch.full((R,), token, dtype=torch.int32)
+        for draft in (y, None):
+            want = ref.draft_verify(both, T2.tolist(), tokens.tolist(), off, au.tolist(), us.tolist(), draft, T.tolist(), _flags(difr))
+            got = difr.draft_verify(d(both), 1.0, d(tokens), d(torch.tensor(off)), d(au), d(us), draft=None if draft is None else d(draft),
+                                    temperatures=d(T2), draft_temperatures=None if draft is None else d(T))
+            _agree(difr, got, want, names)
+    # trees whose drafts are no tokens at all
+    tokens = torch.full((R,), -1, dtype=torch.int32)
+    want = ref.tree_verify(both, T2.tolist(), tokens.tolist(), None, off, us.repeat_interleave(2).tolist(), _flags(difr))
+    got = difr.tree_verify(d(both), 1.0, d(tokens), None, d(torch.tensor(off)), d(us.repeat_interleave(2)), temperatures=d(T2))
+    _agree(difr, got, want, ("accepted", "tokens", "nodes", "logp", "flags"))
+    assert got["accepted"].eq(0).all() and got["tokens"][::2].ge(0).all()
