@@ -236,6 +236,8 @@ __device__ __forceinline__ void cell_stats(const typename Elem<DT>::type *row, u
     __syncthreads();
 }
 
+constexpr float kBelowOne = 0x1.fffffep-1f;  // what larger random numbers count as
+
 // (The value itself in a register: left to itself the compiler puts it in memory of the thread's, to choose between two addresses.)
 __device__ __forceinline__ float temperature_of(const float *Ts, float T, int64_t row)
 {
@@ -404,7 +406,8 @@ __device__ __forceinline__ bool decide_drafts(const DraftBatch &b, const DraftCh
             const double ps = lds.sum[g], qs = lds.sum[d], p = lds.weight[g] / ps;
             const bool scored = ps > 0.0 && (at >= span.drafts || !c.draft || qs > 0.0);
             const double q = c.draft ? lds.weight[d] / qs : t >= 0 ? 1.0 : 0.0;
-            const bool stands = own && scored && at < span.drafts && lds.weight[g] > kNothing && (double)lds.u[g] * q < p;
+            const double u = lds.u[g] > kBelowOne ? kBelowOne : lds.u[g];  // (a NaN accepts nothing)
+            const bool stands = own && scored && at < span.drafts && lds.weight[g] > kNothing && u * q < p;
             const uint64_t stops = __ballot(own && !stands);
             const int first = stops ? __builtin_ctzll(stops) : 64;
             if (lane == 0) lds.go = first < 64 ? 1 : 0;
@@ -578,7 +581,7 @@ template <class C, class W>
 __device__ __forceinline__ int64_t draw_token(int64_t V, int64_t cells, float u, double nothing, PickLds &lds, C &&cell_sum, W &&weight)
 {
     const int tid = threadIdx.x;
-    const double share = (double)(u > 0.0f ? u : 0.0f);
+    const double share = (double)(u > 0.0f ? fminf(u, kBelowOne) : 0.0f);
     const bool at_once = cells <= kBlock;  // (their sum is known when they are searched)
     double total = 0.0;
     if (!at_once) {

@@ -531,3 +531,32 @@ def test_tokens_of_hardly_any_probability(difr, dtype, u):
     got = difr.tree_verify(d(both), 1.0, d(tokens), None, d(torch.tensor(off)), d(us.repeat_interleave(2)), temperatures=d(T2))
     _agree(difr, got, want, ("accepted", "tokens", "nodes", "logp", "flags"))
     assert got["accepted"].eq(0).all() and got["tokens"][::2].ge(0).all()
+
+
+def test_numbers_outside_count_as_the_nearest_inside(difr):
+    """sample_u: NaN and what is below as 0, what is above as 1 - 2^-24; accept_u: the same above and below (a NaN accepts nothing)."""
+    V, big = 3000, 1 - 2.0 ** -24
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn(12, V, generator=g)
+    x[:, 2000:] = -40.0                                   # behind, tokens that no number below 1 - 2^-24 comes to
+    x[:, 0] = -40.0
+    d = lambda t: t.to(DEV)
+    u = torch.tensor([0.0, math.nan, -0.5, -math.inf, big, 1.0, 1.5, math.inf, 0.5, 2.0 ** -149, -0.0, 1e30])
+    same = [0, 0, 0, 0, 4, 4, 4, 4, 8, 9, 0, 4]
+    one = d(x[:1].repeat(12, 1))
+    none, off = torch.empty(0, dtype=torch.int32, device=DEV), torch.zeros(13, dtype=torch.int64, device=DEV)
+    p = ref.probabilities(x[0], 1.0)
+    assert 0 < ref.first_above(p, big) < 2000
+    for got in (difr.tree_verify(one, 1.0, none, None, off, d(u)), difr.draft_verify(one, 1.0, none, off, none.float(), d(u))):
+        t = got["tokens"].tolist()
+        assert t == [t[i] for i in same] and t[0] == 0 and t[4] == ref.first_above(p, big)
+    # p = q, by a draft and by a token that has all there is: only a NaN lets it fall
+    x[1:] = x[:1]
+    tokens, off = torch.full((12,), 7, dtype=torch.int32, device=DEV), torch.arange(13, device=DEV)
+    rows = d(x[:1].repeat(24, 1))
+    su = torch.full((12,), 0.5, device=DEV)
+    stands = [0 if math.isnan(v) else 1 for v in u.tolist()]
+    assert difr.draft_verify(rows, 1.0, tokens, off, d(u), su, draft=rows[:12])["accepted"].tolist() == stands
+    rows[:] = -math.inf
+    rows[:, 7] = 0.0
+    assert difr.draft_verify(rows, 1.0, tokens, off, d(u), su)["accepted"].tolist() == stands
