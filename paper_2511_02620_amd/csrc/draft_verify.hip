@@ -651,7 +651,7 @@ __global__ __launch_bounds__(kBlock) void draft_draw_kernel(DraftBatch b, DraftC
     const float u = c.sample_u[s];
     int64_t t = -1;
     for (bool from_rest = stop.kind == kFromRest;; from_rest = false) {
-        t = draw_token(b.V, cells, u, from_rest ? 0x1p-40 * stop.p_sum : 0.0, lds,
+        t = draw_token(b.V, cells, u, from_rest || its >= 0 ? 0x1p-40 * stop.p_sum : 0.0, lds,
                        [&](int64_t cell, float &reference) {
                            if (from_rest) {
                                // (1024 weights of more than 2^-980 in all are not all up to kNothing)

@@ -560,3 +560,16 @@ def test_numbers_outside_count_as_the_nearest_inside(difr):
     rows[:] = -math.inf
     rows[:, 7] = 0.0
     assert difr.draft_verify(rows, 1.0, tokens, off, d(u), su)["accepted"].tolist() == stands
+
+
+def test_a_draft_that_falls_where_nothing_is_left(difr):
+    """p of the drafted token is 1 - 2^-50: what is left of p - q is below 2^-40, so p is drawn from, with a draft and without."""
+    x = torch.full((2, 5), -math.inf)
+    x[:, 1], x[:, 3] = 0.0, -50 * math.log(2.0)
+    one, tokens = torch.tensor([0, 1]), torch.tensor([1], dtype=torch.int32)
+    for draft in (None, torch.tensor([[-math.inf, 0.0, -math.inf, -math.inf, -math.inf]])):
+        want = ref.draft_verify(x, [1.0, 1.0], [1], [0, 1], [math.nan], [0.5], draft, [1.0], _flags(difr))
+        assert want[:2] == ([0], [1, -1])
+        got = difr.draft_verify(x.to(DEV), 1.0, tokens.to(DEV), one.to(DEV), torch.full((1,), math.nan, device=DEV), torch.full((1,), 0.5, device=DEV),
+                                draft=None if draft is None else draft.to(DEV))
+        _agree(difr, got, want, ("accepted", "tokens", "logp", "flags"))
