@@ -641,8 +641,8 @@ int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64
  * has the tokens [offsets[b], offsets[b + 1]) and one row of logits more than tokens, rows offsets[b] + b ... offsets[b + 1] + b: row 0 is
  * the position after the last token that is certain.  offsets [B + 1] is non-decreasing from 0 to D (what is outside is held in [0, D]).
  * A masked logit (-inf, the type's lowest value) has no probability, and a masked token is never emitted.
- * Weights of a row, exp((x - its largest logit) / T), and their sums are fp64, good to 2^-45; the result does not depend on the order in
- * which workgroups run.  Random numbers are the caller's: fp32 in [0, 1); what is below counts as 0, what is above as the largest (1 - 2^-24).
+ * Weights of a row, exp((x - its largest logit) / T), and their sums are fp64, good to 2^-44 down to 2^-60 of the largest; the result
+ * does not depend on the order in which workgroups run.  Random numbers are the caller's: fp32 in [0, 1); what is below counts as 0, what is above as the largest (1 - 2^-24).
  * A NaN in sample_u counts as 0, one in accept_u accepts nothing.
  */
 typedef struct {

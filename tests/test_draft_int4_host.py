@@ -1,6 +1,10 @@
 """What the calls on drafted tokens and on 4-bit integers refuse before they touch the device, and the reference forms by hand."""
 import ctypes as C
+import decimal
 import math
+import os
+import re
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -169,3 +173,25 @@ def test_the_reference_by_hand():
     assert got[:3] == ([2], [1, 1, 0, -1], [1, 2, -1, -1]) and got[4] == [1, 1, 0, 0]
     codes, scales, zeros, values = ref.int4(torch.tensor([[7.0, -7.0, 3.4] + [0.0] * 29]), 32, False)
     assert codes[0, 0] == 15 | 1 << 4 and scales[0, 0] == 1.0 and values[0, :3].tolist() == [7.0, -7.0, 3.0]
+
+
+def test_the_polynomial_of_the_weights():
+    """2^f over |f| <= 1/2, with the coefficients of the source in exact arithmetic: within 2^-45.9 of the value, so that a weight moved by two more
+    such factors is good to 2^-44."""
+    source = open(os.path.join(os.path.dirname(binding.__file__), "csrc", "draft_verify.hip")).read()
+    body = source[source.index("double power(double d, double c)"):]
+    body = body[:body.index("return")]
+    first = re.search(r"double p = (0x1\.[0-9a-f]+p-\d+);", body).group(1)
+    rest = re.findall(r"p = __builtin_fma\(p, f, ([^)]+)\);", body)
+    coefficients = [Fraction(float.fromhex(c)) if "x" in c else Fraction(c) for c in [first] + rest]
+    assert len(coefficients) == 10 and coefficients[-1] == 1
+    decimal.getcontext().prec = 40
+    ln2, worst = decimal.Decimal(2).ln(), decimal.Decimal(0)
+    for i in range(-500, 501):
+        f = Fraction(i, 1000)
+        p = Fraction(0)
+        for c in coefficients:
+            p = p * f + c
+        want = (decimal.Decimal(f.numerator) / decimal.Decimal(f.denominator) * ln2).exp()
+        worst = max(worst, abs(decimal.Decimal(p.numerator) / decimal.Decimal(p.denominator) / want - 1))
+    assert worst < decimal.Decimal(2) ** decimal.Decimal("-45.9"), worst
