@@ -640,7 +640,9 @@ int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64
  * of their positions at once, and keeps what the target's own distribution would give.  B sequences, D drafted tokens in all; sequence b
  * has the tokens [offsets[b], offsets[b + 1]) and one row of logits more than tokens, rows offsets[b] + b ... offsets[b + 1] + b: row 0 is
  * the position after the last token that is certain.  offsets [B + 1] is non-decreasing from 0 to D (what is outside is held in [0, D]).
- * A masked logit (-inf, the type's lowest value) has no probability, and a masked token is never emitted.
+ * A masked logit (-inf, the type's lowest value; what is 691 T and more below the row's largest may count as one) has no probability and is
+ * never emitted.  But a row that holds nothing above the lowest value is not masked whole: its entries of that value are
+ * uniform, here as in the log-probabilities above.  A mask that may leave nothing has to be -inf to end the sequence.
  * Weights of a row, exp((x - its largest logit) / T), and their sums are fp64, good to 2^-44 down to 2^-60 of the largest; the result
  * does not depend on the order in which workgroups run.  Random numbers are the caller's: fp32 in [0, 1); what is below counts as 0, what is above as the largest (1 - 2^-24).
  * A NaN in sample_u counts as 0, one in accept_u accepts nothing.
