@@ -573,3 +573,58 @@ def test_a_draft_that_falls_where_nothing_is_left(difr):
         got = difr.draft_verify(x.to(DEV), 1.0, tokens.to(DEV), one.to(DEV), torch.full((1,), math.nan, device=DEV), torch.full((1,), 0.5, device=DEV),
                                 draft=None if draft is None else draft.to(DEV))
         _agree(difr, got, want, ("accepted", "tokens", "logp", "flags"))
+
+
+@pytest.mark.parametrize("V", [196609, 262144, 262145, 600000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_vocabularies(difr, V, dtype):
+    """More cells than a wave holds of a row (192), and than are searched at once (256 of 1024 entries): draws in each round of the search, beside its
+    border, and behind cells that are masked whole."""
+    g = torch.Generator().manual_seed(V)
+    T = float(torch.tensor(0.9))                          # as fp32 holds it
+    x = (torch.randn(9, V, generator=g) * 2).to(dtype)
+    edge = min(262144, V - 1025)
+    x[3, :edge] = -math.inf
+    x[4, :edge] = torch.finfo(dtype).min
+    x[5, 1024:edge] = -math.inf
+    x[6, :] = -math.inf
+    x[6, edge], x[6, V - 1] = 0.0, 1.0
+    x[7, 1024:] = -1e9
+    x[8, :-1] = -math.inf
+    us = []
+    for row in range(9):
+        p = ref.probabilities(x[row], T)
+        c = np.cumsum(p)
+        near_edge = [float(np.nextafter(np.float32(c[edge - 1]), np.float32(s))) for s in (0, 2)]
+        us.append([u for u in [0.0, 0.31, 0.77, 1 - 2.0 ** -24] + near_edge if 0 <= u < 1 and not ref.near(p, u, 1e-12)])
+        assert len(us[-1]) >= 2, row
+    rows = [i for i in range(9) for _ in us[i]]
+    flat = torch.tensor([u for row in us for u in row])
+    R = len(rows)
+    y, off, none = x[rows], [0] * (R + 1), torch.empty(0, dtype=torch.int32)
+    want = ref.tree_verify(y, [T] * R, [], [], off, flat.tolist(), _flags(difr))
+    args = (y.to(DEV), T, none.to(DEV))
+    _agree(difr, difr.tree_verify(*args, None, torch.tensor(off).to(DEV), flat.to(DEV)), want, ("accepted", "tokens", "nodes", "logp", "flags"))
+    want = want[:2] + want[3:]
+    _agree(difr, difr.draft_verify(*args, torch.tensor(off).to(DEV), torch.empty(0, device=DEV), flat.to(DEV)), want, ("accepted", "tokens", "logp", "flags"))
+    for with_draft in (True, False):
+        case = _chains(V + 1, [2, 0, 1, 2], V, dtype)
+        case[1][6, :edge], case[2][3, 7:edge] = -math.inf, -math.inf
+        _check_chain(difr, case, 0.8, 0.8, with_draft)
+    case = _trees(V + 2, [5, 3], V, dtype, hit=1.0)
+    case[2][0, 5:edge] = -math.inf
+    _hit(case, torch.ones(10), 1)
+    assert int(_check_tree(difr, case, 1.0)["accepted"].sum()) >= 2
+
+
+def test_large_batches_of_large_vocabularies(difr):
+    """The same, level by level."""
+    V = 300000
+    case = _chains(5, [2] * 70, V, torch.bfloat16, drift=0.4, spread=1.0)
+    case[1][::4, :262144] = -math.inf
+    got, _ = _check_chain(difr, case, 0.9, 0.9)
+    assert int(got["accepted"].sum()) > 30
+    case = _trees(6, [6] * 30, V, torch.bfloat16, hit=1.0)
+    case[2][::5, 100:262200] = -math.inf
+    _hit(case, torch.ones(210), 2)
+    assert int(_check_tree(difr, case, 1.0)["accepted"].sum()) > 30
