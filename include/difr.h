@@ -623,9 +623,11 @@ int difr_int4_dequantize(const uint8_t *codes, const void *scales, const uint8_t
                          int32_t dtype, int64_t ld, void *hip_stream);
 /*
  * out[n][v] = sum_k hidden[n][k] w[v][k], k < d: the logits of N hidden states (bf16 or fp32, [N, ldh]) under a head of V rows.  Products
- * of elements and codes are exact, accumulation and scaling are fp32, and the sum is rounded once to bf16 or fp32 ([N, ld], ld >= V).
- * Meant for the few rows that are decoded together: the head is read once for every 64 of them (fp32 states: every 32; heads of fewer than 16,369 rows: every 16).  Rows that hold a NaN, an infinity or
- * magnitudes above 2^120 get NaN or infinities.  A row's result does not depend on the rows beside it.  V < 2^31, bases aligned to the element size; out overlaps nothing.
+ * of states and (code - zero) are exact, their accumulation and scaling are fp32, and the sum is rounded once to bf16 or fp32 ([N, ld], ld >= V).
+ * States count to 2^-39 of their row's largest magnitude (bf16 ones that are above 2^-32 of it, exactly); scales of 2^80 and more may overflow.
+ * Meant for the few rows that are decoded together: the head is read once for every 64 of them (fp32 states: every 32; heads of fewer than
+ * 16,369 rows: every 16).  Rows that hold a NaN or an infinity get NaN or infinities.  A row's result does not depend on the rows beside it.
+ * V < 2^31, bases aligned to the element size; out overlaps nothing.
  * workspace  DEVICE scratch of at least difr_int4_product_workspace_bytes(N, d, hidden_dtype, group) bytes (host only; 0: none is needed and
  * NULL will do), 16-byte aligned, contents irrelevant before and after; calls that overlap in time need distinct workspaces.  Too small:
  * DIFR_ERR_SHAPE.

@@ -671,7 +671,7 @@ size_t difr_int4_product_workspace_bytes(int64_t N, int64_t d, int32_t hidden_dt
 {
     if (N < 1 || N >= (int64_t)1 << 31 || d < 1 || d >= (int64_t)1 << 23 || !int4_group(group) || (hidden_dtype != DIFR_BF16 && hidden_dtype != DIFR_F32))
         return 0;
-    return difr::int4_product_workspace_bytes(N, d, hidden_dtype, group);
+    return difr::int4_product_workspace_bytes(N, d, hidden_dtype);
 }
 
 int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64_t d, int64_t ldh, const uint8_t *codes, const void *scales,
@@ -685,7 +685,7 @@ int difr_int4_product(const void *hidden, int32_t hidden_dtype, int64_t N, int64
     if (rc != DIFR_OK || N == 0 || V == 0) return rc;
     if (!hidden) return DIFR_ERR_NULL;
     if ((uintptr_t)hidden % element_size(hidden_dtype) || (uintptr_t)workspace % 16u) return DIFR_ERR_ALIGN;
-    const size_t need = difr::int4_product_workspace_bytes(N, d, hidden_dtype, group);
+    const size_t need = difr::int4_product_workspace_bytes(N, d, hidden_dtype);
     if (workspace_bytes < need) return DIFR_ERR_SHAPE;
     if (need && !workspace) return DIFR_ERR_NULL;
     if ((rc = check_device()) != DIFR_OK) return rc;

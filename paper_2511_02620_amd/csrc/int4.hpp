@@ -22,6 +22,6 @@ int launch_int4_quantize(const void *x, int dtype, int64_t N, int64_t d, int64_t
 int launch_int4_dequantize(const Int4Matrix &m, int64_t d, void *x, int dtype, int64_t ld, hipStream_t stream);
 int launch_int4_product(const void *h, int h_dtype, int64_t N, int64_t d, int64_t ldh, const Int4Matrix &m, void *out, int dtype, int64_t ld,
                         void *workspace, hipStream_t stream);
-size_t int4_product_workspace_bytes(int64_t N, int64_t d, int dtype, int group);
+size_t int4_product_workspace_bytes(int64_t N, int64_t d, int dtype);
 
 }  // namespace difr

@@ -1,24 +1,24 @@
 // out[n][v] = sum_k h[n][k] w[v][k] for a head w in 4-bit integers with group scales: the few hidden states that are decoded together.
 //
 // What bounds it is reading the codes once, so everything else has to hide behind that: a compute unit gets some 10 bytes of codes a
-// cycle.  A code goes to the matrix cores as the bf16 number 16 + code, which is two instructions for two codes (a shift, and one that masks
-// them into bits 3 ... 6 of 0x4180), and exact.  With S_g = sum_{k in g} h_k over a group,
-//   sum_{k in g} s (code - zero) h_k = s (sum_{k in g} (16 + code) h_k)  -  s (16 + zero) S_g:
-// products of whole numbers below 32 by bf16 numbers are exact in fp32, a group's sum is scaled in fp32, and the second part is a product of
-// its own on the matrix cores, four groups at once: S_g in three bf16 parts (24 bits), s (16 + zero) in two (13 bits, exact), so that nothing
-// but fp32 accumulation is rounded.  fp32 hidden states are three bf16 parts too, one matrix instruction each.
+// cycle.  A code goes to the matrix cores as the fp16 number code - zero: masked into the fraction of 1024 (or, from bits 4 ... 7, 16 times
+// itself), which takes an instruction for two codes, and an addition (or multiply-add) of two more, all of them exact.  Hidden states are scaled by a
+// power of two that brings their row's largest magnitude between 2^15 and 2^16, and go there as one fp16 number (bf16 states: exact down to 2^-32 of that
+// magnitude) or three (fp32 states); what is cut off is below 2^-39 of it.  A group's sum of exact products is accumulated in fp32 and scaled in
+// fp32; the row's power of two comes off at the end.
 #include "difr_host.hpp"
 #include "int4.hpp"
 #include "softmax_row.hpp"
 
 namespace difr {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef u32x2 u32x2_any __attribute__((aligned(1)));
 typedef uint32_t u32_any __attribute__((aligned(1)));
 typedef uint16_t u16_any __attribute__((aligned(1)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 struct Int4Product {
     const void *h;
@@ -29,40 +29,27 @@ struct Int4Product {
     int f32_out;
     int passes, per_pass;   // of the blocks of 16 rows of the head that a wave has, `per_pass` at a time
     const uint8_t *image;   // hidden states as the matrix instructions want them (int4_image_kernel), or null
+    const uint32_t *tops;   // with the image: the largest magnitudes of its rows, by which they are scaled
 };
 
 constexpr int kSlab = 256;                     // elements of a row that a step takes
 constexpr int kHiddenBytes = 122 * 1024;       // of LDS for hidden states that stay there
 
-// The order in which the codes of four bytes come out of two at a time: 0 4 1 5 2 6 3 7.  Hidden states are put in that order in LDS.
-__device__ __forceinline__ u32x4 code_order(u32x4 q)
-{
-    return u32x4{__builtin_amdgcn_perm(q.z, q.x, 0x05040100u), __builtin_amdgcn_perm(q.z, q.x, 0x07060302u),
-                 __builtin_amdgcn_perm(q.w, q.y, 0x05040100u), __builtin_amdgcn_perm(q.w, q.y, 0x07060302u)};
-}
-// Eight codes as bf16 numbers 16 + code, in that order.  (The two constants in registers: one instruction takes one of another kind.)
+// Eight codes as fp16 numbers code - zero, two at a time: 0 4 1 5 2 6 3 7.  Hidden states are put in that order.  (Masks and 1024 in registers: one
+// instruction takes one constant of another kind.)
 struct CodeBits {
-    uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
-    __device__ __forceinline__ CodeBits() { asm("" : "+v"(mask), "+v"(sixteen)); }
-    __device__ __forceinline__ bf16x8 of(uint32_t w) const
+    uint32_t low = 0x000F000Fu, high = 0x00F000F0u, one = 0x64006400u;
+    __device__ __forceinline__ CodeBits() { asm("" : "+v"(low), "+v"(high), "+v"(one)); }
+    __device__ __forceinline__ f16x8 of(uint32_t w, f16x2 less) const  // less: -(1024 + zero), twice
     {
-        return __builtin_bit_cast(bf16x8, u32x4{(w << 3 & mask) | sixteen, (w >> 1 & mask) | sixteen, (w >> 5 & mask) | sixteen, (w >> 9 & mask) | sixteen});
+        const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, less64 = less + f16x2{(_Float16)960.0f, (_Float16)960.0f};
+        auto pair = [](uint32_t bits) { return __builtin_bit_cast(f16x2, bits); };
+        const uint32_t up = w >> 8;
+        const f16x2 a = pair((w & low) | one) + less, b = __builtin_elementwise_fma(pair((w & high) | one), sixteenth, less64);
+        const f16x2 c = pair((up & low) | one) + less, d = __builtin_elementwise_fma(pair((up & high) | one), sixteenth, less64);
+        return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
     }
 };
-// An fp32 number as three bf16 numbers whose sum it is (the first two cut).
-struct Three {
-    uint32_t h, m, l;  // upper halves
-};
-__device__ __forceinline__ Three three_parts(float f)
-{
-    Three t;
-    t.h = __float_as_uint(f) & 0xFFFF0000u;
-    const float r = f - __uint_as_float(t.h);
-    t.m = __float_as_uint(r) & 0xFFFF0000u;
-    t.l = __float_as_uint(r - __uint_as_float(t.m)) & 0xFFFF0000u;
-    return t;
-}
-__device__ __forceinline__ uint32_t halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }  // of upper halves
 
 // A block of 16 rows and a slab as a wave fetches it: neighbouring lanes neighbouring bytes (the caches are asked for each run of lanes apart; a lane
 // a row of its own took four times the requests, and those were what the time went to).  Codes: lane l 16 bytes l % 8 of rows l / 8 and 8 + l / 8.
@@ -89,65 +76,98 @@ struct Int4Slab {
         else
             return __uint_as_float(GS % 2 ? s[GS / 2] & 0xFFFF0000u : s[GS / 2] << 16);
     }
-    // of group 4 q + kg (G = 128: kg % 2)
-    __device__ __forceinline__ float scale_of(int q, int kg) const
+    template <int GS>
+    __device__ __forceinline__ f16x2 less() const  // -(1024 + zero point) of group GS, twice
     {
-        if constexpr (G == 128) return __uint_as_float((uint32_t)(kg & 1 ? s[1] : s[0]) << 16);
-        const uint32_t pair = G == 64 ? (kg & 2 ? s[1] : s[0]) : q ? (kg & 2 ? s[3] : s[2]) : (kg & 2 ? s[1] : s[0]);
-        return __uint_as_float(kg & 1 ? pair & 0xFFFF0000u : pair << 16);
-    }
-    __device__ __forceinline__ uint32_t zero_of(int q, int kg) const
-    {
-        if constexpr (G == 128) return kg & 1 ? z[1] : z[0];
-        if constexpr (G == 64) return (uint32_t)(kg & 2 ? z[1] : z[0]) >> (8 * (kg & 1)) & 0xFFu;
-        return (q ? z[1] : z[0]) >> (8 * kg) & 0xFFu;
+        const uint32_t zero = G == 128 ? z[GS % 2] : G == 64 ? z[GS / 2 % 2] >> (8 * (GS % 2)) & 0xFFu : z[GS / 4 % 2] >> (8 * (GS % 4)) & 0xFFu;
+        return __builtin_bit_cast(f16x2, (zero << 16 | zero) + 0xE400E400u);
     }
 };
 
-// Two vectors of eight elements in the order of the codes, and their sum, as the matrix instructions want them.
+// Eight elements of a row of at least eight, zeros from element d on: there the row's last eight are loaded and moved down.  (In two steps, so that no
+// branch stands between loads.)
+template <int HT>
+struct EightStates {
+    static constexpr int E = Elem<HT>::kPerVec;
+    u32x4 q[8 / E];
+    int down;
+    __device__ __forceinline__ void load(const typename Elem<HT>::type *p, int64_t at, int64_t d)
+    {
+        const int64_t from = at + 8 <= d ? at : d - 8;
+        down = at - from < 8 ? (int)(at - from) : 8;
+#pragma unroll
+        for (int i = 0; i < 8 / E; ++i) q[i] = *reinterpret_cast<const u32x4_any *>(p + from + i * E);
+    }
+    // The largest magnitude among the row's elements that were loaded, as the bits of an fp32 number (of a NaN above those of an infinity).
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        if constexpr (HT == 0) {
+            auto magnitudes = [](uint32_t w) { return __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu); };
+            const u16x2 top = __builtin_elementwise_max(__builtin_elementwise_max(magnitudes(q[0].x), magnitudes(q[0].y)),
+                                                        __builtin_elementwise_max(magnitudes(q[0].z), magnitudes(q[0].w)));
+            return (uint32_t)max(top.x, top.y) << 16;
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, q[i / 4][i % 4] & 0x7FFFFFFFu);
+            return top;
+        }
+    }
+    __device__ __forceinline__ void values(float (&e)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8 / E; ++i) unpack_vector<HT>(q[i], e + i * E);
+        if (down) {
+#pragma unroll
+            for (int step = 8; step; step >>= 1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float behind = j + step < 8 ? e[j + step] : 0.0f;
+                    e[j] = down & step ? behind : e[j];
+                }
+            }
+        }
+    }
+};
+// Over the lanes of half a wave, whose last has it: by moves between lanes of the vector unit.
+__device__ __forceinline__ uint32_t largest_of_32(uint32_t top)
+{
+    auto step = [&](auto CTRL, auto ROWS) {
+        top = max(top, (uint32_t)__builtin_amdgcn_update_dpp((int)top, (int)top, decltype(CTRL)::value, decltype(ROWS)::value, 0xF, false));
+    };
+    step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xF>());  // the lane before
+    step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xF>());
+    step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xF>());
+    step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xF>());
+    step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());  // the last lane of the 16 before, into the second and fourth 16
+    return top;
+}
+// The exponent of the power of two that brings a row's largest magnitude between 2^15 and 2^16.
+__device__ __forceinline__ int shift_of(uint32_t top) { return 16 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)); }
+
+// Eight elements, scaled, in the order of the codes, as the matrix instructions want them: one fp16 number each, or three whose sum they are.  Cut, not
+// rounded: what is next to 2^16 stays below it.  (What is no finite number stays so, or gives NaN.)
 template <int HT>
 struct Eight {
     static constexpr int P = HT == 0 ? 1 : 3;
     u32x4 part[P];
-    float sum;
-    __device__ __forceinline__ Eight(const typename Elem<HT>::type *p, int64_t at, int64_t d)  // zeros from element d on
+    __device__ __forceinline__ Eight(float (&e)[8], int shift)
     {
-        float e[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = 0.0f;
-        constexpr int E = Elem<HT>::kPerVec;
+        for (int j = 0; j < 8; ++j) e[j] = ldexpf(e[j], shift);
 #pragma unroll
-        for (int j = 0; j < 8; j += E) {
-            if (at + j + E <= d) {
-                unpack_vector<HT>(*reinterpret_cast<const u32x4_any *>(p + at + j), e + j);
-            } else {
+        for (int p = 0; p < P; ++p) {
+            uint32_t pair[4];
 #pragma unroll
-                for (int i = 0; i < E; ++i)
-                    if (at + j + i < d) e[j + i] = Elem<HT>::to_float(p[at + j + i]);
+            for (int j = 0; j < 4; ++j) {
+                const auto h = __builtin_amdgcn_cvt_pkrtz(e[j], e[j + 4]);
+                pair[j] = __builtin_bit_cast(uint32_t, h);
+                e[j] -= (float)h.x, e[j + 4] -= (float)h.y;
             }
-        }
-        sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-        Three t[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = three_parts(e[j]);  // (of bf16 the first part is all)
-        part[0] = u32x4{halves(t[0].h, t[4].h), halves(t[1].h, t[5].h), halves(t[2].h, t[6].h), halves(t[3].h, t[7].h)};
-        if constexpr (P == 3) {
-            part[1] = u32x4{halves(t[0].m, t[4].m), halves(t[1].m, t[5].m), halves(t[2].m, t[6].m), halves(t[3].m, t[7].m)};
-            part[2] = u32x4{halves(t[0].l, t[4].l), halves(t[1].l, t[5].l), halves(t[2].l, t[6].l), halves(t[3].l, t[7].l)};
+            part[p] = u32x4{pair[0], pair[1], pair[2], pair[3]};
         }
     }
 };
-// A group's sum, by the first of the G / 8 lanes that have its elements: in three parts.
-template <int G>
-__device__ __forceinline__ u32x2 group_sum(float sum)
-{
-#pragma unroll
-    for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor(sum, o);
-    const Three t = three_parts(sum);
-    return u32x2{halves(t.h, t.m), t.l >> 16};
-}
-// A fragment of three-part sums, to be multiplied by two-part coefficients: slots h m l h m l.
-__device__ __forceinline__ u32x4 sum_slots(u32x2 m) { return u32x4{m.x, m.y | m.x << 16, m.x >> 16 | m.y << 16, 0u}; }
 
 // The step of a half slab (128 elements) in which the eight elements `piece` of it are multiplied, and the quarter of the lanes that has them.
 template <int G>
@@ -167,29 +187,58 @@ __device__ __forceinline__ int piece_of(int j, int kg)
 }
 
 // Batches of more than 16 hidden states, whose fragments are the same for every workgroup and do not fit its LDS: an image of them in
-// global memory.  For each slab, tile of 16 states and part, 8 fragments of 64 lanes of 16 bytes; then the fragments of the groups' sums.
+// global memory.  For each slab, tile of 16 states and part, 8 fragments of 64 lanes of 16 bytes.
 constexpr int kFragment = 1024;
-template <int G, int P>
-constexpr int image_fragments() { return P * 8 + (kSlab / G + 3) / 4; }  // of a slab and tile
+constexpr int kTopBytes = 1024 * 4;  // of the workspace: the largest magnitudes of the rows of a launch; then the image
 
-// A thread eight elements of a row of 256.
+// A workgroup a row, whose largest magnitude it finds first; it keeps what it has read of up to 8192 elements.
+constexpr int kImageThreads = 512, kImageHeld = 2;
 template <int HT, int G>
-__global__ __launch_bounds__(kBlock) void int4_image_kernel(const typename Elem<HT>::type *h, int64_t N, int64_t d, int64_t ldh, int tiles, uint8_t *image)
+__global__ __launch_bounds__(kImageThreads) void int4_image_kernel(const typename Elem<HT>::type *h, int64_t N, int64_t d, int64_t ldh, int slabs,
+                                                                   int tiles, uint8_t *image, uint32_t *tops)
 {
-    constexpr int P = Eight<HT>::P, F = image_fragments<G, P>();
-    const int id = blockIdx.x * kBlock + threadIdx.x, piece = id & 31, row = id >> 5, tile = row >> 4, n = row & 15;
-    const int64_t slab = blockIdx.y;
-    uint8_t *const to = image + (slab * tiles + tile) * (int64_t)(F * kFragment);
-    const Eight<HT> x(h + (row < N ? row : N - 1) * ldh, slab * kSlab + piece * 8, row < N ? d : 0);
-    int j, kg;
-    step_of<G>(piece & 15, j, kg);
+    constexpr int P = Eight<HT>::P, F = P * 8;
+    __shared__ uint32_t lds_top[kImageThreads / 32];
+    const int first = threadIdx.x, row = blockIdx.x, n = row & 15;
+    const typename Elem<HT>::type *const from = h + (row < N ? row : N - 1) * ldh;  // (what is made of rows behind is not stored)
+    uint8_t *const to = image + (int64_t)(row >> 4) * (F * kFragment) + n * 16;
+    const int pieces = slabs * 32;
+    EightStates<HT> held[kImageHeld];
 #pragma unroll
-    for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4 *>(to + (p * 8 + (piece >> 4) * 4 + j) * kFragment + (kg * 16 + n) * 16) = x.part[p];
-    const u32x2 m = group_sum<G>(x.sum);
-    const int g = piece / (G / 8);
-    if (piece % (G / 8) == 0) *reinterpret_cast<u32x4 *>(to + (P * 8 + g / 4) * kFragment + ((g & 3) * 16 + n) * 16) = sum_slots(m);
-    if (G == 128 && piece % 16 == 0)  // a slab of two groups: the other two quarters
-        *reinterpret_cast<u32x4 *>(to + P * 8 * kFragment + ((g + 2) * 16 + n) * 16) = u32x4{0u, 0u, 0u, 0u};
+    for (int i = 0; i < kImageHeld; ++i) held[i].load(from, (int64_t)(first + i * kImageThreads) * 8, d);
+    uint32_t top = 0;
+    for (int piece = first + kImageHeld * kImageThreads; piece < pieces; piece += kImageThreads) {
+        EightStates<HT> more;
+        more.load(from, (int64_t)piece * 8, d);
+        top = max(top, more.largest());
+    }
+#pragma unroll
+    for (int i = 0; i < kImageHeld; ++i) top = max(top, held[i].largest());
+    top = largest_of_32(top);
+    if (threadIdx.x % 32 == 31) lds_top[threadIdx.x / 32] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kImageThreads / 32; ++w) top = max(top, lds_top[w]);
+    const int shift = shift_of(top);
+    if (first == 0) tops[row] = top;
+    auto put = [&](int piece, const EightStates<HT> &states) __attribute__((always_inline)) {
+        float e[8];
+        states.values(e);
+        const Eight<HT> x(e, shift);
+        int j, kg;
+        step_of<G>(piece & 15, j, kg);
+        uint8_t *const at = to + (int64_t)(piece >> 5) * tiles * (F * kFragment) + (((piece >> 4 & 1) * 4 + j) * kFragment + kg * 256);
+#pragma unroll
+        for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4 *>(at + p * 8 * kFragment) = x.part[p];
+    };
+#pragma unroll
+    for (int i = 0; i < kImageHeld; ++i)
+        if (first + i * kImageThreads < pieces) put(first + i * kImageThreads, held[i]);
+    for (int piece = first + kImageHeld * kImageThreads; piece < pieces; piece += kImageThreads) {
+        EightStates<HT> more;
+        more.load(from, (int64_t)piece * 8, d);
+        put(piece, more);
+    }
 }
 
 // Hidden states in P parts; NT tiles of 16 of them from the image, a step ahead (RESIDENT: up to 16, converted by each workgroup and kept in
@@ -202,13 +251,14 @@ template <int HT, bool RESIDENT, int NT, int KS, int G, bool ZEROS, int RB, int 
 __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
 {
     constexpr int kProductWaves = W, kProductThreads = W * 64;
-    constexpr int P = Eight<HT>::P, kGroups = kSlab / G, kQuads = (kGroups + 3) / 4, F = image_fragments<G, P>();
+    constexpr int P = Eight<HT>::P, kGroups = kSlab / G, F = P * 8;
     constexpr int kSteps = G / 32;     // matrix instructions of a group
-    constexpr int kStage = KS * NT * F * kFragment, kPieces = (kStage / 16 + kProductThreads - 1) / kProductThreads;
+    constexpr int kStage = KS * NT * F * kFragment, kPieces = kStage / 16 / kProductThreads;
     constexpr int kTeams = kProductWaves / KS;
-    static_assert(!RESIDENT || NT == 1, "one tile stays");
+    static_assert(RESIDENT ? NT == 1 : kPieces * 16 * kProductThreads == kStage, "one tile stays; all threads fetch the image");
     __shared__ __attribute__((aligned(16))) uint8_t lds[RESIDENT ? kHiddenBytes : 2 * kStage];
     __shared__ __attribute__((aligned(16))) uint8_t lds_code[kProductWaves][RB * 16 * kCodePitch];  // a wave's own
+    __shared__ uint32_t lds_top[NT * 16];                                                           // rows' largest magnitudes
     static_assert(KS == 1 || RB * NT * kFragment <= RB * 16 * kCodePitch, "a wave's share of the sums fits where its codes were");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -229,21 +279,40 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
         asm volatile("" ::: "memory");
     };
 
-    // ---- hidden states that stay: rows of K elements (and 16 bytes, to spread a fragment over the banks) of each part, then sums
+    // ---- hidden states that stay: rows of K elements (and 16 bytes, to spread a fragment over the banks) of each part
     const int hpitch = nslab * (kSlab * 2) + 16, plane = rows_here * hpitch;
-    u32x2 *const lds_sum = reinterpret_cast<u32x2 *>(lds + P * plane);  // [row][group]
-    const int spitch = nslab * kGroups + 2;
-    if constexpr (RESIDENT) {
-        const int row_pieces = nslab * 32;
-        for (int id = tid; id < rows_here * row_pieces; id += kProductThreads) {
-            const int row = id / row_pieces, piece = id - row * row_pieces;
-            const Eight<HT> x(reinterpret_cast<const typename Elem<HT>::type *>(a.h) + (n0 + row) * a.ldh, (int64_t)piece * 8, a.d);
-#pragma unroll
-            for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4 *>(lds + p * plane + row * hpitch + piece * 16) = x.part[p];
-            const u32x2 m = group_sum<G>(x.sum);  // (32 pieces of a slab go to half a wave: a group's lanes are there together)
-            if (piece % (G / 8) == 0) lds_sum[row * spitch + piece / (G / 8)] = m;
+    // A slab of a row to half a wave at a time: from the first to the last for the magnitudes, and back again.
+    constexpr int kHalves = kProductThreads / 32;
+    EightStates<HT> states;
+    const int all = rows_here * nslab, lane_piece = lane & 31;
+    const uint32_t part = 65536u / nslab + 1;                      // id / nslab = id part / 2^16: of ids up to 244, which fit the LDS
+    auto row_of = [&](int id) { return (int)((uint32_t)id * part >> 16); };
+    auto fetch_states = [&](int at) __attribute__((always_inline)) {
+        const int id = min(at + (tid >> 5), all - 1), row = row_of(id);
+        states.load(reinterpret_cast<const typename Elem<HT>::type *>(a.h) + (n0 + row) * a.ldh, (id - row * nslab) * kSlab + lane_piece * 8, a.d);
+    };
+    auto put_states = [&]() __attribute__((always_inline)) {
+        barrier();  // (lds_top is 0)
+        int at = 0;
+        for (;; fetch_states(at += kHalves)) {
+            const uint32_t top = largest_of_32(states.largest());
+            if (lane_piece == 31) atomicMax(&lds_top[row_of(min(at + (tid >> 5), all - 1))], top);
+            if (at + kHalves >= all) break;
         }
-    }
+        barrier();
+        for (;; fetch_states(at -= kHalves)) {
+            const int id = at + (tid >> 5), row = row_of(id);
+            if (id < all) {
+                float e[8];
+                states.values(e);
+                const Eight<HT> x(e, shift_of(lds_top[row]));
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    *reinterpret_cast<u32x4 *>(lds + p * plane + row * hpitch + (id - row * nslab) * (kSlab * 2) + lane_piece * 16) = x.part[p];
+            }
+            if (at == 0) break;
+        }
+    };
     // ---- or come from the image, a step ahead: global memory -> registers -> LDS
     u32x4 x[RESIDENT ? 1 : kPieces];
     const uint8_t *const image = RESIDENT ? nullptr : a.image + (int64_t)blockIdx.y * (NT * F * kFragment);
@@ -254,37 +323,21 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
             for (int i = 0; i < kPieces; ++i) {
                 const int id = i * kProductThreads + tid, s = id / (NT * F * 64), at = id - s * (NT * F * 64);
                 const int sl = step * KS + s < nslab ? step * KS + s : nslab - 1;
-                if (i + 1 < kPieces || kPieces * kProductThreads * 16 == kStage)
-                    x[i] = *reinterpret_cast<const u32x4 *>(image + sl * image_slab + at * 16);
-                else  // (the last pieces are for some of the threads)
-                    x[i] = *reinterpret_cast<const u32x4 *>(image + (s < KS ? sl * image_slab + at * 16 : 0));
+                x[i] = *reinterpret_cast<const u32x4 *>(image + sl * image_slab + at * 16);
             }
     };
     auto put_hidden = [&](int stage) __attribute__((always_inline)) {
         if constexpr (!RESIDENT)
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int at = (i * kProductThreads + tid) * 16;
-                if (at < kStage) *reinterpret_cast<u32x4 *>(lds + stage * kStage + at) = x[i];
-            }
+            for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4 *>(lds + stage * kStage + (i * kProductThreads + tid) * 16) = x[i];
     };
-    // fragment of step j of a half slab, or the sums of four groups
+    // fragment of step j of a half slab
     auto hidden = [&](int stage, int sl, int t, int p, int seg, int j) __attribute__((always_inline)) {
         if constexpr (RESIDENT)
-            return *reinterpret_cast<const bf16x8 *>(lds + p * plane + (v < rows_here ? v : 0) * hpitch + (sl * 32 + seg * 16 + piece_of<G>(j, kg)) * 16);
+            return *reinterpret_cast<const f16x8 *>(lds + p * plane + (v < rows_here ? v : 0) * hpitch + (sl * 32 + seg * 16 + piece_of<G>(j, kg)) * 16);
         else
-            return *reinterpret_cast<const bf16x8 *>(lds + stage * kStage + ((ks * NT + t) * F + p * 8 + seg * 4 + j) * kFragment + lane * 16);
+            return *reinterpret_cast<const f16x8 *>(lds + stage * kStage + ((ks * NT + t) * F + p * 8 + seg * 4 + j) * kFragment + lane * 16);
     };
-    auto hidden_sums = [&](int stage, int sl, int t, int q) __attribute__((always_inline)) {
-        if constexpr (RESIDENT) {
-            const int g = q * 4 + kg;
-            u32x2 m = lds_sum[(v < rows_here ? v : 0) * spitch + sl * kGroups + (g < kGroups ? g : 0)];
-            return __builtin_bit_cast(bf16x8, sum_slots(g < kGroups ? m : u32x2{0u, 0u}));
-        } else {
-            return *reinterpret_cast<const bf16x8 *>(lds + stage * kStage + ((ks * NT + t) * F + P * 8 + q) * kFragment + lane * 16);
-        }
-    };
-
     // ---- the head: registers, D steps ahead.  Rows of the workgroup by 32-bit offsets from its first.
     Int4Fetched slab[D][RB];
     const int pitch = (int)(a.m.K / 2), groups = (int)(a.m.K / G);
@@ -397,17 +450,19 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
             f32x4 part[RB][NT];
             static_for<4>([&](auto J) __attribute__((always_inline)) {
                 constexpr int j = decltype(J)::value, g = j / kSteps, js = j % kSteps, gs = seg * (128 / G) + g;  // step of the half, group, step of it
-                bf16x8 f[NT][P];
+                f16x8 f[NT][P];
                 static_for<NT * P>([&](auto I) __attribute__((always_inline)) {
                     constexpr int t = decltype(I)::value / P, p = decltype(I)::value % P;
                     f[t][p] = hidden(stage, sl, t, p, seg, j);
                 });
                 static_for<RB>([&](auto B) __attribute__((always_inline)) {
                     constexpr int b = decltype(B)::value;
-                    const bf16x8 c = code_values.of(w[b].w[seg * 4 + j]);
+                    f16x2 less = {(_Float16)-1032.0f, (_Float16)-1032.0f};
+                    if constexpr (ZEROS) less = w[b].template less<gs>();
+                    const f16x8 c = code_values.of(w[b].w[seg * 4 + j], less);
                     static_for<NT * P>([&](auto I) __attribute__((always_inline)) {
                         constexpr int t = decltype(I)::value / P, p = decltype(I)::value % P;
-                        part[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t][p], c, js == 0 && p == 0 ? zero : part[b][t], 0, 0, 0);
+                        part[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][p], c, js == 0 && p == 0 ? zero : part[b][t], 0, 0, 0);
                     });
                     if constexpr (js + 1 == kSteps) {
                         const float scale = gs < live ? w[b].template scale<gs>() : 0.0f;
@@ -417,26 +472,6 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
                             for (int r = 0; r < 4; ++r) acc[b][t][r] = __builtin_fmaf(scale, part[b][t][r], acc[b][t][r]);
                         });
                     }
-                });
-            });
-        });
-        // less s (16 + zero) times the groups' sums: lane (kg, v) has the scale of group kg (and 4 + kg) of the slab, lane (kg, n) its sum
-        static_for<kQuads>([&](auto Q) __attribute__((always_inline)) {
-            constexpr int q = decltype(Q)::value;
-            const int gs = q * 4 + kg;
-            const bool there = gs < (live < kGroups ? live : kGroups);
-            bf16x8 sums[NT];
-            static_for<NT>([&](auto TT) __attribute__((always_inline)) { sums[decltype(TT)::value] = hidden_sums(stage, sl, decltype(TT)::value, q); });
-            static_for<RB>([&](auto B) __attribute__((always_inline)) {
-                constexpr int b = decltype(B)::value;
-                const float scale = w[b].scale_of(q, kg);
-                const uint32_t z = ZEROS ? w[b].zero_of(q, kg) : 8u;
-                const float c = there ? -scale * (float)(16u + z) : 0.0f;
-                const uint32_t hi = __float_as_uint(c) & 0xFFFF0000u, lo = __float_as_uint(c - __uint_as_float(hi));
-                const bf16x8 cs = __builtin_bit_cast(bf16x8, u32x4{halves(hi, hi), halves(hi, lo), halves(lo, lo), 0u});
-                static_for<NT>([&](auto TT) __attribute__((always_inline)) {
-                    constexpr int t = decltype(TT)::value;
-                    acc[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sums[t], cs, acc[b][t], 0, 0, 0);
                 });
             });
         });
@@ -453,11 +488,12 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int n = t * 16 + kg * 4 + i;
+                    const float sum = ldexpf(acc[b][t][i], -shift_of(lds_top[n]));
                     if (in_pass && r < row_end && n < rows_here) {
                         if (a.f32_out)
-                            reinterpret_cast<float *>(a.out)[(n0 + n) * a.ld + row0 + r] = acc[b][t][i];
+                            reinterpret_cast<float *>(a.out)[(n0 + n) * a.ld + row0 + r] = sum;
                         else
-                            store_element<0>(reinterpret_cast<uint16_t *>(a.out) + (n0 + n) * a.ld + row0 + r, acc[b][t][i]);
+                            store_element<0>(reinterpret_cast<uint16_t *>(a.out) + (n0 + n) * a.ld + row0 + r, sum);
                     }
                     acc[b][t][i] = 0.0f;
                 }
@@ -482,12 +518,19 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
     };
 
     // Loads go out in the order of the loop below, from the start on, and stay in it: waits count what has gone out since.
+    if constexpr (RESIDENT) {
+        fetch_states(0);
+        if (tid < 16) lds_top[tid] = 0;
+    } else if (tid < NT * 16) {
+        lds_top[tid] = a.tops[n0 + tid];
+    }
     fetch_hidden(0);
     static_for<D>([&](auto U) __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
         fetch_head(slab[decltype(U)::value]);
     });
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (RESIDENT) put_states();
     put_hidden(0);
     int n_put = per > 1 ? 1 : 0;  // the next step to put in LDS
     fetch_hidden(n_put);
@@ -527,10 +570,10 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
 // sums do not depend on the rows beside it).
 static bool shared_slabs(int64_t V) { return (V + 15) / 16 < 1024; }
 // Whether N hidden states stay in LDS.
-static bool resident(int64_t N, int64_t K, int group, int parts)
+static bool resident(int64_t N, int64_t K, int parts)
 {
     const int64_t slabs = (K + kSlab - 1) / kSlab;
-    return N <= 16 && N * (parts * (slabs * kSlab * 2 + 16) + (slabs * (kSlab / group) + 2) * 8) <= kHiddenBytes;
+    return N <= 16 && N * parts * (slabs * kSlab * 2 + 16) <= kHiddenBytes;
 }
 
 template <int HT, bool RESIDENT, int NT, int KS, int RB, int D, int W>
@@ -545,8 +588,9 @@ static void run_product(Int4Product a, hipStream_t stream)
     auto run = [&](auto G) {
         constexpr int group = decltype(G)::value;
         if constexpr (!RESIDENT)
-            int4_image_kernel<HT, group><<<dim3(tiles * NT * 2, (unsigned)((a.m.K + kSlab - 1) / kSlab)), dim3(kBlock), 0, stream>>>(
-                (const typename Elem<HT>::type *)a.h, a.N, a.d, a.ldh, (int)(tiles * NT), const_cast<uint8_t *>(a.image));
+            int4_image_kernel<HT, group><<<dim3(tiles * NT * 16), dim3(kImageThreads), 0, stream>>>(
+                (const typename Elem<HT>::type *)a.h, a.N, a.d, a.ldh, (int)((a.m.K + kSlab - 1) / kSlab), (int)(tiles * NT),
+                const_cast<uint8_t *>(a.image), const_cast<uint32_t *>(a.tops));
         auto go = [&](auto ZEROS, auto PAST) {
             int4_product_kernel<HT, RESIDENT, NT, KS, group, decltype(ZEROS)::value, RB, D, W, decltype(PAST)::value>
                 <<<dim3((unsigned)grid, tiles), dim3(W * 64), 0, stream>>>(a);
@@ -586,22 +630,22 @@ __global__ __launch_bounds__(kBlock) void int4_short_kernel(Int4Product a)
 // Rows of hidden states whose image is made at once, and tiles of them that it holds.
 static int64_t image_rows(int64_t N) { return N < 1024 ? (N + 63) / 64 * 64 : 1024; }
 
-size_t int4_product_workspace_bytes(int64_t N, int64_t d, int dtype, int group)
+size_t int4_product_workspace_bytes(int64_t N, int64_t d, int dtype)
 {
     const int64_t K = (d + kInt4Slab - 1) / kInt4Slab * kInt4Slab;
     const int parts = dtype == 0 ? 1 : 3;
-    if (d < 8 || resident(N, K, group, parts)) return 0;
-    return (size_t)(image_rows(N) / 16 * ((K + kSlab - 1) / kSlab) * (parts * 8 + (kSlab / group + 3) / 4) * kFragment);
+    if (d < 8 || resident(N, K, parts)) return 0;
+    return (size_t)(kTopBytes + image_rows(N) / 16 * ((K + kSlab - 1) / kSlab) * (parts * 8) * kFragment);
 }
 
 int launch_int4_product(const void *h, int h_dtype, int64_t N, int64_t d, int64_t ldh, const Int4Matrix &m, void *out, int dtype, int64_t ld,
                         void *workspace, hipStream_t stream)
 {
     const int64_t most = 1024;  // rows of hidden states of a launch
-    const bool stay = resident(N, m.K, m.group, h_dtype == 0 ? 1 : 3), shared = shared_slabs(m.V);
+    const bool stay = resident(N, m.K, h_dtype == 0 ? 1 : 3), shared = shared_slabs(m.V);
     for (int64_t n = 0; n < N; n += most) {
         const Int4Product a{(const char *)h + n * ldh * (h_dtype == 0 ? 2 : 4), N - n < most ? N - n : most, d, ldh, m,
-                            (char *)out + n * ld * (dtype == 0 ? 2 : 4), ld, dtype != 0, 0, 0, (const uint8_t *)workspace};
+                            (char *)out + n * ld * (dtype == 0 ? 2 : 4), ld, dtype != 0, 0, 0, stay || !workspace ? nullptr : (const uint8_t *)workspace + kTopBytes, (const uint32_t *)workspace};
         if (d < 8) {
             const dim3 grid((unsigned)((m.V + kBlock - 1) / kBlock), (unsigned)((a.N + kShortRows - 1) / kShortRows));
             if (h_dtype == 0)

@@ -176,3 +176,91 @@ def test_a_quantised_head_gives_the_dense_products(difr):
     want = h.double().cpu() @ dense.double().cpu().t()
     got = difr.int4_product(h, q["codes"], q["scales"], q["zeros"], dtype=torch.float32)
     assert (got.cpu().double() - want).abs().max() < 1e-4 * want.abs().max()
+
+
+def _bound(h, w, group):
+    """Of fp32 accumulation: group + d / group + 8 additions, each off by up to 2^-23 (the matrix cores may cut) of what has been added up, and
+    states cut below 2^-39 of their row's largest: its scale is a power of two that brings it to 2^15 at least, and fp16 numbers end at 2^-24."""
+    h, size = h.double().abs(), h.double().abs() @ w.abs().t()
+    return size * (group + w.shape[1] // group + 9) * 2.0 ** -23 + h.amax(1, keepdim=True) * w.abs().sum(1) * 2.0 ** -39
+
+
+SOME = [(1, 3, 300, 8), (1, 100, 256, 128), (7, 17000, 300, 64), (16, 500, 1000, 32), (17, 300, 1030, 128), (33, 17000, 200, 32), (50, 17000, 130, 64), (64, 16500, 256, 128)]
+
+
+@pytest.mark.parametrize("N,V,d,group", [(n, v, d, max(g, 32)) for n, v, d, g in SOME])
+@pytest.mark.parametrize("zero_points", [False, True])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_codes_at_their_zero_points_add_nothing(difr, N, V, d, group, zero_points, hidden):
+    """Whatever the states: elements whose code is the zero point have the value 0.  All of them so: the sum is 0.  Those of channels that are much larger
+    than the others: what is lost of the others does not depend on them, beyond 2^-39."""
+    g = torch.Generator().manual_seed(N + V)
+    codes, scales, zeros, _ = _matrix(difr, V, d, group, zero_points, d)
+    K = difr.int4_padded(d)
+    z = (torch.full((V, K // group), 8, dtype=torch.uint8) if zeros is None else zeros.cpu()).repeat_interleave(group, 1)
+    h = (torch.randn(N, d, generator=g) * (4 * torch.randn(N, d, generator=g)).exp()).to(hidden)
+    none = (z[:, 0::2] | (z[:, 1::2] << 4)).to(DEV)
+    assert difr.int4_product(h.to(DEV), none, scales, zeros, dtype=torch.float32).eq(0).all()
+    c = torch.randint(0, 16, (V, K), generator=g, dtype=torch.uint8)
+    h = torch.randn(N, d, generator=g)
+    for k, times in ((5, 2.0 ** 13), (d // 2, -2.0 ** 10), (d - 1, 2.0 ** 16)):
+        h[:, k] = times * (1 + torch.rand(N, generator=g))
+        c[:, k] = z[:, k]
+    h = h.to(hidden)
+    w = ((c.double() - z.double()) * scales.cpu().double().repeat_interleave(group, 1))[:, :d]
+    got = difr.int4_product(h.to(DEV), (c[:, 0::2] | (c[:, 1::2] << 4)).to(DEV), scales, zeros, dtype=torch.float32)
+    assert ((got.cpu().double() - h.double() @ w.t()).abs() <= _bound(h, w, group)).all()
+
+
+@pytest.mark.parametrize("N,V,d,group", [(n, v, d, max(g, 32)) for n, v, d, g in SOME])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_states_of_every_size(difr, N, V, d, group, hidden):
+    """Rows near the ends of fp32, of one sign and of both, and rows whose elements differ by 2^30: as good as others."""
+    g = torch.Generator().manual_seed(N)
+    codes, scales, zeros, w = _matrix(difr, V, d, group, True, 3, lambda g, r, c: (torch.rand(r, c, generator=g) + 0.5) * 2.0 ** -12)
+    sizes = (2.0 ** 127, 2.0 ** 117, 1.0, 2.0 ** -60, 2.0 ** -110)
+    for first in range(0, len(sizes), N):
+        u = torch.rand(N, d, generator=g, dtype=torch.float64)
+        h = torch.stack([(u[n] + 0.25 if n % 2 else u[n] - 0.5) * sizes[(first + n) % len(sizes)] for n in range(N)])
+        h[:, ::7] *= 2.0 ** -30
+        h = h.to(hidden)
+        assert h.isfinite().all()
+        want = h.double() @ w.t()
+        want[want.abs() > torch.finfo(torch.float32).max] = math.nan                    # (infinities are right too)
+        got = difr.int4_product(h.to(DEV), codes, scales, zeros, dtype=torch.float32).cpu().double()
+        near = want.abs() > 2.0 ** 127
+        good = ((got - want).abs() <= _bound(h, w, group) + 2.0 ** -149) | want.isnan() | (near & ~got.isfinite())
+        assert good.all()
+
+
+@pytest.mark.parametrize("N,V,d,group", [(1, 1024, 256, 128), (9, 17000, 512, 128), (40, 2000, 640, 128)])
+@pytest.mark.parametrize("zero_points", [False, True])
+def test_fp32_states_are_summed_in_fp32(difr, N, V, d, group, zero_points):
+    """Normal weights, most of whose codes are near their zero points.  What the bound over all signs does not see: independent errors add as squares.  n = 2 (3 d / 32 + d / group) accumulations (a matrix instruction
+    for each part of 32 states, taken to round twice) of at most 2^-23 of the sum: sqrt(n) 2^-23 of it altogether."""
+    weights = torch.randn(V, d, generator=torch.Generator().manual_seed(11))
+    codes, scales, zeros, w = ref.int4(weights, group, zero_points)
+    codes, scales, zeros, w = codes.to(DEV), scales.to(DEV), None if zeros is None else zeros.to(DEV), w[:, :d]
+    h = torch.randn(N, d, generator=torch.Generator().manual_seed(4))
+    want = h.double() @ w.t()
+    got = difr.int4_product(h.to(DEV), codes, scales, zeros, dtype=torch.float32).cpu().double()
+    error = (got - want).square().mean().sqrt() / want.square().mean().sqrt()
+    assert error < math.sqrt(2 * (3 * d // 32 + d // group)) * 2.0 ** -23, float(error)
+
+
+@pytest.mark.parametrize("N,V,d,group", [(1, 100, 256, 128), (5, 17000, 300, 64), (33, 500, 1000, 32), (20, 17000, 130, 128)])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_small_states_beside_a_large_one(difr, N, V, d, group, hidden):
+    """A channel of 1 whose codes are the zero points, and others of up to 8 times 2^-31 (in fp16, scaled, numbers below the normal ones): exact, with
+    scales of 1, 2 and 4, as the sums are whole numbers below 2^24 times 2^-31."""
+    g = torch.Generator().manual_seed(V + d)
+    codes, scales, zeros, _ = _matrix(difr, V, d, group, True, 9, lambda g, r, c: 2.0 ** torch.randint(0, 3, (r, c), generator=g))
+    K = difr.int4_padded(d)
+    z = zeros.cpu().repeat_interleave(group, 1)
+    c = torch.randint(0, 16, (V, K), generator=g, dtype=torch.uint8)
+    c[:, 7] = z[:, 7]
+    h = torch.randint(-8, 9, (N, d), generator=g) * 2.0 ** -31
+    h[:, 7] = 1.0
+    w = ((c.double() - z.double()) * scales.cpu().double().repeat_interleave(group, 1))[:, :d]
+    got = difr.int4_product(h.to(hidden).to(DEV), (c[:, 0::2] | (c[:, 1::2] << 4)).to(DEV), scales, zeros, dtype=torch.float32)
+    assert torch.equal(got.cpu().double(), h.double() @ w.t())
