@@ -619,11 +619,12 @@ __global__ __launch_bounds__(kBlock) void int4_short_kernel(Int4Product a)
     for (int64_t n = n0; n < n0 + kShortRows && n < a.N; ++n) {
         const typename Elem<HT>::type *row = reinterpret_cast<const typename Elem<HT>::type *>(a.h) + n * a.ldh;
         float sum = 0.0f;
-        for (int k = 0; k < (int)a.d; ++k) sum = __builtin_fmaf((float)(w >> (4 * k) & 15u) - z, Elem<HT>::to_float(row[k]), sum);
+        // (a weight is exact in fp32)
+        for (int k = 0; k < (int)a.d; ++k) sum = __builtin_fmaf(s * ((float)(w >> (4 * k) & 15u) - z), Elem<HT>::to_float(row[k]), sum);
         if (a.f32_out)
-            reinterpret_cast<float *>(a.out)[n * a.ld + v] = s * sum;
+            reinterpret_cast<float *>(a.out)[n * a.ld + v] = sum;
         else
-            store_element<0>(reinterpret_cast<uint16_t *>(a.out) + n * a.ld + v, s * sum);
+            store_element<0>(reinterpret_cast<uint16_t *>(a.out) + n * a.ld + v, sum);
     }
 }
 

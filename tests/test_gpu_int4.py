@@ -264,3 +264,14 @@ def test_small_states_beside_a_large_one(difr, N, V, d, group, hidden):
     w = ((c.double() - z.double()) * scales.cpu().double().repeat_interleave(group, 1))[:, :d]
     got = difr.int4_product(h.to(hidden).to(DEV), (c[:, 0::2] | (c[:, 1::2] << 4)).to(DEV), scales, zeros, dtype=torch.float32)
     assert torch.equal(got.cpu().double(), h.double() @ w.t())
+
+
+@pytest.mark.parametrize("d", [1, 4, 7])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_short_states_of_every_size(difr, d, hidden):
+    """Fewer than eight elements, near the ends of fp32: d products and additions, each rounded once."""
+    codes, scales, zeros, w = _matrix(difr, 300, d, 32, True, 3, lambda g, r, c: (torch.rand(r, c, generator=g) + 0.5) * 2.0 ** -12)
+    h = (torch.rand(6, d, generator=torch.Generator().manual_seed(1), dtype=torch.float64) + 0.5) * torch.tensor([2.0 ** 127, -2.0 ** 126, 2.0 ** 120, 1.0, 2.0 ** -60, 2.0 ** -100])[:, None]
+    h = h.clamp(-3e38, 3e38).to(hidden)
+    got = difr.int4_product(h.to(DEV), codes, scales, zeros, dtype=torch.float32).cpu().double()
+    assert ((got - h.double() @ w.t()).abs() <= (h.double().abs() @ w.abs().t()) * d * 2.0 ** -24).all()
