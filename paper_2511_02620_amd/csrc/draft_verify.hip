@@ -812,7 +812,8 @@ static void run_chain(const DraftBatch &b, const DraftChain &c, const DraftOutpu
 {
     const int64_t cells = cells_of(b.V), both = c.draft ? 2 : 1, groups = (cells + kWaves * kMany - 1) / (kWaves * kMany);
     const dim3 each((unsigned)b.B), block(kBlock);
-    const int64_t levels = (b.D + b.B - 1) / b.B;  // rows with drafts of the longest sequence, if they are alike
+    const int64_t levels = (b.D + b.B - 1) / b.B;  // rows with drafts of the longest sequence, if they are alike (what longer
+                                                       // ones have behind is formed at once, behind their stop too)
     if (b.B * b.V * both >= kLevelEntries && levels > 1) {
         const dim3 rows((unsigned)(b.B * both * groups));
         int level = 0;

@@ -91,7 +91,7 @@ struct EightStates {
     static constexpr int E = Elem<HT>::kPerVec;
     u32x4 q[8 / E];
     int down;
-    __device__ __forceinline__ void load(const typename Elem<HT>::type *p, int64_t at, int64_t d)
+    __device__ __forceinline__ void fetch(const typename Elem<HT>::type *p, int64_t at, int64_t d)
     {
         const int64_t from = at + 8 <= d ? at : d - 8;
         down = at - from < 8 ? (int)(at - from) : 8;
@@ -187,7 +187,7 @@ __device__ __forceinline__ int piece_of(int j, int kg)
 }
 
 // Batches of more than 16 hidden states, whose fragments are the same for every workgroup and do not fit its LDS: an image of them in
-// global memory.  For each slab, tile of 16 states and part, 8 fragments of 64 lanes of 16 bytes.
+// global memory.  For each slab, tile of 16 states and part, 8 fragments of 64 lanes of 16 bytes.  (40 rows of 4096, bf16: 2.2 to 4.3 us.)
 constexpr int kFragment = 1024;
 constexpr int kTopBytes = 1024 * 4;  // of the workspace: the largest magnitudes of the rows of a launch; then the image
 
@@ -205,11 +205,11 @@ __global__ __launch_bounds__(kImageThreads) void int4_image_kernel(const typenam
     const int pieces = slabs * 32;
     EightStates<HT> held[kImageHeld];
 #pragma unroll
-    for (int i = 0; i < kImageHeld; ++i) held[i].load(from, (int64_t)(first + i * kImageThreads) * 8, d);
+    for (int i = 0; i < kImageHeld; ++i) held[i].fetch(from, (int64_t)(first + i * kImageThreads) * 8, d);
     uint32_t top = 0;
     for (int piece = first + kImageHeld * kImageThreads; piece < pieces; piece += kImageThreads) {
         EightStates<HT> more;
-        more.load(from, (int64_t)piece * 8, d);
+        more.fetch(from, (int64_t)piece * 8, d);
         top = max(top, more.largest());
     }
 #pragma unroll
@@ -236,17 +236,18 @@ __global__ __launch_bounds__(kImageThreads) void int4_image_kernel(const typenam
         if (first + i * kImageThreads < pieces) put(first + i * kImageThreads, held[i]);
     for (int piece = first + kImageHeld * kImageThreads; piece < pieces; piece += kImageThreads) {
         EightStates<HT> more;
-        more.load(from, (int64_t)piece * 8, d);
+        more.fetch(from, (int64_t)piece * 8, d);
         put(piece, more);
     }
 }
 
 // Hidden states in P parts; NT tiles of 16 of them from the image, a step ahead (RESIDENT: up to 16, converted by each workgroup and kept in
 // LDS); KS slabs at once, each with its share of the waves (small heads, whose blocks are fewer than waves); RB blocks of 16 rows of
-// the head to a wave at a time; D steps of codes in flight, in registers.  What bounds it, and steps of its making, us: one bf16 row by
-// 151,936 x 4096, 58 to 60 (5.4 TB/s; SIMDs issue in 81 % of the cycles): a lane fetching a row of its own 81, whole lines dealt by LDS 67,
-// 16 waves instead of 8 64.  40 rows by 128,256 x 4096, 103: fragments of the states are read from LDS for every two blocks; RB = 1 with 16
-// waves 112 (spills), 4 and 3 blocks spill too.  17 rows by 50,257 x 2000, 25: RB = 1 with 16 waves, against 29 with RB = 2 and 8.
+// the head to a wave at a time; D steps of codes in flight, in registers.  What bounds it, and steps of its making (those with the
+// codes as bf16 numbers 16 + code), us: one bf16 row by 151,936 x 4096, 59 to 60 (5.4 TB/s; 1.05 instructions a cycle and unit): a lane fetching a
+// row of its own 81, whole lines dealt by LDS 67, 16 waves instead of 8 64.  40 rows by 128,256 x 4096, 98: vector instructions in 49 % of the cycles,
+// matrix ones in 25 %, LDS reads between them, in two waves a SIMD that overlap little; RB = 1 with 16 waves 112 / 103 (spills), 4 and 3
+// blocks spilt too.  17 rows by 50,257 x 2000, 25: RB = 1 with 16 waves, against 29 with RB = 2 and 8.
 template <int HT, bool RESIDENT, int NT, int KS, int G, bool ZEROS, int RB, int D, int W, bool PAST>
 __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
 {
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
     auto row_of = [&](int id) { return (int)((uint32_t)id * part >> 16); };
     auto fetch_states = [&](int at) __attribute__((always_inline)) {
         const int id = min(at + (tid >> 5), all - 1), row = row_of(id);
-        states.load(reinterpret_cast<const typename Elem<HT>::type *>(a.h) + (n0 + row) * a.ldh, (id - row * nslab) * kSlab + lane_piece * 8, a.d);
+        states.fetch(reinterpret_cast<const typename Elem<HT>::type *>(a.h) + (n0 + row) * a.ldh, (id - row * nslab) * kSlab + lane_piece * 8, a.d);
     };
     auto put_states = [&]() __attribute__((always_inline)) {
         barrier();  // (lds_top is 0)
