@@ -245,8 +245,8 @@ __global__ __launch_bounds__(kImageThreads) void int4_image_kernel(const typenam
 // LDS); KS slabs at once, each with its share of the waves (small heads, whose blocks are fewer than waves); RB blocks of 16 rows of
 // the head to a wave at a time; D steps of codes in flight, in registers.  What bounds it, and steps of its making (those with the
 // codes as bf16 numbers 16 + code), us: one bf16 row by 151,936 x 4096, 59 to 60 (5.4 TB/s; 1.05 instructions a cycle and unit): a lane fetching a
-// row of its own 81, whole lines dealt by LDS 67, 16 waves instead of 8 64.  40 rows by 128,256 x 4096, 98: vector instructions in 49 % of the cycles,
-// matrix ones in 25 %, LDS reads between them, in two waves a SIMD that overlap little; RB = 1 with 16 waves 112 / 103 (spills), 4 and 3
+// row of its own 81, whole lines dealt by LDS 67, 16 waves instead of 8 64.  40 rows by 128,256 x 4096, 98: 0.49 vector instructions a cycle and
+// unit, matrix cores busy in 25 % of the cycles, LDS reads between them, in two waves a SIMD that overlap little; RB = 1 with 16 waves 112 / 103 (spills), 4 and 3
 // blocks spilt too.  17 rows by 50,257 x 2000, 25: RB = 1 with 16 waves, against 29 with RB = 2 and 8.
 template <int HT, bool RESIDENT, int NT, int KS, int G, bool ZEROS, int RB, int D, int W, bool PAST>
 __global__ __launch_bounds__(W * 64, 1) void int4_product_kernel(Int4Product a)
