@@ -275,3 +275,41 @@ def test_short_states_of_every_size(difr, d, hidden):
     h = h.clamp(-3e38, 3e38).to(hidden)
     got = difr.int4_product(h.to(DEV), codes, scales, zeros, dtype=torch.float32).cpu().double()
     assert ((got - h.double() @ w.t()).abs() <= (h.double().abs() @ w.abs().t()) * d * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("N,V,d", [(17, 100, 8), (33, 17000, 9), (40, 50, 100), (20, 17000, 127), (3, 100, 20000), (2, 17000, 8200), (17, 100, 8200), (20, 40, 20001), (7, 17000, 2049)])
+@pytest.mark.parametrize("group,zero_points", [(32, True), (64, True), (128, False)])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_short_and_long_states_are_exact(difr, N, V, d, group, zero_points, hidden):
+    """Half a slab and less, rows that end anywhere in it, and more elements than are kept while a row's largest is sought: whole numbers below
+    2^24 (20,001 elements * 15 * 4 * 8), so that nothing is rounded."""
+    codes, scales, zeros, w = _matrix(difr, V, d, group, zero_points, V + d, lambda g, r, c: 2.0 ** torch.randint(0, 3, (r, c), generator=g))
+    h = torch.randint(-8, 9, (N, d), generator=torch.Generator().manual_seed(N)).to(hidden)
+    h[0, d - 1], h[N - 1, 0] = 8, -8
+    got = difr.int4_product(_rows(h, 1, 3), codes, scales, zeros, dtype=torch.float32)
+    assert torch.equal(got.cpu().double(), h.double() @ w.t())
+
+
+@pytest.mark.parametrize("N", [3, 20, 70])
+@pytest.mark.parametrize("hidden", [torch.bfloat16, torch.float32])
+def test_products_captured_and_replayed(difr, N, hidden):
+    """Two graphs of one shape, replayed in turn with states of other sizes and eager calls between them."""
+    codes, scales, zeros, _ = _matrix(difr, 700, 640, 64, True, 5)
+    h = [torch.empty(N, 640, dtype=hidden, device=DEV) for _ in range(2)]
+    g = torch.Generator().manual_seed(8)
+    load = lambda size: [t.copy_(torch.randn(N, 640, generator=g) * size) for t in h]
+    step = lambda t: difr.int4_product(t, codes, scales, zeros, dtype=torch.float32)
+    load(1.0)
+    step(h[0])
+    torch.cuda.synchronize()
+    graphs, got = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for graph, t in zip(graphs, h):
+        with torch.cuda.graph(graph):
+            got.append(step(t))
+    for size in (1.0, 1e-20, 1e20, 3.0):
+        load(size)
+        want = [step(t) for t in h]
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and not torch.equal(got[0], got[1])
